@@ -17,7 +17,9 @@
  * and, from the same stages, tl_select_freq_binary (the controller's binary
  * search as the paper states it, querying the model only at probed
  * frequencies) and tl_admit (the admission control of Sec. 4.3.2 for one new
- * query per scenario).
+ * query per scenario).  Below them stands the machine that they plan: the paged
+ * cache whose blocks tl_project counts (tl_pages_*, tl_kv_append) and the
+ * attention over it (tl_attend).
  *
  * Conventions shared by every entry point
  *   - Pointers are DEVICE pointers (memory of the device that is current on
@@ -437,6 +439,180 @@ typedef struct tl_admit_args {
 } tl_admit_args;
 
 tl_status tl_admit(const tl_admit_args* args, void* stream);
+
+/* ------------------------------------------------------------------------
+ * The paged cache whose blocks tl_project counts (Sec. 4.2), and the
+ * attention that reads it: the part of an engine's iteration whose time goes
+ * with the batch and its KV blocks, which M is trained on (Sec. 4.3.1).
+ *
+ * A cache layer is a pool of n_pages pages of page_tokens tokens (the
+ * projection's blocks of N tokens).  Token t of sequence b is row t % N of
+ * page page_table[b][t / N]; length[b] tokens of b are in the cache.  A table
+ * entry outside [0, n_pages) has no page: such tokens are neither written nor
+ * seen.  Tokens past table_width * N do not exist, and a negative length is 0.
+ * Keys and values have the same layout: element d of token row r of head g of
+ * page p is at p * page_stride + g * head_stride + r * token_stride + d
+ * (elements), so pages may be [head][token] or [token][head].  Strides are
+ * multiples of 8 elements, pointers 16-byte aligned, and head_dim is a
+ * multiple of 8 of at most TL_MAX_HEAD_DIM.  Offsets are 64-bit.
+ *
+ * New tokens come as rows of a packed array: sequence b has the rows
+ * q_offset[b] .. q_offset[b+1]-1 (non-decreasing; clamped into [0, n_tokens]),
+ * or row b alone when q_offset is NULL (n_tokens == n_seqs).  They are the last
+ * ones of the sequence: with n rows, row i is at position length[b] - n + i
+ * (length counts them already); rows of a negative position are not written
+ * and see nothing.
+ * ---------------------------------------------------------------------- */
+#define TL_BF16 1
+#define TL_F16  2
+#define TL_MAX_HEAD_DIM 256
+
+typedef struct tl_kv_view {
+    uint32_t struct_size;          /* sizeof(tl_kv_view) */
+    int32_t dtype;                 /* TL_BF16 or TL_F16 */
+    int32_t n_kv_heads;            /* >= 1 */
+    int32_t head_dim;              /* D */
+    int32_t page_tokens;           /* N, 1 .. TL_MAX_BLOCK_TOKENS */
+    int32_t table_width;           /* entries per table row, >= 0 */
+    int64_t n_pages;               /* 0 .. 2^31-1 */
+    int64_t n_seqs;                /* B >= 0 */
+    int64_t page_stride;
+    int64_t head_stride;
+    int64_t token_stride;
+    void* key_pages;               /* written by tl_kv_append only */
+    void* value_pages;
+    const int32_t* page_table;     /* [B][table_width] */
+    const int32_t* length;         /* [B] */
+} tl_kv_view;
+
+/* New keys and values to their pages: row i of key and value (strides in
+ * elements between tokens and heads, multiples of 8) to its sequence's
+ * position.  A page that two rows write (a shared page: fork copies those) gets
+ * one of them. */
+typedef struct tl_kv_append_args {
+    uint32_t struct_size;          /* sizeof(tl_kv_append_args) */
+    uint32_t reserved;
+    tl_kv_view cache;
+    int64_t n_tokens;              /* T >= 0 */
+    const int64_t* q_offset;       /* [B+1]; NULL = one token each */
+    const void* key;               /* [T][n_kv_heads][D] */
+    const void* value;
+    int64_t key_token_stride, key_head_stride;
+    int64_t value_token_stride, value_head_stride;
+} tl_kv_append_args;
+
+tl_status tl_kv_append(const tl_kv_append_args* args, void* stream);
+
+/* Attention of the new tokens over their sequences' cached ones, the new ones
+ * included (append them first).  Query head h reads KV head h / (n_heads /
+ * n_kv_heads).  The token at position p sees the cached tokens t <= p, with
+ * window W > 0 only those with t > p - W or t < sinks (a sliding window and a few
+ * first tokens that stay visible):
+ *   out = sum_t w_t v_t,  w = softmax over the visible t of scale * (q . k_t)
+ *   lse = log sum_t exp(scale * (q . k_t))
+ * A row that sees no token, or whose scores are all -inf, gives zeros and lse
+ * -inf.  What lies in pages beyond the visible tokens, infinities and NaN
+ * included, is not used.  Rows that belong to no sequence are left alone.
+ *
+ * Scores, the softmax's maximum and sum and the output's sums are fp32.
+ * workspace: device memory of the caller, 16-byte aligned, for the parts of
+ * sequences that are split over their length and joined;
+ * tl_attend_workspace_bytes(args) says how much a call can use.  With less, or
+ * NULL, there are fewer parts (the same values up to rounding, in more time
+ * where there are few rows); for one workspace size the results are
+ * bit-identical from call to call.  A workspace serves one call at a time.
+ * max_length: an upper bound of length that the caller knows (0: table_width
+ * * N); it sizes the parts and limits nothing. */
+typedef struct tl_attend_args {
+    uint32_t struct_size;          /* sizeof(tl_attend_args) */
+    int32_t n_heads;               /* a multiple of cache.n_kv_heads */
+    tl_kv_view cache;
+    int64_t n_tokens;              /* T >= 0 */
+    const int64_t* q_offset;       /* [B+1]; NULL = one token each */
+    const void* query;             /* [T][n_heads][D], strides in elements (multiples of 8) */
+    int64_t query_token_stride, query_head_stride;
+    float scale;                   /* finite, > 0 */
+    int32_t window;                /* W >= 0; 0 = every earlier token */
+    int32_t sinks;                 /* >= 0 */
+    int32_t max_length;            /* 0 = unknown */
+    void* out;                     /* [T][n_heads][D], contiguous, of the cache's dtype */
+    float* lse;                    /* [T][n_heads]; NULL = not wanted */
+    void* workspace;               /* nullable */
+    uint64_t workspace_bytes;
+} tl_attend_args;
+
+tl_status tl_attend(const tl_attend_args* args, void* stream);
+uint64_t tl_attend_workspace_bytes(const tl_attend_args* args);   /* 0 for arguments that tl_attend refuses */
+
+/* ------------------------------------------------------------------------
+ * The pool's pages.  ref[p] (int32 [n_pages]) counts the table entries that
+ * hold page p; 0 = free.  Sequence slots are rows of page_table [n_slots]
+ * [table_width]; the first ceil(length / N) entries of a row are its pages.
+ * Free pages are taken in ascending order, so equal states give equal tables.
+ * All state is the caller's, on the device; the calls change it in place in
+ * stream order.  n_pages and n_slots are at most 2^31-1.
+ *
+ * Status per slot or fork, as the projection's queue decides: pages are given
+ * in order, and an entry whose pages do not fit behind all earlier ones' gets
+ * none (entries that need none are served all the same).
+ * ---------------------------------------------------------------------- */
+#define TL_PAGES_OK         0
+#define TL_PAGES_NONE_FREE  1   /* the pool has too few free pages                    */
+#define TL_PAGES_TABLE_FULL 2   /* more pages than table_width                        */
+#define TL_PAGES_BAD        3   /* malformed entry (see each call)                    */
+
+typedef struct tl_pages {
+    uint32_t struct_size;          /* sizeof(tl_pages) */
+    int32_t page_tokens;           /* N, 1 .. TL_MAX_BLOCK_TOKENS */
+    int64_t n_pages;
+    int64_t n_slots;
+    int32_t table_width;
+    int32_t reserved;
+    int32_t* ref;                  /* [n_pages] */
+    int32_t* page_table;           /* [n_slots][table_width] */
+    int32_t* length;               /* [n_slots] */
+} tl_pages;
+
+/* int32 words that `work` of the calls below has to hold. */
+uint64_t tl_pages_work_words(const tl_pages* pages);
+
+/* Room for add[b] more tokens in every slot b, in slot order: the pages
+ * behind its last one, ref 1, and length[b] += add[b].  TL_PAGES_BAD: add < 0
+ * or length < 0.  Slots that are not served keep their length. */
+tl_status tl_pages_extend(const tl_pages* pages, const int32_t* add, int32_t* status, int32_t* work, void* stream);
+
+/* Fork i makes the empty slot child[i] a copy of parent[i]: it shares the full
+ * pages (ref + 1) and gets a free page (ref 1) for a partly filled last one, which
+ * tl_pages_copy has to fill from copy_src[i] to copy_dst[i] (both -1 when there
+ * is nothing to copy).  So a page with room is only ever one sequence's.
+ * Lengths are those before the call.  TL_PAGES_BAD: a slot out of range or of
+ * negative length, child not empty, or an earlier fork's child; the child stays
+ * empty then, as with TL_PAGES_NONE_FREE. */
+tl_status tl_pages_fork(const tl_pages* pages, int64_t n_forks, const int32_t* parent, const int32_t* child,
+                        int32_t* copy_src, int32_t* copy_dst, int32_t* status, int32_t* work, void* stream);
+
+/* The slots leave: ref - 1 for each of their pages, length 0 (their table rows
+ * are left as they are).  Slots out of range are ignored. */
+tl_status tl_pages_free(const tl_pages* pages, int64_t n_free, const int32_t* slots, void* stream);
+
+/* With L pages in use, pages L and up move to the free ones below L, both in
+ * ascending order: copy_src[i] -> copy_dst[i] for i < *n_copies (each array has
+ * room for n_pages / 2 entries), which tl_pages_copy does.  ref_out and
+ * table_out (which may be pages->ref and pages->page_table) are the state
+ * after that; entries past a slot's pages are copied, an entry that holds a
+ * page nobody counts becomes -1. */
+tl_status tl_pages_compact(const tl_pages* pages, int32_t* ref_out, int32_t* table_out, int32_t* copy_src,
+                           int32_t* copy_dst, int32_t* n_copies, int32_t* work, void* stream);
+
+/* Page copy_src[i] to page copy_dst[i] in every one of n_planes planes (the
+ * layers' keys and values), for i < n_pairs, or i < *n_live (device, nullable;
+ * at most n_pairs).  Page p of plane q is page_bytes bytes at pages + q *
+ * plane_stride + p * page_stride (bytes; all multiples of 16, pages 16-byte
+ * aligned).  Pairs with an index outside [0, n_pages) are skipped.  No page may
+ * be both read and written. */
+tl_status tl_pages_copy(void* pages, int64_t n_pages, int64_t page_bytes, int64_t page_stride, int32_t n_planes,
+                        int64_t plane_stride, const int32_t* copy_src, const int32_t* copy_dst, int64_t n_pairs,
+                        const int32_t* n_live, void* stream);
 
 #ifdef __cplusplus
 }

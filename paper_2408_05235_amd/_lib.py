@@ -19,12 +19,17 @@ FLAG_BAD_REQUEST, FLAG_LOST, FLAG_OVERCOMMIT, FLAG_OVERFLOW, FLAG_UNSORTED = 1, 
 FLAG_BAD_CANDIDATE = 32
 STATUS_OK, STATUS_INFEASIBLE, STATUS_LOST, STATUS_INVALID = 0, 1, 2, 3
 ADMIT_OK, ADMIT_LOST, ADMIT_QUEUE_CAPACITY, ADMIT_QUEUE_TBT, ADMIT_QUEUE_E2E, ADMIT_INVALID = 0, 1, 2, 3, 4, 5
+BF16, F16 = 1, 2
+PAGES_OK, PAGES_NONE_FREE, PAGES_TABLE_FULL, PAGES_BAD = 0, 1, 2, 3
+MAX_HEAD_DIM = 256
 MAX_HORIZON, MAX_BLOCK_TOKENS, MAX_FREQS, MAX_FEATURES, MAX_DEPTH = 8192, 65536, 4096, 4, 14
 
 EXPORTED = ("tl_abi_version", "tl_last_error", "tl_forest_create", "tl_forest_destroy",
             "tl_project", "tl_forest_predict", "tl_forest_predict_grid", "tl_select_freq", "tl_admit",
             "tl_select_freq_binary", "tl_adjust_lengths", "tl_lattice_create", "tl_lattice_destroy",
-            "tl_lattice_bytes", "tl_lattice_predict_grid", "tl_forest_predict_grid_noalloc")
+            "tl_lattice_bytes", "tl_lattice_predict_grid", "tl_forest_predict_grid_noalloc",
+            "tl_kv_append", "tl_attend", "tl_attend_workspace_bytes", "tl_pages_work_words", "tl_pages_extend",
+            "tl_pages_fork", "tl_pages_free", "tl_pages_compact", "tl_pages_copy")
 
 
 class ProjectArgs(ctypes.Structure):
@@ -43,6 +48,37 @@ class AdmitArgs(ctypes.Structure):
         ("struct_size", u32), ("reserved", u32), ("proj", ProjectArgs), ("forest", P),
         ("max_freq_mhz", f32), ("engine_size", P), ("tbt_slo_ns", P), ("cand_prompt", P),
         ("cand_len", P), ("cand_deadline_ns", P), ("ips", P), ("decision", P), ("lattice", P),
+    ]
+
+
+class KvView(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", u32), ("dtype", i32), ("n_kv_heads", i32), ("head_dim", i32), ("page_tokens", i32),
+        ("table_width", i32), ("n_pages", i64), ("n_seqs", i64), ("page_stride", i64), ("head_stride", i64),
+        ("token_stride", i64), ("key_pages", P), ("value_pages", P), ("page_table", P), ("length", P),
+    ]
+
+
+class KvAppendArgs(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", u32), ("reserved", u32), ("cache", KvView), ("n_tokens", i64), ("q_offset", P), ("key", P),
+        ("value", P), ("key_token_stride", i64), ("key_head_stride", i64), ("value_token_stride", i64),
+        ("value_head_stride", i64),
+    ]
+
+
+class AttendArgs(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", u32), ("n_heads", i32), ("cache", KvView), ("n_tokens", i64), ("q_offset", P), ("query", P),
+        ("query_token_stride", i64), ("query_head_stride", i64), ("scale", f32), ("window", i32), ("sinks", i32),
+        ("max_length", i32), ("out", P), ("lse", P), ("workspace", P), ("workspace_bytes", ctypes.c_uint64),
+    ]
+
+
+class Pages(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", u32), ("page_tokens", i32), ("n_pages", i64), ("n_slots", i64), ("table_width", i32),
+        ("reserved", i32), ("ref", P), ("page_table", P), ("length", P),
     ]
 
 
@@ -98,6 +134,24 @@ def lib():
     L.tl_adjust_lengths.restype = ctypes.c_int
     L.tl_admit.argtypes = [ctypes.POINTER(AdmitArgs), P]
     L.tl_admit.restype = ctypes.c_int
+    L.tl_kv_append.argtypes = [ctypes.POINTER(KvAppendArgs), P]
+    L.tl_kv_append.restype = ctypes.c_int
+    L.tl_attend.argtypes = [ctypes.POINTER(AttendArgs), P]
+    L.tl_attend.restype = ctypes.c_int
+    L.tl_attend_workspace_bytes.argtypes = [ctypes.POINTER(AttendArgs)]
+    L.tl_attend_workspace_bytes.restype = ctypes.c_uint64
+    L.tl_pages_work_words.argtypes = [ctypes.POINTER(Pages)]
+    L.tl_pages_work_words.restype = ctypes.c_uint64
+    L.tl_pages_extend.argtypes = [ctypes.POINTER(Pages)] + [P] * 4
+    L.tl_pages_extend.restype = ctypes.c_int
+    L.tl_pages_fork.argtypes = [ctypes.POINTER(Pages), i64] + [P] * 7
+    L.tl_pages_fork.restype = ctypes.c_int
+    L.tl_pages_free.argtypes = [ctypes.POINTER(Pages), i64, P, P]
+    L.tl_pages_free.restype = ctypes.c_int
+    L.tl_pages_compact.argtypes = [ctypes.POINTER(Pages)] + [P] * 7
+    L.tl_pages_compact.restype = ctypes.c_int
+    L.tl_pages_copy.argtypes = [P, i64, i64, i64, i32, i64, P, P, i64, P, P]
+    L.tl_pages_copy.restype = ctypes.c_int
     _lib = L
     return L
 

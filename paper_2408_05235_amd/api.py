@@ -363,12 +363,267 @@ def tl_adjust_lengths(req_offset, generated, pred_len, scale_num, scale_den, max
     return rem
 
 
+_KV_DTYPES = {torch.bfloat16: _lib.BF16, torch.float16: _lib.F16}
+_VIEW_SIZE = ctypes.sizeof(_lib.KvView)
+
+
+def _strides(t):
+    """Strides, 0 where there is nothing to step over."""
+    return [0 if n <= 1 else s for n, s in zip(t.shape, t.stride())]
+
+
+def _rows3(t, dtype, name, heads=None, dim=None, tokens=None):
+    """Packed rows [tokens, heads, dim] with any token and head strides (a
+    view into a layer's fused product, say)."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name} must be [tokens, heads, head_dim] with contiguous heads")
+    want = (tokens, heads, dim)
+    if any(w is not None and w != g for w, g in zip(want, t.shape)):
+        raise ValueError(f"{name} must have shape {want}, got {tuple(t.shape)}")
+    return t
+
+
+def _kv_view(key_pages, value_pages, page_table, length):
+    if key_pages.dtype not in _KV_DTYPES:
+        raise ValueError(f"key_pages must be bfloat16 or float16, got {key_pages.dtype}")
+    if not key_pages.is_cuda or not value_pages.is_cuda:
+        raise ValueError("pages must be device tensors")
+    if key_pages.dim() != 4 or key_pages.shape != value_pages.shape or key_pages.dtype != value_pages.dtype:
+        raise ValueError("key_pages and value_pages must be [n_pages, n_kv_heads, page_tokens, head_dim] alike")
+    strides = _strides(key_pages)
+    if strides != _strides(value_pages) or strides[3] > 1:
+        raise ValueError("key_pages and value_pages must have the same strides and contiguous heads")
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be [n_seqs, table_width]")
+    n_pages, heads, tokens, dim = key_pages.shape
+    n_seqs, width = page_table.shape
+    _need(page_table, torch.int32, "page_table")
+    _need(length, torch.int32, "length", (n_seqs,))
+    return _lib.KvView(_VIEW_SIZE, _KV_DTYPES[key_pages.dtype], heads, dim, tokens, width, n_pages, n_seqs,
+                       strides[0], strides[1], strides[2], key_pages.data_ptr(), value_pages.data_ptr(),
+                       page_table.data_ptr(), length.data_ptr())
+
+
+def tl_kv_append(key, value, key_pages, value_pages, page_table, length, q_offset=None):
+    """New keys and values [T, n_kv_heads, head_dim] to their pages
+    (tl_kv_append).  Pages are [n_pages, n_kv_heads, page_tokens, head_dim]
+    with any strides (``x.transpose(1, 2)`` of token-major pages); page_table
+    [B, width] and length [B] int32, length with the new tokens; q_offset
+    [B + 1] int64, or None for one token per sequence."""
+    v = _kv_view(key_pages, value_pages, page_table, length)
+    T = key.shape[0]
+    _rows3(key, key_pages.dtype, "key", v.n_kv_heads, v.head_dim)
+    _rows3(value, key_pages.dtype, "value", v.n_kv_heads, v.head_dim, T)
+    _opt(q_offset, torch.int64, "q_offset", (v.n_seqs + 1,))
+    ks, vs = _strides(key), _strides(value)
+    a = _lib.KvAppendArgs(ctypes.sizeof(_lib.KvAppendArgs), 0, v, T, _p(q_offset), key.data_ptr(), value.data_ptr(),
+                          ks[0], ks[1], vs[0], vs[1])
+    check(lib().tl_kv_append(ctypes.byref(a), _stream()))
+
+
+def tl_attend(query, key_pages, value_pages, page_table, length, q_offset=None, window=0, sinks=0, scale=None,
+              max_length=0, out=None, want_lse=False, workspace=None):
+    """Attention of the new tokens' queries [T, n_heads, head_dim] over the
+    paged cache (tl_attend); the cache as in tl_kv_append, with the new tokens
+    already in it.  ``window`` 0 sees every earlier token, else the last
+    ``window`` and the first ``sinks``; ``scale`` is head_dim ** -0.5 unless
+    given; ``max_length`` is an upper bound of ``length`` where the caller
+    knows one.  ``workspace`` is an uint8 tensor (as many bytes as the call can
+    use are allocated when None).  Returns out [T, n_heads, head_dim], and the
+    log-sums [T, n_heads] fp32 too with ``want_lse``."""
+    v = _kv_view(key_pages, value_pages, page_table, length)
+    _rows3(query, key_pages.dtype, "query", None, v.head_dim)
+    T, heads, dim = query.shape
+    _opt(q_offset, torch.int64, "q_offset", (v.n_seqs + 1,))
+    if out is None:
+        out = torch.empty((T, heads, dim), dtype=query.dtype, device=query.device)
+    _need(out, query.dtype, "out", (T, heads, dim))
+    lse = torch.empty((T, heads), dtype=torch.float32, device=query.device) if want_lse else None
+    qs = _strides(query)
+    a = _lib.AttendArgs(ctypes.sizeof(_lib.AttendArgs), heads, v, T, _p(q_offset), query.data_ptr(), qs[0], qs[1],
+                        dim ** -0.5 if scale is None else float(scale), int(window), int(sinks), int(max_length),
+                        out.data_ptr(), _p(lse), None, 0)
+    if workspace is None:
+        n = lib().tl_attend_workspace_bytes(ctypes.byref(a))
+        if n:
+            workspace = torch.empty(n, dtype=torch.uint8, device=query.device)
+    elif workspace.dtype != torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 device tensor")
+    if workspace is not None:
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    check(lib().tl_attend(ctypes.byref(a), _stream()))
+    return (out, lse) if want_lse else out
+
+
+def _pages(ref, page_table, length, page_tokens, work):
+    _need(ref, torch.int32, "ref")
+    _need(page_table, torch.int32, "page_table")
+    if ref.dim() != 1 or page_table.dim() != 2:
+        raise ValueError("ref must be [n_pages] and page_table [n_slots, table_width]")
+    n_slots, width = page_table.shape
+    _need(length, torch.int32, "length", (n_slots,))
+    g = _lib.Pages(ctypes.sizeof(_lib.Pages), int(page_tokens), ref.numel(), n_slots, width, 0, _p(ref),
+                   _p(page_table), _p(length))
+    if work is None:
+        work = torch.empty(lib().tl_pages_work_words(ctypes.byref(g)), dtype=torch.int32, device=ref.device)
+    else:
+        _need(work, torch.int32, "work")
+        if work.numel() < lib().tl_pages_work_words(ctypes.byref(g)):
+            raise ValueError("work is too small (tl_pages_work_words)")
+    return g, work
+
+
+def tl_pages_extend(ref, page_table, length, add, page_tokens, status=None, work=None):
+    """Room for ``add`` [n_slots] int32 more tokens in every slot, in place
+    (tl_pages_extend).  Returns status [n_slots] int32 (PAGES_* codes)."""
+    g, work = _pages(ref, page_table, length, page_tokens, work)
+    _need(add, torch.int32, "add", (g.n_slots,))
+    if status is None:
+        status = torch.empty(g.n_slots, dtype=torch.int32, device=ref.device)
+    _need(status, torch.int32, "status", (g.n_slots,))
+    check(lib().tl_pages_extend(ctypes.byref(g), _p(add), _p(status), _p(work), _stream()))
+    return status
+
+
+def tl_pages_fork(ref, page_table, length, parent, child, page_tokens, work=None):
+    """Empty slots ``child`` become copies of slots ``parent`` (int32 [F]), in
+    place (tl_pages_fork).  Returns (copy_src, copy_dst, status) int32 [F]; the
+    pages still have to be copied (tl_pages_copy)."""
+    g, work = _pages(ref, page_table, length, page_tokens, work)
+    F = parent.numel()
+    _need(parent, torch.int32, "parent", (F,))
+    _need(child, torch.int32, "child", (F,))
+    src, dst, status = torch.empty((3, F), dtype=torch.int32, device=ref.device).unbind(0)
+    check(lib().tl_pages_fork(ctypes.byref(g), F, _p(parent), _p(child), _p(src), _p(dst), _p(status), _p(work),
+                              _stream()))
+    return src, dst, status
+
+
+def tl_pages_free(ref, page_table, length, slots, page_tokens):
+    """The sequences in ``slots`` (int32) leave, in place (tl_pages_free)."""
+    _need(slots, torch.int32, "slots")
+    _need(ref, torch.int32, "ref")
+    _need(page_table, torch.int32, "page_table")
+    n_slots, width = page_table.shape
+    _need(length, torch.int32, "length", (n_slots,))
+    g = _lib.Pages(ctypes.sizeof(_lib.Pages), int(page_tokens), ref.numel(), n_slots, width, 0, _p(ref),
+                   _p(page_table), _p(length))
+    check(lib().tl_pages_free(ctypes.byref(g), slots.numel(), _p(slots), _stream()))
+
+
+def tl_pages_compact(ref, page_table, length, page_tokens, out=None, work=None):
+    """The live pages to the front of the pool (tl_pages_compact).  Returns a
+    dict with the state after it (ref, page_table; taken from ``out``, which may
+    hold the arguments themselves, or allocated) and the moves (copy_src,
+    copy_dst, n_copies [1], all int32), which tl_pages_copy has to make."""
+    g, work = _pages(ref, page_table, length, page_tokens, work)
+    o = out or {}
+
+    def buf(name, shape):
+        t = o.get(name) if o.get(name) is not None else torch.empty(shape, dtype=torch.int32, device=ref.device)
+        return _need(t, torch.int32, name, shape)
+
+    half = ref.numel() // 2
+    r = dict(ref=buf("ref", (ref.numel(),)), page_table=buf("page_table", tuple(page_table.shape)),
+             copy_src=buf("copy_src", (half,)), copy_dst=buf("copy_dst", (half,)), n_copies=buf("n_copies", (1,)))
+    check(lib().tl_pages_compact(ctypes.byref(g), _p(r["ref"]), _p(r["page_table"]), _p(r["copy_src"]),
+                                 _p(r["copy_dst"]), _p(r["n_copies"]), _p(work), _stream()))
+    return r
+
+
+def tl_pages_copy(pages, copy_src, copy_dst, n_copies=None):
+    """Pages ``copy_src`` to ``copy_dst`` (int32) in every plane of ``pages``
+    [..., n_pages, n_kv_heads, page_tokens, head_dim] (contiguous; the leading
+    dimensions are planes); only the first ``n_copies`` (int32 [1], on the
+    device) when given (tl_pages_copy)."""
+    if not pages.is_cuda or not pages.is_contiguous() or pages.dim() < 4:
+        raise ValueError("pages must be a contiguous device tensor [..., n_pages, n_kv_heads, page_tokens, head_dim]")
+    n = copy_src.numel()
+    _need(copy_src, torch.int32, "copy_src", (n,))
+    _need(copy_dst, torch.int32, "copy_dst", (n,))
+    _opt(n_copies, torch.int32, "n_copies", (1,))
+    n_pages = pages.shape[-4]
+    page = pages.shape[-3] * pages.shape[-2] * pages.shape[-1] * pages.element_size()
+    planes = pages.numel() * pages.element_size() // (page * n_pages) if page * n_pages else 0
+    check(lib().tl_pages_copy(_p(pages), n_pages, page, page, planes, page * n_pages, _p(copy_src), _p(copy_dst), n,
+                              _p(n_copies), _stream()))
+
+
+class KVCache:
+    """A paged cache of ``n_layers`` layers and the sequences in its slots:
+    pages of ``page_tokens`` tokens, the page table, the lengths and the pages'
+    counts, all on the device.  One iteration of an engine extends the slots
+    by their new tokens, then appends and attends in every layer; finished
+    sequences are freed.  Nothing here waits for the device."""
+
+    def __init__(self, n_layers, n_pages, n_kv_heads, page_tokens, head_dim, n_slots, max_tokens,
+                 dtype=torch.bfloat16, device="cuda"):
+        if dtype not in _KV_DTYPES:
+            raise ValueError(f"dtype must be bfloat16 or float16, got {dtype}")
+        self.page_tokens, self.max_tokens = int(page_tokens), int(max_tokens)
+        width = -(-self.max_tokens // self.page_tokens)
+        i32 = dict(dtype=torch.int32, device=device)
+        self.pages = torch.empty((n_layers, 2, n_pages, n_kv_heads, page_tokens, head_dim), dtype=dtype, device=device)
+        self.ref = torch.zeros(n_pages, **i32)
+        self.page_table = torch.full((n_slots, width), -1, **i32)
+        self.length = torch.zeros(n_slots, **i32)
+        g = _lib.Pages(ctypes.sizeof(_lib.Pages), self.page_tokens, n_pages, n_slots, width, 0, _p(self.ref),
+                       _p(self.page_table), _p(self.length))
+        self.work = torch.empty(lib().tl_pages_work_words(ctypes.byref(g)), **i32)
+
+    def _state(self):
+        return self.ref, self.page_table, self.length
+
+    def extend(self, add, status=None):
+        """Room for ``add`` [n_slots] new tokens; returns the statuses."""
+        return tl_pages_extend(*self._state(), add, self.page_tokens, status, self.work)
+
+    def append(self, layer, key, value, q_offset=None):
+        """The new tokens' keys and values (after extend) into one layer."""
+        k, v = self.pages[layer]
+        tl_kv_append(key, value, k, v, self.page_table, self.length, q_offset)
+
+    def attend(self, layer, query, q_offset=None, **kw):
+        """The new tokens' attention over one layer (after append)."""
+        k, v = self.pages[layer]
+        return tl_attend(query, k, v, self.page_table, self.length, q_offset, **kw)
+
+    def fork(self, parent, child):
+        """Empty slots ``child`` become copies of ``parent``; returns the
+        statuses."""
+        src, dst, status = tl_pages_fork(*self._state(), parent, child, self.page_tokens, self.work)
+        tl_pages_copy(self.pages, src, dst)
+        return status
+
+    def free(self, slots):
+        """The sequences in ``slots`` leave."""
+        tl_pages_free(*self._state(), slots, self.page_tokens)
+
+    def compact(self):
+        """The live pages to the front of the pool; returns the number of
+        pages moved (int32 [1], on the device)."""
+        r = tl_pages_compact(*self._state(), self.page_tokens, dict(ref=self.ref, page_table=self.page_table),
+                             self.work)
+        tl_pages_copy(self.pages, r["copy_src"], r["copy_dst"], r["n_copies"])
+        return r["n_copies"]
+
+    def pages_used(self):
+        """Pages in use (int64 scalar, on the device)."""
+        return (self.ref > 0).sum()
+
+
 # short names
 project = tl_project
 select_freq = tl_select_freq
 select_freq_binary = tl_select_freq_binary
 admit = tl_admit
 adjust_lengths = tl_adjust_lengths
+kv_append = tl_kv_append
+attend = tl_attend
 
 
 def upload(inp, device="cuda"):

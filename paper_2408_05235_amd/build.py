@@ -15,9 +15,10 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_DIR = os.path.join(PKG, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "libtl.so")
-SOURCES = ["api.cpp", "host_forest.cpp", "project.hip", "forest.hip", "column.hip", "small.hip", "lattice.hip", "select.hip"]
+SOURCES = ["api.cpp", "host_forest.cpp", "project.hip", "forest.hip", "column.hip", "small.hip", "lattice.hip", "select.hip",
+           "cache_api.cpp", "pages.hip", "attend.hip"]
 HEADERS = ["device_util.h", "tl_internal.h", "forest_walk.h", "record_format.h", "host_forest.h", "queue_tries.h",
-           "scratch.h"]
+           "scratch.h", "status.h", "cache.h", "cache_rows.h"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

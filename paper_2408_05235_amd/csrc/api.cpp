@@ -13,6 +13,7 @@
 #include "device_util.h"
 #include "host_forest.h"
 #include "scratch.h"
+#include "status.h"
 #include "tl.h"
 #include "tl_internal.h"
 
@@ -38,6 +39,10 @@ namespace {
 
 thread_local char g_err[512] = "";
 
+}  // namespace
+
+namespace tl {
+
 tl_status fail(tl_status st, const char* fmt, ...) {
     va_list ap;
     va_start(ap, fmt);
@@ -55,6 +60,14 @@ tl_status from_hip(hipError_t e, const char* what) {
     if (e == hipSuccess) return ok();
     return fail(e == hipErrorOutOfMemory ? TL_ENOMEM : TL_EDEVICE, "%s: %s", what, hipGetErrorString(e));
 }
+
+}  // namespace tl
+
+namespace {
+
+using tl::fail;
+using tl::from_hip;
+using tl::ok;
 
 tl_status forest_create(int32_t n_trees, int32_t depth, int32_t n_features, float base_score, const uint8_t* feature,
                         const float* threshold, const float* leaf, tl_forest** out) {

@@ -1,0 +1,497 @@
+// The paged cache's pool: rows written to their pages, and pages given out,
+// shared, freed, moved together and copied.
+//
+// All of it is memory traffic and latency: no call computes more than
+// prefix sums of counts.  Free pages are listed by ballots in ascending order, so
+// that the tables do not depend on timing; the only atomics add to page
+// counts, whose sums do not depend on the order.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "cache.h"
+#include "cache_rows.h"
+#include "device_util.h"
+#include "tl_internal.h"
+
+namespace tl {
+namespace {
+
+constexpr int kAppendThreads = 256;
+constexpr int kAppendTokens = 16;       // most tokens of a workgroup
+
+// One workgroup moves `tokens` consecutive rows, 16 bytes per lane.
+__global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendParams P, int tokens) {
+    const CacheView& c = P.c;
+    __shared__ int64_t dst[kAppendTokens];
+    const int64_t first = (int64_t)blockIdx.x * tokens;
+    if ((int)threadIdx.x < tokens) {
+        const int64_t i = first + threadIdx.x;
+        int64_t at = -1, b;
+        if (i < c.n_tokens && find_seq(c, i, &b)) {
+            const SeqRows s = seq_rows(c, b);
+            const int64_t pos = (int64_t)s.length - s.n + (i - s.first);
+            if (i >= s.first && i - s.first < s.n && pos >= 0 && pos < table_tokens(c))
+                at = token_offset(c, c.table + b * c.table_width, (int32_t)pos);
+        }
+        dst[threadIdx.x] = at;
+    }
+    __syncthreads();
+    const int per_head = c.head_dim / 8;
+    const int per_row = c.n_kv_heads * per_head;
+    for (int x = threadIdx.x; x < tokens * per_row; x += kAppendThreads) {
+        const int r = x / per_row, y = x - r * per_row;
+        const int h = y / per_head, d = (y - h * per_head) * 8;
+        const int64_t at = dst[r];
+        if (at < 0) continue;
+        const int64_t to = at + (int64_t)h * c.head_stride + d;
+        const uint4 k = *(const uint4*)(P.src[0] + (first + r) * P.token_stride[0] + h * P.head_stride[0] + d);
+        const uint4 v = *(const uint4*)(P.src[1] + (first + r) * P.token_stride[1] + h * P.head_stride[1] + d);
+        *(uint4*)(c.key + to) = k;
+        *(uint4*)(c.value + to) = v;
+    }
+}
+
+constexpr int kPoolThreads = 1024;
+constexpr int kPoolWaves = kPoolThreads / kWave;
+constexpr int kBallots = 16;            // of 64 pages, per wavefront and step
+
+// Words of `work`: for the slots, what the calls note (three arrays), then for
+// the pages two arrays and the counts of blocks of 4096.
+__host__ __device__ inline int64_t work_list(const PagesParams& p) { return 3 * p.n_slots; }
+
+// The first `want` free pages in ascending order, to list[]; returns how many
+// free pages were seen (at least min(want, all)).  One workgroup of
+// kPoolThreads; each wavefront's ballots cover 1024 consecutive pages.
+__device__ int64_t list_free(const PagesParams& P, int64_t want, int32_t* list) {
+    __shared__ int32_t counts[2][kPoolWaves];
+    const int wave = threadIdx.x / kWave, lane = lane_id();
+    int64_t found = 0;
+    int parity = 0;
+    for (int64_t base = 0; base < P.n_pages && found < want; base += kPoolWaves * kBallots * kWave, parity ^= 1) {
+        const int64_t w0 = base + (int64_t)wave * kBallots * kWave;
+        int32_t r[kBallots];
+#pragma unroll
+        for (int i = 0; i < kBallots; ++i) {
+            const int64_t p = w0 + i * kWave + lane;
+            r[i] = p < P.n_pages ? P.ref[p] : 1;
+        }
+        uint64_t bits[kBallots];
+        int32_t n = 0;
+#pragma unroll
+        for (int i = 0; i < kBallots; ++i) {
+            bits[i] = __ballot(r[i] == 0);
+            n += __popcll(bits[i]);
+        }
+        if (lane == 0) counts[parity][wave] = n;
+        __syncthreads();
+        int32_t before = 0, all = 0;
+        for (int w = 0; w < kPoolWaves; ++w) {
+            before += w < wave ? counts[parity][w] : 0;
+            all += counts[parity][w];
+        }
+        int64_t rank = found + before;
+#pragma unroll
+        for (int i = 0; i < kBallots; ++i) {
+            const int64_t at = rank + __popcll(bits[i] & ((1ull << lane) - 1));
+            if ((bits[i] >> lane & 1) && at < want) list[at] = (int32_t)(w0 + i * kWave + lane);
+            rank += __popcll(bits[i]);
+        }
+        found += all;
+    }
+    __syncthreads();
+    return found;
+}
+
+// Sum of x over the lanes before this one and over earlier calls (`carry`,
+// uniform); one workgroup of kPoolThreads.
+__device__ int64_t running_sum(int64_t x, int64_t* carry) {
+    __shared__ uint64_t sums[kPoolWaves];
+    const int wave = threadIdx.x / kWave;
+    const uint64_t incl = wave_incl_scan_u64((uint64_t)x);
+    __syncthreads();                    // sums of the call before are read
+    if (lane_id() == kWave - 1) sums[wave] = incl;
+    __syncthreads();
+    uint64_t before = 0, all = 0;
+    for (int w = 0; w < kPoolWaves; ++w) {
+        before += w < wave ? sums[w] : 0;
+        all += sums[w];
+    }
+    const int64_t r = *carry + (int64_t)(before + incl) - x;
+    *carry += (int64_t)all;
+    return r;
+}
+
+__device__ __forceinline__ int32_t saturate(int64_t x) { return (int32_t)min(x, (int64_t)INT32_MAX); }
+
+// What slot b asks for: its pages now and after, and the status that does not
+// depend on the pool.
+struct Wish {
+    int64_t old_len, new_len;
+    int32_t have, need;
+    int32_t status;
+};
+
+__device__ __forceinline__ Wish wish(const PagesParams& P, int32_t length, int32_t add) {
+    Wish w;
+    w.old_len = length;
+    w.new_len = (int64_t)length + add;
+    w.status = TL_PAGES_OK;
+    w.have = w.need = 0;
+    const int64_t room = (int64_t)P.table_width * P.page_tokens;
+    if (length < 0 || add < 0) w.status = TL_PAGES_BAD;
+    else if (w.new_len > room || w.new_len > INT32_MAX) w.status = TL_PAGES_TABLE_FULL;
+    else {
+        w.have = (int32_t)((w.old_len + P.page_tokens - 1) / P.page_tokens);
+        w.need = (int32_t)((w.new_len + P.page_tokens - 1) / P.page_tokens) - w.have;
+    }
+    return w;
+}
+
+// One workgroup: (1) where each slot's pages begin among the free ones, (2)
+// the free pages, (3) page k to the slot that it falls to (found in the starts,
+// which are sorted), (4) lengths and statuses.
+__global__ __launch_bounds__(kPoolThreads) void extend_kernel(PagesParams P, const int32_t* add, int32_t* status,
+                                                              int32_t* work) {
+    int32_t* const starts = work;
+    int32_t* const list = work + work_list(P);
+    int64_t total = 0;
+    for (int64_t b0 = 0; b0 < P.n_slots; b0 += kPoolThreads) {
+        const int64_t b = b0 + threadIdx.x;
+        const int64_t n = b < P.n_slots ? wish(P, P.length[b], add[b]).need : 0;
+        const int64_t at = running_sum(n, &total);
+        if (b < P.n_slots) starts[b] = saturate(at);
+    }
+    const int64_t want = min(total, P.n_pages);
+    const int64_t found = min(list_free(P, want, list), P.n_pages);
+    for (int64_t k = threadIdx.x; k < min(want, found); k += kPoolThreads) {
+        int64_t lo = 0, hi = P.n_slots;     // starts[lo] <= k < starts[hi]
+        while (hi - lo > 1) {
+            const int64_t mid = (lo + hi) >> 1;
+            if (starts[mid] <= k) lo = mid;
+            else hi = mid;
+        }
+        const Wish w = wish(P, P.length[lo], add[lo]);
+        if (starts[lo] + (int64_t)w.need > found) continue;
+        const int32_t page = list[k];
+        P.table[lo * P.table_width + w.have + (k - starts[lo])] = page;
+        P.ref[page] = 1;
+    }
+    __syncthreads();
+    for (int64_t b = threadIdx.x; b < P.n_slots; b += kPoolThreads) {
+        const Wish w = wish(P, P.length[b], add[b]);
+        const bool fits = w.need == 0 || starts[b] + (int64_t)w.need <= found;
+        status[b] = w.status != TL_PAGES_OK ? w.status : fits ? TL_PAGES_OK : TL_PAGES_NONE_FREE;
+        if (w.status == TL_PAGES_OK && fits) P.length[b] = (int32_t)w.new_len;
+    }
+}
+
+// One workgroup decides the forks: validity (of several with one child the
+// first counts), which need a page, and which page that is.  lens[f]: the
+// child's length, -1 where the fork is not served.
+__global__ __launch_bounds__(kPoolThreads) void fork_kernel(PagesParams P, int64_t n_forks, const int32_t* parent,
+                                                            const int32_t* child, int32_t* copy_src,
+                                                            int32_t* copy_dst, int32_t* status, int32_t* work) {
+    int32_t* const claim = work;
+    int32_t* const lens = work + P.n_slots;
+    int32_t* const starts = work + 2 * P.n_slots;
+    int32_t* const list = work + work_list(P);
+    const int64_t room = (int64_t)P.table_width * P.page_tokens;
+    auto in_range = [&](int32_t s) { return s >= 0 && s < P.n_slots; };
+    for (int64_t f = threadIdx.x; f < n_forks; f += kPoolThreads)
+        if (in_range(child[f])) claim[child[f]] = INT32_MAX;
+    __threadfence();
+    __syncthreads();
+    for (int64_t f = threadIdx.x; f < n_forks; f += kPoolThreads)
+        if (in_range(child[f])) atomicMin(&claim[child[f]], (int32_t)f);
+    __threadfence();
+    __syncthreads();
+    int64_t total = 0;
+    for (int64_t f0 = 0; f0 < n_forks; f0 += kPoolThreads) {
+        const int64_t f = f0 + threadIdx.x;
+        int32_t len = -1;
+        if (f < n_forks && in_range(child[f]) && in_range(parent[f])) {
+            const int32_t first = __hip_atomic_load(&claim[child[f]], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            len = P.length[parent[f]];
+            if (first != f || P.length[child[f]] != 0 || len > room) len = -1;
+        }
+        const bool part = len > 0 && len % P.page_tokens != 0;
+        const int64_t at = running_sum(part, &total);
+        if (f < n_forks) {
+            lens[f] = max(len, -1);
+            starts[f] = saturate(at);
+        }
+    }
+    const int64_t want = min(total, P.n_pages);
+    const int64_t found = list_free(P, want, list);
+    for (int64_t f = threadIdx.x; f < n_forks; f += kPoolThreads) {
+        const int32_t len = lens[f];
+        int32_t src = -1, dst = -1, st = len < 0 ? TL_PAGES_BAD : TL_PAGES_OK;
+        if (len > 0 && len % P.page_tokens != 0) {
+            if (starts[f] < min(found, want)) {
+                src = P.table[(int64_t)parent[f] * P.table_width + len / P.page_tokens];
+                dst = list[starts[f]];
+                P.ref[dst] = 1;
+            } else {
+                st = TL_PAGES_NONE_FREE;
+                lens[f] = -1;
+            }
+        }
+        copy_src[f] = src;
+        copy_dst[f] = dst;
+        status[f] = st;
+    }
+}
+
+// A workgroup per fork: the child's row, the shared pages' counts, its length.
+__global__ __launch_bounds__(256) void fork_rows_kernel(PagesParams P, const int32_t* parent, const int32_t* child,
+                                                        const int32_t* copy_dst, const int32_t* work, int64_t first) {
+    const int64_t f = blockIdx.x + first;
+    const int32_t len = work[P.n_slots + f];
+    if (len < 0) return;
+    const int32_t full = len / P.page_tokens;
+    const int32_t* const from = P.table + (int64_t)parent[f] * P.table_width;
+    int32_t* const to = P.table + (int64_t)child[f] * P.table_width;
+    for (int32_t i = threadIdx.x; i < full; i += 256) {
+        const int32_t page = from[i];
+        to[i] = page;
+        if (page >= 0 && page < P.n_pages) atomicAdd(&P.ref[page], 1);
+    }
+    if (threadIdx.x == 0) {
+        if (len % P.page_tokens != 0) to[full] = copy_dst[f];
+        P.length[child[f]] = len;
+    }
+}
+
+// A workgroup per slot.  Whoever takes the length away frees the pages, so
+// that a slot named twice leaves once.
+__global__ __launch_bounds__(256) void free_kernel(PagesParams P, const int32_t* slots, int64_t first) {
+    __shared__ int32_t taken;
+    const int32_t slot = slots[blockIdx.x + first];
+    if (slot < 0 || slot >= P.n_slots) return;
+    if (threadIdx.x == 0) taken = atomicExch(&P.length[slot], 0);
+    __syncthreads();
+    const int64_t have = min(((int64_t)max(taken, 0) + P.page_tokens - 1) / P.page_tokens, (int64_t)P.table_width);
+    const int32_t* const row = P.table + (int64_t)slot * P.table_width;
+    for (int64_t i = threadIdx.x; i < have; i += 256) {
+        const int32_t page = row[i];
+        if (page >= 0 && page < P.n_pages) atomicSub(&P.ref[page], 1);
+    }
+}
+
+// ---- compaction: pages in blocks of kBlockPages, 256 threads each
+constexpr int kBlockPages = 4096;
+constexpr int kBlockWaves = 4;
+static_assert(kBlockPages == kBlockWaves * kBallots * kWave);
+__host__ __device__ inline int64_t page_blocks(const PagesParams& p) { return (p.n_pages + kBlockPages - 1) / kBlockPages; }
+
+// Of the work array's pages: what becomes of page p (kept: kStays; a page
+// that moves, or a free one that takes it: the move's number; else kUnused),
+// then the moved pages' counts, then the live pages of each block.
+constexpr int32_t kStays = -1, kUnused = -2;
+struct CompactWork {
+    int32_t* fate;
+    int32_t* moved_ref;
+    int32_t* counts;
+    int32_t* n_live;
+};
+__host__ __device__ inline CompactWork compact_work(const PagesParams& p, int32_t* work) {
+    CompactWork w;
+    w.fate = work + work_list(p);
+    w.moved_ref = w.fate + p.n_pages;
+    w.counts = w.moved_ref + p.n_pages / 2;
+    w.n_live = w.counts + page_blocks(p);
+    return w;
+}
+
+// Sum over the workgroup's 256 threads.
+__device__ int64_t block_sum(int64_t x) {
+    __shared__ uint64_t sums[kBlockWaves];
+    const uint64_t s = wave_sum_u64((uint64_t)x);
+    __syncthreads();
+    if (lane_id() == 0) sums[threadIdx.x / kWave] = s;
+    __syncthreads();
+    uint64_t all = 0;
+    for (int w = 0; w < kBlockWaves; ++w) all += sums[w];
+    return (int64_t)all;
+}
+
+__device__ __forceinline__ bool live(const PagesParams& P, int64_t p) { return p < P.n_pages && P.ref[p] > 0; }
+
+__global__ __launch_bounds__(256) void count_live_kernel(PagesParams P, int32_t* counts) {
+    const int64_t base = (int64_t)blockIdx.x * kBlockPages;
+    int64_t n = 0;
+    for (int i = threadIdx.x; i < kBlockPages; i += 256) n += live(P, base + i);
+    n = block_sum(n);
+    if (threadIdx.x == 0) counts[blockIdx.x] = (int32_t)n;
+}
+
+// With L live pages, `low` of them below L: a free page p < L has p - (live
+// pages before p) free ones before it, a live page p >= L has (live pages
+// before p) - low moving ones before it.  Equal numbers meet.
+__global__ __launch_bounds__(256) void plan_moves_kernel(PagesParams P, CompactWork W, int32_t* copy_src,
+                                                         int32_t* copy_dst, int32_t* n_copies) {
+    const int64_t blocks = page_blocks(P), mine = blockIdx.x;
+    int64_t n = 0, mine_before = 0;
+    for (int64_t k = threadIdx.x; k < blocks; k += 256) {
+        n += W.counts[k];
+        mine_before += k < mine ? W.counts[k] : 0;
+    }
+    const int64_t n_live = block_sum(n);
+    mine_before = block_sum(mine_before);
+    const int64_t edge = n_live / kBlockPages;
+    int64_t low = 0;
+    for (int64_t k = threadIdx.x; k < edge; k += 256) low += W.counts[k];
+    for (int64_t p = edge * kBlockPages + threadIdx.x; p < n_live; p += 256) low += live(P, p);
+    low = block_sum(low);
+    if (mine == 0 && threadIdx.x == 0) {
+        *n_copies = (int32_t)(n_live - low);
+        *W.n_live = (int32_t)n_live;
+    }
+    // the ranks of this block's pages
+    __shared__ int32_t counts[kBlockWaves];
+    const int wave = threadIdx.x / kWave, lane = lane_id();
+    const int64_t w0 = mine * kBlockPages + (int64_t)wave * kBallots * kWave;
+    uint64_t bits[kBallots];
+    int32_t own = 0;
+    for (int i = 0; i < kBallots; ++i) {
+        bits[i] = __ballot(live(P, w0 + i * kWave + lane));
+        own += __popcll(bits[i]);
+    }
+    if (lane == 0) counts[wave] = own;
+    __syncthreads();
+    int64_t before = mine_before;
+    for (int w = 0; w < wave; ++w) before += counts[w];
+    for (int i = 0; i < kBallots; ++i) {
+        const int64_t p = w0 + i * kWave + lane;
+        const bool is_live = bits[i] >> lane & 1;
+        const int64_t at = before + __popcll(bits[i] & ((1ull << lane) - 1));
+        before += __popcll(bits[i]);
+        if (p >= P.n_pages) continue;
+        int32_t fate = is_live ? kStays : kUnused;
+        if (is_live && p >= n_live) {
+            fate = (int32_t)(at - low);
+            copy_src[fate] = (int32_t)p;
+            W.moved_ref[fate] = P.ref[p];
+        } else if (!is_live && p < n_live) {
+            fate = (int32_t)(p - at);
+            copy_dst[fate] = (int32_t)p;
+        }
+        W.fate[p] = fate;
+    }
+}
+
+// The state after the moves.  Counts and table entries are each read and
+// written by one thread, so the new state may lie where the old one does.
+__global__ __launch_bounds__(256) void remap_kernel(PagesParams P, CompactWork W, const int32_t* copy_dst,
+                                                    int32_t* ref_out, int32_t* table_out) {
+    const int64_t step = (int64_t)gridDim.x * 256;
+    const int64_t me = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t n_live = *W.n_live;
+    for (int64_t p = me; p < P.n_pages; p += step) {
+        const int32_t fate = W.fate[p];
+        ref_out[p] = p >= n_live ? 0 : fate == kStays ? P.ref[p] : W.moved_ref[fate];
+    }
+    for (int64_t e = me; e < P.n_slots * P.table_width; e += step) {
+        const int64_t b = e / P.table_width, i = e - b * P.table_width;
+        const int32_t page = P.table[e];
+        int32_t to = page;
+        if (i * P.page_tokens < P.length[b] && page >= 0 && page < P.n_pages) {
+            const int32_t fate = W.fate[page];
+            to = page < n_live ? (fate == kStays ? page : -1) : fate >= 0 ? copy_dst[fate] : -1;
+        }
+        table_out[e] = to;
+    }
+}
+
+constexpr int kCopyThreads = 256;
+
+// A workgroup copies whole pages, 64 bytes per lane and step: four loads are
+// under way before the first store waits.
+__global__ __launch_bounds__(kCopyThreads) void copy_kernel(CopyParams P) {
+    int64_t pairs = P.n_pairs;
+    if (P.n_live) pairs = min(pairs, (int64_t)max(*P.n_live, 0));
+    const int64_t items = pairs * P.n_planes;
+    const int64_t n = P.page_bytes / 16;
+    for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+        const int64_t pair = it / P.n_planes, plane = it - pair * P.n_planes;
+        const int32_t s = P.src[pair], d = P.dst[pair];
+        if (s < 0 || s >= P.n_pages || d < 0 || d >= P.n_pages || s == d) continue;
+        unsigned char* const base = P.pages + plane * P.plane_stride;
+        const uint4* const from = (const uint4*)(base + s * P.page_stride);
+        uint4* const to = (uint4*)(base + d * P.page_stride);
+        for (int64_t i = threadIdx.x; i < n; i += 4 * kCopyThreads) {
+            uint4 x[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (i + q * kCopyThreads < n) x[q] = from[i + q * kCopyThreads];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (i + q * kCopyThreads < n) to[i + q * kCopyThreads] = x[q];
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_append(const AppendParams& p, hipStream_t stream) {
+    // few tokens: one a workgroup, so that they are spread over the chip
+    const int tokens = p.c.n_tokens < 4096 ? 1 : kAppendTokens;
+    const int64_t blocks = (p.c.n_tokens + tokens - 1) / tokens;
+    if (!grid_fits(blocks, kAppendThreads)) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL(append_kernel, dim3((unsigned)blocks), dim3(kAppendThreads), 0, stream, p, tokens);
+    return hipGetLastError();
+}
+
+uint64_t pages_work_words(const PagesParams& p) {
+    return (uint64_t)(work_list(p) + p.n_pages + p.n_pages / 2 + page_blocks(p) + 1);
+}
+
+hipError_t launch_pages_extend(const PagesParams& p, const int32_t* add, int32_t* status, int32_t* work,
+                               hipStream_t stream) {
+    hipLaunchKernelGGL(extend_kernel, dim3(1), dim3(kPoolThreads), 0, stream, p, add, status, work);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_fork(const PagesParams& p, int64_t n_forks, const int32_t* parent, const int32_t* child,
+                             int32_t* copy_src, int32_t* copy_dst, int32_t* status, int32_t* work,
+                             hipStream_t stream) {
+    hipLaunchKernelGGL(fork_kernel, dim3(1), dim3(kPoolThreads), 0, stream, p, n_forks, parent, child, copy_src,
+                       copy_dst, status, work);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    return launch_parts(n_forks, 256, [&](dim3 grid, int64_t first) {
+        hipLaunchKernelGGL(fork_rows_kernel, grid, dim3(256), 0, stream, p, parent, child, copy_dst, work, first);
+    });
+}
+
+hipError_t launch_pages_free(const PagesParams& p, int64_t n_free, const int32_t* slots, hipStream_t stream) {
+    return launch_parts(n_free, 256, [&](dim3 grid, int64_t first) {
+        hipLaunchKernelGGL(free_kernel, grid, dim3(256), 0, stream, p, slots, first);
+    });
+}
+
+hipError_t launch_pages_compact(const PagesParams& p, int32_t* ref_out, int32_t* table_out, int32_t* copy_src,
+                                int32_t* copy_dst, int32_t* n_copies, int32_t* work, hipStream_t stream) {
+    const CompactWork w = compact_work(p, work);
+    const unsigned blocks = (unsigned)std::max<int64_t>(page_blocks(p), 1);
+    hipLaunchKernelGGL(count_live_kernel, dim3(blocks), dim3(256), 0, stream, p, w.counts);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(plan_moves_kernel, dim3(blocks), dim3(256), 0, stream, p, w, copy_src, copy_dst, n_copies);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int64_t work_items = std::max<int64_t>(p.n_pages, p.n_slots * p.table_width);
+    const int64_t remap = std::min<int64_t>(std::max<int64_t>((work_items + 255) / 256, 1), 4096);
+    hipLaunchKernelGGL(remap_kernel, dim3((unsigned)remap), dim3(256), 0, stream, p, w, copy_dst, ref_out, table_out);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_copy(const CopyParams& p, hipStream_t stream) {
+    // eight workgroups of a CU at most, twice over
+    const int64_t blocks = std::min<int64_t>(p.n_pairs * p.n_planes, 256 * 16);
+    hipLaunchKernelGGL(copy_kernel, dim3((unsigned)blocks), dim3(kCopyThreads), 0, stream, p);
+    return hipGetLastError();
+}
+
+}  // namespace tl
