@@ -37,8 +37,11 @@ struct AttendParams {
     int64_t query_token_stride, query_head_stride;
     float scale;
     int32_t window, sinks;
+    int32_t max_length;             // 0 = unknown
     uint16_t* out;
     float* lse;                     // nullable
+    void* workspace;                // nullable
+    uint64_t workspace_bytes;
 };
 
 struct PagesParams {
@@ -61,6 +64,8 @@ struct CopyParams {
 
 hipError_t launch_append(const AppendParams& p, hipStream_t stream);
 hipError_t launch_attend(const AttendParams& p, hipStream_t stream);
+// Workspace bytes that launch_attend splits its work with.
+uint64_t attend_workspace_bytes(const AttendParams& p);
 
 // int32 words of `work` of the page calls.
 uint64_t pages_work_words(const PagesParams& p);

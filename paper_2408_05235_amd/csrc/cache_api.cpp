@@ -104,6 +104,10 @@ tl_status attend_params(const tl_attend_args* a, const char* who, tl::AttendPara
     p->sinks = a->sinks;
     p->out = (uint16_t*)a->out;
     p->lse = a->lse;
+    p->max_length = a->max_length;
+    p->workspace = a->workspace;
+    p->workspace_bytes = a->workspace ? a->workspace_bytes : 0;
+    if (p->c.n_pages == 0) p->c.table_width = 0;    // nothing is in the cache
     return TL_OK;
 }
 
@@ -176,7 +180,7 @@ tl_status tl_attend(const tl_attend_args* a, void* stream) {
 uint64_t tl_attend_workspace_bytes(const tl_attend_args* a) {
     tl::AttendParams p;
     if (!a || attend_params(a, "tl_attend_workspace_bytes", &p) != TL_OK) return 0;
-    return 0;
+    return tl::attend_workspace_bytes(p);
 }
 
 uint64_t tl_pages_work_words(const tl_pages* g) {
