@@ -19,107 +19,9 @@
 namespace tl {
 namespace {
 
-template <bool F16>
-__device__ __forceinline__ void load8(const uint16_t* p, float (&x)[8]) {
-    const uint4 v = *(const uint4*)p;
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[2 * i] = to_float<F16>((uint16_t)w[i]);
-        x[2 * i + 1] = to_float<F16>((uint16_t)(w[i] >> 16));
-    }
-}
-
-// One row by itself over the tokens of tiles v0 .. v1 - 1, as the definition
-// has it: a wavefront's halves take a token each in turn, 8 elements a lane.
-// The way of rows whose step holds values that are not finite and that only
-// some of its rows see, and where speed does not matter.
-struct RowSums {
-    float acc[8];           // of elements 8 (lane % 32) ..
-    float m, l;             // the maximum in log2 and the sum of weights
-};
-
-template <bool F16, int TILE>
-__device__ RowSums row_alone(const AttendParams& P, int64_t b, int64_t token, int32_t head, int32_t pos,
-                             const TileList& tiles, int32_t v0, int32_t v1, float score_scale) {
-    const CacheView& c = P.c;
-    const int lane = lane_id(), half = lane / 32, d = (lane & 31) * 8;
-    const bool in = d < c.head_dim;
-    RowSums r = {{}, kNone, 0.0f};
-    float q[8] = {};
-    if (in) load8<F16>(P.query + token * P.query_token_stride + (int64_t)head * P.query_head_stride + d, q);
-    const int32_t* const table_row = c.table + b * c.table_width;
-    const int64_t at0 = (int64_t)(head / P.group) * c.head_stride + d;
-    for (int32_t v = v0; v < v1; ++v) {
-#pragma unroll 1
-        for (int k = half; k < TILE; k += 2) {
-            const int64_t t = (int64_t)tiles.tile(v) * TILE + k;
-            const int64_t at = t < tiles.end && sees(P.window, P.sinks, pos, (int32_t)t)
-                                   ? token_offset(c, table_row, (int32_t)t) : -1;
-            float x[8] = {};
-            if (in && at >= 0) load8<F16>(c.key + at + at0, x);
-            float dot = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) dot = fmaf(q[e], x[e], dot);
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor(dot, o);
-            if (at < 0) continue;
-            const float sc = dot * score_scale;
-            const float m2 = fmaxf(r.m, sc);
-            const float keep = exp2_fast(r.m - m2), w = exp2_fast(sc - m2);
-            r.l = fmaf(r.l, keep, w);
-            if (in) load8<F16>(c.value + at + at0, x);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) r.acc[e] = fmaf(r.acc[e], keep, w * x[e]);
-            r.m = m2;
-        }
-    }
-    const float mo = __shfl_xor(r.m, 32), lo = __shfl_xor(r.l, 32);
-    const float m2 = fmaxf(r.m, mo), a = exp2_fast(r.m - m2), z = exp2_fast(mo - m2);
-    r.l = r.l * a + lo * z;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) r.acc[e] = r.acc[e] * a + __shfl_xor(r.acc[e], 32) * z;
-    r.m = m2;
-    return r;
-}
-
-constexpr int kRowWaves = 4;
-
-// Rows of sequences with more than `few` rows, a wavefront each.
-template <bool F16>
-__global__ __launch_bounds__(kRowWaves * kWave) void row_kernel(AttendParams P, int few, float score_scale) {
-    const CacheView& c = P.c;
-    const int64_t item = (int64_t)blockIdx.x * kRowWaves + threadIdx.x / kWave;
-    if (item >= c.n_tokens * P.n_heads) return;
-    const int64_t i = item / P.n_heads;
-    const int32_t h = (int32_t)(item - i * P.n_heads);
-    int64_t b;
-    if (!find_seq(c, i, &b)) return;
-    const SeqRows s = seq_rows(c, b);
-    if (i < s.first || i - s.first >= s.n) return;
-    if ((int64_t)s.n * P.group <= few) return;
-    const int32_t pos = s.length - s.n + (int32_t)(i - s.first);
-    const TileList tiles = visible_tiles<32>(c, P.window, P.sinks, pos, pos);
-    const RowSums y = row_alone<F16, 32>(P, b, i, h, pos, tiles, 0, tiles.count, score_scale);
-    const int lane = lane_id(), d = lane * 8;
-    if (lane < 32 && d < c.head_dim) {
-        uint16_t* const out = P.out + item * c.head_dim + d;
-        for (int e = 0; e < 8; ++e) out[e] = from_float<F16>(y.l == 0.0f ? 0.0f : y.acc[e] / y.l);
-        if (P.lse && d == 0) P.lse[item] = y.l == 0.0f ? -INFINITY : (y.m + log2f(y.l)) * kLn2;
-    }
-}
-
-constexpr int kFewRows = 16;
 constexpr int kFewWaves = 4;
 constexpr int kFewThreads = kFewWaves * kWave;
 constexpr int kFewTile = 32;            // tokens of a wavefront's step
-
-struct FewParams {
-    AttendParams a;
-    Parts parts;
-    int32_t row_tiles;                  // of a sequence and head, without q_offset
-    float score_scale;                  // scale x log2 e
-};
 
 __device__ __forceinline__ int64_t shuffle64(int64_t x, int lane) {
     const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)x, lane), hi = (uint32_t)__shfl((int)(x >> 32), lane);
@@ -137,7 +39,7 @@ __device__ __forceinline__ int64_t shuffle64(int64_t x, int lane) {
 //
 // DP: head_dim or the next of 64, 128, 256; pieces beyond head_dim are zero.
 template <bool F16, int DP, bool EXACT>
-__global__ __launch_bounds__(kFewThreads) void few_rows_kernel(FewParams F) {
+__global__ __launch_bounds__(kFewThreads) void few_rows_kernel(AttendLaunch F) {
     constexpr int kSteps = DP / 32;     // matrix instructions of a score
     constexpr int kPer = DP / 16;       // elements of a value row in a lane
     const AttendParams& P = F.a;
@@ -353,7 +255,8 @@ __global__ __launch_bounds__(kFewThreads) void few_rows_kernel(FewParams F) {
         const int32_t rr = row_tile * kFewRows + r, tok = rr / P.group;
         const int64_t to = (s.first + tok) * P.n_heads + kvh * P.group + (rr - tok * P.group);
         if (F.parts.count > 1) {
-            const int64_t slot = to * F.parts.count + part;
+            const int64_t slot =
+                (((b * F.row_tiles + row_tile) * c.n_kv_heads + kvh) * kFewRows + r) * F.parts.count + part;
             if (d < D && all != 0.0f) *(f32x4*)(F.parts.sums + slot * D + d) = o;
             if (d == 0) *(float2*)(F.parts.stats + slot * 2) = make_float2(top, all);
         } else {
@@ -366,130 +269,123 @@ __global__ __launch_bounds__(kFewThreads) void few_rows_kernel(FewParams F) {
     }
 }
 
-// A wavefront per row joins its parts in their order.
 template <bool F16>
-__global__ __launch_bounds__(kFewThreads) void join_kernel(FewParams F) {
+__global__ __launch_bounds__(kFewThreads) void join_few_kernel(AttendLaunch F) {
     const AttendParams& P = F.a;
-    const CacheView& c = P.c;
-    const int64_t r = (int64_t)blockIdx.x * kFewWaves + threadIdx.x / kWave;
-    if (r >= c.n_tokens * P.n_heads) return;
-    const int64_t i = r / P.n_heads;
-    int64_t b;
-    if (!find_seq(c, i, &b)) return;
-    const SeqRows s = seq_rows(c, b);
-    if (i < s.first || i - s.first >= s.n) return;
-    if (c.q_offset && (int64_t)s.n * P.group > kFewRows) return;
-    const int lane = lane_id(), n = F.parts.count, D = c.head_dim;
-    const float2* const st = (const float2*)F.parts.stats + r * n;
-    float top = kNone;
-    for (int k = lane; k < n; k += kWave) top = fmaxf(top, st[k].x);
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-    const float* const sums = F.parts.sums + r * n * D;
-    const int d = lane * 4;
-    float all = 0.0f;
-    f32x4 o = {0, 0, 0, 0};
-    for (int k = 0; k < n; ++k) {
-        const float2 y = st[k];
-        if (y.y == 0.0f) continue;      // an empty part: its sums are not written
-        const float f = exp2_fast(y.x - top);
-        all = fmaf(y.y, f, all);
-        if (d < D) {
-            const f32x4 v = *(const f32x4*)(sums + (int64_t)k * D + d);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = fmaf(v[e], f, o[e]);
-        }
-    }
-    const float f = all == 0.0f ? 0.0f : 1.0f / all;
-    if (all == 0.0f) o = f32x4{0, 0, 0, 0};
-    if (d < D) *(uint2*)(P.out + r * D + d) = make_uint2(pack2<F16>(o[0] * f, o[1] * f), pack2<F16>(o[2] * f, o[3] * f));
-    if (lane == 0 && P.lse) P.lse[r] = all == 0.0f ? -INFINITY : (top + log2f(all)) * kLn2;
+    const int64_t slot = (int64_t)blockIdx.x * kFewWaves + threadIdx.x / kWave;
+    int64_t x = slot / kFewRows;
+    const int32_t kvh = (int32_t)(x % P.c.n_kv_heads);
+    x /= P.c.n_kv_heads;
+    const int64_t b = x / F.row_tiles;
+    const SeqRows s = seq_rows(P.c, b);
+    const int64_t rows = (int64_t)s.n * P.group, row = x % F.row_tiles * kFewRows + slot % kFewRows;
+    if ((P.c.q_offset && rows > kFewRows) || row >= rows) return;
+    const int64_t token = row / P.group;
+    join_row<F16>(F, slot, (s.first + token) * P.n_heads + kvh * P.group + (row - token * P.group));
 }
 
 template <bool F16, int DP>
-void launch_few_dim(const FewParams& f, dim3 grid, hipStream_t stream) {
+void launch_few_dim(const AttendLaunch& f, dim3 grid, hipStream_t stream) {
     if (f.a.c.head_dim == DP) hipLaunchKernelGGL((few_rows_kernel<F16, DP, true>), grid, dim3(kFewThreads), 0, stream, f);
     else hipLaunchKernelGGL((few_rows_kernel<F16, DP, false>), grid, dim3(kFewThreads), 0, stream, f);
 }
 
 template <bool F16>
-void launch_few(const FewParams& f, dim3 grid, hipStream_t stream) {
+void launch_few(const AttendLaunch& f, dim3 grid, hipStream_t stream) {
     if (f.a.c.head_dim <= 64) launch_few_dim<F16, 64>(f, grid, stream);
     else if (f.a.c.head_dim <= 128) launch_few_dim<F16, 128>(f, grid, stream);
     else launch_few_dim<F16, 256>(f, grid, stream);
 }
 
-constexpr int64_t kPartAlign = 256;
-
-int64_t part_bytes(const AttendParams& p) {
-    const int64_t rows = p.c.n_tokens * p.n_heads;
-    return rows * (p.c.head_dim + 2) * (int64_t)sizeof(float);
-}
-
-// Row tiles of a sequence and head for the few-rows kernel.
+// Row tiles of a sequence and head for few_rows_kernel.
 int32_t few_row_tiles(const AttendParams& p) { return p.c.q_offset ? 1 : (p.group + kFewRows - 1) / kFewRows; }
+int64_t few_blocks(const AttendParams& p) { return p.c.n_seqs * p.c.n_kv_heads * few_row_tiles(p); }
 
-// How far the tokens of a sequence are split: into parts of at least
-// kMinPart tokens (a step of each wavefront) as long as there are fewer than
-// kFillBlocks workgroups, and of at most kMaxPart, so that a long sequence does
-// not end alone.
-constexpr int64_t kMinPart = kFewWaves * kFewTile, kMaxPart = 4096, kFillBlocks = 768, kMostParts = 256;
+// Which kernels a call needs, from what the host knows.
+bool needs_few(const AttendParams& p) { return p.group <= kFewRows || !p.c.q_offset; }
+bool needs_tiles(const AttendParams& p) { return p.c.q_offset && p.c.n_tokens * p.group > kFewRows; }
 
-int64_t wanted_parts(const AttendParams& p) {
+// How far the tokens of a sequence are split: as long as there are fewer
+// workgroups than fill the chip, into parts of at least `least` tokens, and
+// into parts of at most `most`.
+struct SplitRule {
+    int64_t fill, least, most;
+};
+// few_rows_kernel: three workgroups a CU; a step of each wavefront; and a
+// long sequence does not end alone.
+constexpr SplitRule kSplitFew = {768, kFewWaves * kFewTile, 4096};
+// tile_kernel: two workgroups a CU.
+constexpr SplitRule kSplitTiles = {512, 512, INT64_MAX};
+constexpr int64_t kMostParts = 256;
+
+int64_t wanted_parts(const AttendParams& p, const SplitRule& rule, int64_t blocks) {
     int64_t tokens = (int64_t)p.c.table_width * p.c.page_tokens;
     if (p.max_length > 0) tokens = std::min<int64_t>(tokens, p.max_length);
-    if (p.window > 0) tokens = std::min<int64_t>(tokens, (int64_t)p.window + p.sinks + kFewTile);
-    const int64_t blocks = p.c.n_seqs * p.c.n_kv_heads * few_row_tiles(p);
-    const int64_t fill = std::min((kFillBlocks + blocks - 1) / blocks, (tokens + kMinPart - 1) / kMinPart);
-    return std::max<int64_t>(1, std::min(std::max(fill, (tokens + kMaxPart - 1) / kMaxPart), kMostParts));
+    if (p.window > 0) tokens = std::min<int64_t>(tokens, (int64_t)p.window + p.sinks);
+    const int64_t fill = std::min((rule.fill + blocks - 1) / blocks, (tokens + rule.least - 1) / rule.least);
+    const int64_t n = std::max(fill, tokens / rule.most + (tokens % rule.most != 0));
+    return std::max<int64_t>(1, std::min(n, kMostParts));
+}
+
+constexpr int64_t kAlign = 256;
+int64_t aligned(int64_t bytes) { return (bytes + kAlign - 1) / kAlign * kAlign; }
+int64_t sums_bytes(const AttendParams& p, int64_t slots, int64_t parts) {
+    return aligned(slots * parts * p.c.head_dim * (int64_t)sizeof(float));
+}
+int64_t parts_bytes(const AttendParams& p, int64_t slots, int64_t parts) {
+    return parts > 1 ? sums_bytes(p, slots, parts) + aligned(slots * parts * 2 * (int64_t)sizeof(float)) : 0;
+}
+
+// Takes room for up to `want` parts from the workspace's front.
+Parts take_parts(AttendParams* p, const SplitRule& rule, int64_t slots, int64_t want) {
+    while (want > 1 && (uint64_t)parts_bytes(*p, slots, want) > p->workspace_bytes) --want;
+    Parts r = {(int32_t)want, (int32_t)rule.least, nullptr, nullptr};
+    if (want > 1) {
+        unsigned char* const at = (unsigned char*)p->workspace;
+        r.sums = (float*)at;
+        r.stats = (float*)(at + sums_bytes(*p, slots, want));
+        p->workspace = at + parts_bytes(*p, slots, want);
+        p->workspace_bytes -= (uint64_t)parts_bytes(*p, slots, want);
+    }
+    return r;
 }
 
 }  // namespace
 
 uint64_t attend_workspace_bytes(const AttendParams& p) {
     if (p.c.n_tokens == 0 || p.c.n_seqs == 0) return 0;
-    const int64_t n = wanted_parts(p);
-    return n > 1 ? (uint64_t)(n * part_bytes(p) + kPartAlign) : 0;
+    uint64_t n = 0;
+    if (needs_few(p))
+        n += (uint64_t)parts_bytes(p, few_blocks(p) * kFewRows, wanted_parts(p, kSplitFew, few_blocks(p)));
+    if (needs_tiles(p)) n += (uint64_t)parts_bytes(p, tile_slots(p), wanted_parts(p, kSplitTiles, tile_blocks(p)));
+    return n;
 }
 
 hipError_t launch_attend(const AttendParams& p, hipStream_t stream) {
-    FewParams f;
+    AttendLaunch f{};
     f.a = p;
     f.row_tiles = few_row_tiles(p);
     f.score_scale = p.scale * kLog2e;
-    int64_t n = wanted_parts(p);
-    if (p.workspace_bytes < (uint64_t)kPartAlign) n = 1;
-    else n = std::max<int64_t>(1, std::min<int64_t>(n, (int64_t)((p.workspace_bytes - kPartAlign) / part_bytes(p))));
-    int64_t tokens = (int64_t)p.c.table_width * p.c.page_tokens;
-    if (p.max_length > 0) tokens = std::min<int64_t>(tokens, p.max_length);
-    f.parts.count = (int32_t)n;
-    f.parts.tokens = (int32_t)kMinPart;
-    f.parts.sums = (float*)p.workspace;
-    f.parts.stats = nullptr;
-    if (n > 1) {
-        const int64_t sums = p.c.n_tokens * p.n_heads * n * p.c.head_dim * (int64_t)sizeof(float);
-        f.parts.stats = (float*)((unsigned char*)p.workspace + (sums + kPartAlign - 1) / kPartAlign * kPartAlign);
-    }
-    const int64_t few = p.c.n_seqs * p.c.n_kv_heads * f.row_tiles * n;
-    if (!grid_fits(few, kFewThreads)) return hipErrorInvalidConfiguration;
-    if (p.f16) launch_few<true>(f, dim3((unsigned)few), stream);
-    else launch_few<false>(f, dim3((unsigned)few), stream);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    const int64_t row_blocks = (p.c.n_tokens * p.n_heads + kRowWaves - 1) / kRowWaves;
-    if (!grid_fits(row_blocks, kFewThreads)) return hipErrorInvalidConfiguration;
-    if (n > 1) {
-        if (p.f16) hipLaunchKernelGGL((join_kernel<true>), dim3((unsigned)row_blocks), dim3(kFewThreads), 0, stream, f);
-        else hipLaunchKernelGGL((join_kernel<false>), dim3((unsigned)row_blocks), dim3(kFewThreads), 0, stream, f);
-        e = hipGetLastError();
+    if (needs_few(p)) {
+        const int64_t blocks = few_blocks(p);
+        f.parts = take_parts(&f.a, kSplitFew, blocks * kFewRows, wanted_parts(p, kSplitFew, blocks));
+        if (!grid_fits(blocks * f.parts.count, kFewThreads)) return hipErrorInvalidConfiguration;
+        const dim3 grid((unsigned)(blocks * f.parts.count)), block(kFewThreads);
+        if (p.f16) launch_few<true>(f, grid, stream);
+        else launch_few<false>(f, grid, stream);
+        hipError_t e = hipGetLastError();
+        if (e == hipSuccess && f.parts.count > 1) {
+            const dim3 joins((unsigned)(blocks * (kFewRows / kFewWaves)));
+            if (!grid_fits(joins.x, kFewThreads)) return hipErrorInvalidConfiguration;
+            if (p.f16) hipLaunchKernelGGL((join_few_kernel<true>), joins, block, 0, stream, f);
+            else hipLaunchKernelGGL((join_few_kernel<false>), joins, block, 0, stream, f);
+            e = hipGetLastError();
+        }
         if (e != hipSuccess) return e;
     }
-    if (p.c.q_offset) {
-        const dim3 grid((unsigned)row_blocks), block(kRowWaves * kWave);
-        if (p.f16) hipLaunchKernelGGL((row_kernel<true>), grid, block, 0, stream, p, kFewRows, f.score_scale);
-        else hipLaunchKernelGGL((row_kernel<false>), grid, block, 0, stream, p, kFewRows, f.score_scale);
-    }
-    return hipGetLastError();
+    if (!needs_tiles(p)) return hipSuccess;
+    f.parts = take_parts(&f.a, kSplitTiles, tile_slots(p), wanted_parts(p, kSplitTiles, tile_blocks(p)));
+    return launch_tiles(f, stream);
 }
 
 }  // namespace tl

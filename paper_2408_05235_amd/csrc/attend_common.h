@@ -60,6 +60,19 @@ __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 acc) {
                                                        acc, 0, 0, 0);
 }
 
+// acc + A B for A 32 x 16 and B 16 x 32: lane (i = lane % 32, g = lane / 32)
+// holds A[i][8g .. 8g + 7] and B[8g .. 8g + 7][i], and acc element e is row 8
+// (e / 4) + 4 g + e % 4 of column i.
+template <bool F16>
+__device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 acc) {
+    if constexpr (F16)
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), acc,
+                                                      0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b),
+                                                       acc, 0, 0, 0);
+}
+
 // The softmax's maximum before any score: finite, so that no difference of
 // two maxima is NaN; a score below it is -inf, whose weight is 0.
 constexpr float kNone = -FLT_MAX;
@@ -94,14 +107,127 @@ __device__ __forceinline__ bool sees(int32_t window, int32_t sinks, int32_t p, i
     return t <= p && (window == 0 || t > p - window || t < sinks);
 }
 
-// Where the parts of a split call go: per row (token x n_heads + head) and
-// part, first all sums [rows][parts][D], then (maximum in log2, sum of weights)
-// [rows][parts][2].
+// Where the parts of a split call go: per slot (a row of a workgroup) and
+// part, first all sums [slots][parts][D], then (maximum in log2, sum of weights)
+// [slots][parts][2].
 struct Parts {
     int32_t count;          // 1 = not split
     int32_t tokens;         // of a part, at least
     float* sums;
     float* stats;
 };
+
+// A launch of the attention's kernels.
+struct AttendLaunch {
+    AttendParams a;
+    Parts parts;
+    float score_scale;      // scale x log2 e
+    int32_t row_tiles;      // few_rows_kernel: of a sequence and head, without q_offset
+};
+
+// Sequences of up to so many rows (new tokens x query heads of a KV head) are
+// few_rows_kernel's, the others tile_kernel's.
+constexpr int kFewRows = 16;
+
+hipError_t launch_tiles(const AttendLaunch& f, hipStream_t stream);
+// Workgroups of launch_tiles per part, and slots of its parts.
+int64_t tile_blocks(const AttendParams& p);
+int64_t tile_slots(const AttendParams& p);
+
+template <bool F16>
+__device__ __forceinline__ void load8(const uint16_t* p, float (&x)[8]) {
+    const uint4 v = *(const uint4*)p;
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = to_float<F16>((uint16_t)w[i]);
+        x[2 * i + 1] = to_float<F16>((uint16_t)(w[i] >> 16));
+    }
+}
+
+// One row by itself over the tokens of tiles v0 .. v1 - 1, as the definition
+// has it: a wavefront's halves take a token each in turn, 8 elements a lane.
+// The way of rows whose step holds values that are not finite and that only
+// some of its rows see, and where speed does not matter.
+struct RowSums {
+    float acc[8];           // of elements 8 (lane % 32) ..
+    float m, l;             // the maximum in log2 and the sum of weights
+};
+
+template <bool F16, int TILE>
+__device__ RowSums row_alone(const AttendParams& P, int64_t b, int64_t token, int32_t head, int32_t pos,
+                             const TileList& tiles, int32_t v0, int32_t v1, float score_scale) {
+    const CacheView& c = P.c;
+    const int lane = lane_id(), half = lane / 32, d = (lane & 31) * 8;
+    const bool in = d < c.head_dim;
+    RowSums r = {{}, kNone, 0.0f};
+    float q[8] = {};
+    if (in) load8<F16>(P.query + token * P.query_token_stride + (int64_t)head * P.query_head_stride + d, q);
+    const int32_t* const table_row = c.table + b * c.table_width;
+    const int64_t at0 = (int64_t)(head / P.group) * c.head_stride + d;
+    for (int32_t v = v0; v < v1; ++v) {
+#pragma unroll 1
+        for (int k = half; k < TILE; k += 2) {
+            const int64_t t = (int64_t)tiles.tile(v) * TILE + k;
+            const int64_t at = t < tiles.end && sees(P.window, P.sinks, pos, (int32_t)t)
+                                   ? token_offset(c, table_row, (int32_t)t) : -1;
+            float x[8] = {};
+            if (in && at >= 0) load8<F16>(c.key + at + at0, x);
+            float dot = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dot = fmaf(q[e], x[e], dot);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor(dot, o);
+            if (at < 0) continue;
+            const float sc = dot * score_scale;
+            const float m2 = fmaxf(r.m, sc);
+            const float keep = exp2_fast(r.m - m2), w = exp2_fast(sc - m2);
+            r.l = fmaf(r.l, keep, w);
+            if (in) load8<F16>(c.value + at + at0, x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) r.acc[e] = fmaf(r.acc[e], keep, w * x[e]);
+            r.m = m2;
+        }
+    }
+    const float mo = __shfl_xor(r.m, 32), lo = __shfl_xor(r.l, 32);
+    const float m2 = fmaxf(r.m, mo), a = exp2_fast(r.m - m2), z = exp2_fast(mo - m2);
+    r.l = r.l * a + lo * z;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r.acc[e] = r.acc[e] * a + __shfl_xor(r.acc[e], 32) * z;
+    r.m = m2;
+    return r;
+}
+
+// A wavefront joins the parts of a slot, in their order, to output row `to`
+// (token x n_heads + head).
+template <bool F16>
+__device__ __forceinline__ void join_row(const AttendLaunch& F, int64_t slot, int64_t to) {
+    const AttendParams& P = F.a;
+    const int lane = lane_id(), n = F.parts.count, D = P.c.head_dim;
+    const float2* const st = (const float2*)F.parts.stats + slot * n;
+    float top = kNone;
+    for (int k = lane; k < n; k += kWave) top = fmaxf(top, st[k].x);
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+    const float* const sums = F.parts.sums + slot * n * D;
+    const int d = lane * 4;
+    float all = 0.0f;
+    f32x4 o = {0, 0, 0, 0};
+    for (int k = 0; k < n; ++k) {
+        const float2 y = st[k];
+        if (y.y == 0.0f) continue;      // an empty part: its sums are not written
+        const float f = exp2_fast(y.x - top);
+        all = fmaf(y.y, f, all);
+        if (d < D) {
+            const f32x4 v = *(const f32x4*)(sums + (int64_t)k * D + d);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(v[e], f, o[e]);
+        }
+    }
+    const float f = all == 0.0f ? 0.0f : 1.0f / all;
+    if (all == 0.0f) o = f32x4{0, 0, 0, 0};
+    if (d < D) *(uint2*)(P.out + to * D + d) = make_uint2(pack2<F16>(o[0] * f, o[1] * f), pack2<F16>(o[2] * f, o[3] * f));
+    if (lane == 0 && P.lse) P.lse[to] = all == 0.0f ? -INFINITY : (top + log2f(all)) * kLn2;
+}
 
 }  // namespace tl
