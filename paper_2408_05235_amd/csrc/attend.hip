@@ -314,8 +314,8 @@ struct SplitRule {
 // few_rows_kernel: three workgroups a CU; a step of each wavefront; and a
 // long sequence does not end alone.
 constexpr SplitRule kSplitFew = {768, kFewWaves * kFewTile, 4096};
-// tile_kernel: two workgroups a CU.
-constexpr SplitRule kSplitTiles = {512, 512, INT64_MAX};
+// tile_kernel: a workgroup a CU.
+constexpr SplitRule kSplitTiles = {256, 512, INT64_MAX};
 constexpr int64_t kMostParts = 256;
 
 int64_t wanted_parts(const AttendParams& p, const SplitRule& rule, int64_t blocks) {

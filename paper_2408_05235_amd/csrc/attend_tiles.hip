@@ -19,25 +19,28 @@
 namespace tl {
 namespace {
 
-constexpr int kTileWaves = 4;
-constexpr int kTileThreads = kTileWaves * kWave;
 constexpr int kWaveRows = 32;
-constexpr int kTileRows = kTileWaves * kWaveRows;       // rows of a workgroup
-constexpr int kKeys = 64;                               // cached tokens of a step
+constexpr int kKeys = 64;               // cached tokens of a step
+// Wavefronts and rows of a workgroup: two wavefronts a SIMD where their
+// registers allow it.
+constexpr int tile_waves(int head_dim) { return head_dim > 128 ? 4 : 8; }
+constexpr int tile_rows(int head_dim) { return tile_waves(head_dim) * kWaveRows; }
 
 // Row tiles are numbered through the batch with gaps: sequence b's begin at
-// floor(q_offset[b] x group / kTileRows) + b, which leaves room for all of
-// them, and needs no sum over the batch.
+// floor(q_offset[b] x group / ROWS) + b, which leaves room for all of them, and
+// needs no sum over the batch.
+template <int ROWS>
 __device__ __forceinline__ int64_t first_tile(const AttendParams& P, int64_t b) {
-    return clamp_offset(P.c, P.c.q_offset[b]) * P.group / kTileRows + b;
+    return clamp_offset(P.c, P.c.q_offset[b]) * P.group / ROWS + b;
 }
 
 // The last sequence whose first tile is at most `tile`: 64 ways at a time.
+template <int ROWS>
 __device__ __forceinline__ int64_t tile_seq(const AttendParams& P, int64_t tile) {
     int64_t lo = 0, hi = P.c.n_seqs;
     while (hi - lo > 1) {
         const int64_t step = (hi - lo + kWave - 1) / kWave, at = lo + lane_id() * step;
-        const bool below = at < hi && first_tile(P, at) <= tile;
+        const bool below = at < hi && first_tile<ROWS>(P, at) <= tile;
         const int k = max(__popcll(__ballot(below)) - 1, 0);
         lo += k * step;
         hi = min(lo + step, hi);
@@ -45,35 +48,99 @@ __device__ __forceinline__ int64_t tile_seq(const AttendParams& P, int64_t tile)
     return lo;
 }
 
-// 128 rows of one sequence and KV head over one part of its tokens, 32 rows a
-// wavefront.  The products run as K Q^T and V^T P^T (32 x 32 matrix instructions), so
-// that a lane keeps one row (lane % 32) throughout: scores, weights, maximum and
-// sums; the first product's result is the second's operand as it lies: in both,
-// lane group g = lane / 32 has the tokens 4 g .. 4 g + 3 and 8 + 4 g .. of
-// each 16.  Keys are staged in LDS row by row and values turned, in that order of
-// tokens; 16-byte pieces are exchanged (xor) so that neither the writes nor the
-// reads of a piece by 8 lanes meet in a bank.  While a step is computed the next
-// one's keys and values are under way in registers, and the one after that is
-// looked up in the page table.
+// One piece: lane l copies the 16 bytes at its `src` to LDS address lds + 16 l
+// (lds the same in every lane), straight from memory.  An instruction that the
+// compiler does not track, so that reads of the other buffer do not wait for
+// it; `settle` waits for the copies (vmcnt) before a barrier hands them over.
+__device__ __forceinline__ void copy_piece(const uint16_t* src, uint32_t lds) {
+    const uint32_t to = __builtin_amdgcn_readfirstlane(lds);
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(src) : "memory", "m0");
+}
+
+// The same for 4 bytes a lane.
+__device__ __forceinline__ void copy_words(const int32_t* src, uint32_t lds) {
+    const uint32_t to = __builtin_amdgcn_readfirstlane(lds);
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(src) : "memory", "m0");
+}
+
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+
+// Four 16-bit words of a column: within 16 lanes, lane i gives the address of
+// 4 words of row i / 4 (of 4 rows x 16 words) and takes column i.
+__device__ __forceinline__ uint2 read_column4(const void* lds) {
+    typedef __attribute__((ext_vector_type(4))) short s16x4;
+    return __builtin_bit_cast(uint2,
+                              __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)lds));
+}
+
+// The value of the lane 32 away.
+__device__ __forceinline__ float other_half(float x) {
+    typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+    const uint32_t b = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    return __builtin_bit_cast(float, lane_id() < 32 ? r[1] : r[0]);
+}
+
+// Bits 0 .. k of 64 (none for k < 0).
+__device__ __forceinline__ uint64_t bits_to(int32_t k) { return k < 0 ? 0 : ~0ull >> (63 - min(k, 63)); }
+
+// The tokens t0 .. t0 + 63 that a row at position p sees.
+__device__ __forceinline__ uint64_t seen_bits(int32_t window, int32_t sinks, int32_t p, int32_t t0) {
+    uint64_t r = bits_to(p - t0);
+    if (window > 0) r &= ~bits_to(p - window - t0) | bits_to(sinks - 1 - t0);
+    return r;
+}
+
+// What the piece numbers of a token's row are exchanged with: the same piece of
+// 16 consecutive tokens lies in 16 places of the 256 bytes that the banks
+// hold (keys), and so do 4 consecutive pieces of 4 (values).
+template <int PIECES>
+__device__ __forceinline__ int key_exchange(int token) {
+    return PIECES > 8 ? token & 15 : token >> 1 & 7;
+}
+template <int PIECES>
+__device__ __forceinline__ int value_exchange(int token) {
+    return PIECES > 8 ? (token & 3) << 2 : (token >> 1 & 1) << 2;
+}
+
+// 256 rows (128 for head_dim > 128) of one sequence and KV head over one part
+// of its tokens, 32 rows a wavefront.  The products run as K Q^T and V^T P^T
+// (32 x 32 matrix instructions), so that a lane keeps one row (lane % 32)
+// throughout: scores, weights, maximum and sums; the first product's result is
+// the second's operand as it lies: in both, lane group g = lane / 32 has the
+// tokens 4 g .. 4 g + 3 and 8 + 4 g .. of each 16.  Keys and values go from memory
+// straight to LDS, token by token; the values are turned when they are read.
+// 16-byte pieces of a token's row are exchanged (xor) so that the lanes that read
+// together meet in no bank.
+//
+// A step (64 tokens) has a matrix phase, the last step's V^T P^T and this
+// one's K Q^T, and a softmax phase, which take about as long.  The two wavefronts of
+// a SIMD are a phase apart, a barrier after each phase keeps them so: one's matrix
+// instructions run under the other's softmax.  Keys of the next step and this
+// one's values are copied meanwhile, and the step after is looked up in the page
+// table.
 template <bool F16, int DP, bool EXACT>
-__global__ __launch_bounds__(kTileThreads, DP > 128 ? 1 : 2) void tile_kernel(AttendLaunch F) {
+__global__ __launch_bounds__(tile_waves(DP) * kWave, DP > 128 ? 1 : 2) void tile_kernel(AttendLaunch F) {
+    constexpr int kTileWaves = tile_waves(DP), kTileThreads = kTileWaves * kWave, kTileRows = tile_rows(DP);
     constexpr int kSteps = DP / 16;                     // matrix instructions of a score
     constexpr int kBlocks = DP / 32;                    // of 32 elements of the output
     constexpr int kPieces = DP / 8;                     // 16-byte pieces of a row
-    constexpr int kKeyLoads = kKeys * kPieces / kTileThreads;       // pieces a thread stages
-    constexpr int kQuads = kKeys / 4 * kPieces / kTileThreads;      // 4 tokens x 8 elements it turns
-    static_assert(kKeyLoads >= 1);
-    constexpr int kQuadThreads = kKeys / 4 * kPieces;   // < kTileThreads for DP = 64
-    constexpr int kTurns = kQuads > 0 ? kQuads : 1;
+    constexpr int kLoads = kKeys * kPieces / kTileThreads;          // pieces of keys, and of values, a thread stages
+    constexpr int kTokenStep = kTileThreads / kPieces;              // from one to the next
     const AttendParams& P = F.a;
     const CacheView& c = P.c;
     const int D = EXACT ? DP : c.head_dim;
-    const int tid = threadIdx.x, wave = tid / kWave, lane = lane_id(), n = lane & 31, g = lane >> 5;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int lane = lane_id(), n = lane & 31, g = lane >> 5;
+    const bool second = wave >= 4;                      // the wavefronts that are a phase behind
 
-    __shared__ u32x4 key_lds[2][kKeys * kPieces];
-    __shared__ u32x4 value_lds[2][DP * (kKeys / 8)];
-    __shared__ int64_t where[2][kKeys];
-    __shared__ uint64_t present[2];
+    __shared__ u32x4 key_lds[2][kKeys * kPieces];       // of step v in v % 2
+    __shared__ u32x4 value_lds[2][kKeys * kPieces];
+    __shared__ int64_t where[4][kKeys];                 // of step v in v % 4
+    __shared__ uint64_t present[4];
+    __shared__ int32_t pages[kKeys];                    // of the step that is looked up
 
     // KV head fastest, then the part, then the row tile, the last (longest) first
     int64_t x = blockIdx.x;
@@ -82,10 +149,10 @@ __global__ __launch_bounds__(kTileThreads, DP > 128 ? 1 : 2) void tile_kernel(At
     const int32_t part = (int32_t)(x % F.parts.count);
     x /= F.parts.count;
     const int64_t tile = (int64_t)(gridDim.x / ((uint32_t)c.n_kv_heads * (uint32_t)F.parts.count)) - 1 - x;
-    const int64_t b = tile_seq(P, tile);
+    const int64_t b = tile_seq<kTileRows>(P, tile);
     const SeqRows s = seq_rows(c, b);
     const int64_t rows = (int64_t)s.n * P.group;
-    const int64_t row0 = (tile - first_tile(P, b)) * kTileRows;
+    const int64_t row0 = (tile - first_tile<kTileRows>(P, b)) * kTileRows;
     if (rows <= kFewRows || row0 < 0 || row0 >= rows) return;
 
     const int32_t base = s.length - s.n;                // position of the first new token
@@ -106,6 +173,7 @@ __global__ __launch_bounds__(kTileThreads, DP > 128 ? 1 : 2) void tile_kernel(At
     const int32_t per = max(F.parts.tokens / kKeys, (tiles.count + F.parts.count - 1) / F.parts.count);
     const int32_t v_first = (int32_t)min((int64_t)tiles.count, (int64_t)part * per);
     const int32_t v_end = (int32_t)min((int64_t)tiles.count, (int64_t)(part + 1) * per);
+    const int32_t count = v_end - v_first;              // steps, numbered from 0 below
 
     f32x16 acc[kBlocks];
 #pragma unroll
@@ -115,7 +183,7 @@ __global__ __launch_bounds__(kTileThreads, DP > 128 ? 1 : 2) void tile_kernel(At
     float m = kNone, l = 0.0f;
     bool special = false;               // this thread's values need the rows one by one
 
-    if (v_first < v_end) {
+    if (count > 0) {
         u32x4 q[kSteps];
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
@@ -126,123 +194,215 @@ __global__ __launch_bounds__(kTileThreads, DP > 128 ? 1 : 2) void tile_kernel(At
                                        (int64_t)head * P.query_head_stride + d);
         }
         const int32_t* const table_row = c.table + b * c.table_width;
-        const uint16_t* const keys = c.key + (int64_t)kvh * c.head_stride;
-        const uint16_t* const values = c.value + (int64_t)kvh * c.head_stride;
 
-        // where token lane of step v lies; -1: it has no page, or no row sees it
-        auto lookup = [&](int32_t v) -> int64_t {
-            const int64_t t = (int64_t)tiles.tile(v) * kKeys + lane;
-            if (t >= tiles.end || !sees(P.window, P.sinks, max(first_pos, (int32_t)t), (int32_t)t)) return -1;
-            return token_offset(c, table_row, (int32_t)t);
+        // What this thread stages: slot tid + i kTileThreads of the keys and
+        // of the values, which hold piece (slot ^ exchange) of token slot / kPieces.
+        const int my_token = tid / kPieces, slot = tid % kPieces;
+        const int key_piece = slot ^ key_exchange<kPieces>(my_token);
+        constexpr int kOdd = kTokenStep % 16;       // 8: every other token has another exchange
+        const int value_piece = slot ^ value_exchange<kPieces>(my_token);
+        const uint16_t* const keys = c.key + (int64_t)kvh * c.head_stride + key_piece * 8;
+        const uint16_t* const values = c.value + (int64_t)kvh * c.head_stride + value_piece * 8;
+        const int odd_step = (key_piece ^ kOdd) * 8 - key_piece * 8;
+        const bool key_in[2] = {EXACT || key_piece * 8 < D, EXACT || (key_piece ^ kOdd) * 8 < D};
+        const bool value_in = EXACT || value_piece * 8 < D;
+
+        // The pages of step v's tokens, a token a lane; and, when they are here,
+        // where the tokens lie.  (A token that no row sees, or without a page,
+        // copies some page's, which is not used.)
+        auto lookup = [&](int32_t v) {
+            const int64_t t = (int64_t)tiles.tile(v_first + v) * kKeys + lane;
+            copy_words(table_row + div_u32((uint32_t)min(t, tiles.end - 1), c.div_page), lds_address(pages));
         };
-        auto keep_lookup = [&](int buffer, int64_t at) {
-            const uint64_t mask = __ballot(at >= 0);
-            where[buffer][lane] = at;
-            if (lane == 0) present[buffer] = mask;
+        auto keep_lookup = [&](int32_t v) {
+            const int64_t t = (int64_t)tiles.tile(v_first + v) * kKeys + lane;
+            const bool seen = t < tiles.end && sees(P.window, P.sinks, max(first_pos, (int32_t)t), (int32_t)t);
+            const uint32_t u = (uint32_t)min(t, tiles.end - 1);
+            const uint32_t in_page = u - div_u32(u, c.div_page) * (uint32_t)c.page_tokens;
+            const int32_t page = pages[lane];
+            const bool there = seen && page >= 0 && page < c.n_pages;
+            const uint64_t mask = __ballot(there);
+            where[v & 3][lane] = there ? page * c.page_stride + (int64_t)in_page * c.token_stride : 0;
+            if (lane == 0) present[v & 3] = mask;
         };
-        u32x4 key_regs[kKeyLoads];
-        u32x4 value_regs[kTurns][4];
-        // loads of the step whose tokens are in where[buffer]
-        auto load = [&](int buffer) {
+        // What is copied while step v runs: the next one's keys and this one's
+        // values.  `find` reads where they lie, a phase before `copy`.
+        int64_t key_from[kLoads], value_from[kLoads];
+        const uint32_t key_to = lds_address(key_lds) + wave * (kWave * 16), value_to = lds_address(value_lds) + wave * (kWave * 16);
+        constexpr uint32_t kBufferBytes = kKeys * kPieces * 16, kLoadBytes = kTileThreads * 16;
+        uint64_t there = 0;             // tokens of the step that are copied
+        auto find = [&](int32_t v) {
 #pragma unroll
-            for (int i = 0; i < kKeyLoads; ++i) {
-                const int e = tid + i * kTileThreads, t = e / kPieces, piece = e % kPieces;
-                const int64_t at = where[buffer][t];
-                key_regs[i] = u32x4{0, 0, 0, 0};
-                if (at >= 0 && (EXACT || piece * 8 < D)) key_regs[i] = *(const u32x4*)(keys + at + piece * 8);
+            for (int i = 0; i < kLoads; ++i) {
+                key_from[i] = where[(v + 1) & 3][my_token + i * kTokenStep];
+                value_from[i] = where[v & 3][my_token + i * kTokenStep];
             }
+            there = present[v & 3];
+        };
+        auto copy_keys = [&](int32_t v) {
 #pragma unroll
-            for (int i = 0; i < kTurns; ++i) {
-                const int e = tid + i * kTileThreads, quad = e / kPieces, piece = e % kPieces;
+            for (int i = 0; i < kLoads; ++i)
+                if (key_in[i & 1])
+                    copy_piece(keys + (key_from[i] + (i & 1 ? odd_step : 0)),
+                               key_to + (v & 1) * kBufferBytes + i * kLoadBytes);
+        };
+        auto copy = [&](int32_t v) {
+            if (v + 1 < count) copy_keys(v + 1);
+            if (v >= count) return;
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    value_regs[i][u] = u32x4{0, 0, 0, 0};
-                    if (kQuadThreads < kTileThreads && e >= kQuadThreads) continue;
-                    const int64_t at = where[buffer][4 * quad + u];
-                    if (at >= 0 && (EXACT || piece * 8 < D)) value_regs[i][u] = *(const u32x4*)(values + at + piece * 8);
+            for (int i = 0; i < kLoads; ++i)
+                if (value_in) copy_piece(values + value_from[i], value_to + (v & 1) * kBufferBytes + i * kLoadBytes);
+        };
+        // After the copies of step v: values of tokens that nobody sees are 0;
+        // and whether one that some rows see and others do not is not finite,
+        // which would reach the others as 0 x value.
+        auto settle = [&](int32_t v, uint64_t there) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            const int32_t t0 = tiles.tile(v_first + v) * kKeys, t_last = t0 + kKeys - 1;
+            const bool all = t_last <= first_pos && (P.window == 0 || t0 > last_pos - P.window || t_last < P.sinks);
+            if (v >= count || (there == ~0ull && all)) return;
+            for (int i = 0; i < kLoads; ++i) {
+                u32x4* const at = &value_lds[v & 1][tid + i * kTileThreads];
+                if (!(there >> (my_token + i * kTokenStep) & 1)) {
+                    *at = u32x4{0, 0, 0, 0};
+                } else if (!all) {
+                    const u32x4 y = *at;
+                    special |= not_finite2<F16>(y[0]) || not_finite2<F16>(y[1]) || not_finite2<F16>(y[2]) ||
+                               not_finite2<F16>(y[3]);
                 }
             }
         };
-        // values that some rows see and others do not: one that is not finite
-        // would reach the others as 0 x value
-        auto look_at = [&](int32_t v) {
-            const int32_t t0 = tiles.tile(v) * kKeys, t_last = t0 + kKeys - 1;
-            if (t_last <= first_pos && (P.window == 0 || t0 > last_pos - P.window || t_last < P.sinks)) return;
-#pragma unroll
-            for (int i = 0; i < kTurns; ++i)
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) special |= not_finite2<F16>(value_regs[i][u][y]);
-        };
-        auto store = [&](int buffer) {
-#pragma unroll
-            for (int i = 0; i < kKeyLoads; ++i) {
-                const int e = tid + i * kTileThreads, t = e / kPieces, piece = e % kPieces;
-                key_lds[buffer][t * kPieces + (piece ^ (t & (kPieces - 1) & 15))] = key_regs[i];
-            }
-#pragma unroll
-            for (int i = 0; i < kTurns; ++i) {
-                const int e = tid + i * kTileThreads, quad = e / kPieces, piece = e % kPieces;
-                if (kQuadThreads < kTileThreads && e >= kQuadThreads) continue;
-                // tokens 4 quad ..: step 16 (quad / 4), upper half, lane group
-                const int to = 2 * (quad / 4) + (quad & 1), half = quad >> 1 & 1;
-#pragma unroll
-                for (int y = 0; y < 8; ++y) {
-                    const uint32_t sel = y & 1 ? 0x07060302u : 0x05040100u;
-                    const int d = 8 * piece + y;
-                    uint2 z;
-                    z.x = __builtin_amdgcn_perm(value_regs[i][1][y / 2], value_regs[i][0][y / 2], sel);
-                    z.y = __builtin_amdgcn_perm(value_regs[i][3][y / 2], value_regs[i][2][y / 2], sel);
-                    ((uint2*)&value_lds[buffer][d * (kKeys / 8) + (to ^ y ^ (piece & 7))])[half] = z;
-                }
-            }
+        // A barrier after a phase: nothing moves across it.
+        auto phase_end = [&] {
+            __builtin_amdgcn_sched_barrier(0);
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
         };
 
-        if (wave == 0) {
-            keep_lookup(0, lookup(v_first));
-            if (v_first + 1 < v_end) keep_lookup(1, lookup(v_first + 1));
+        // pieces beyond head_dim stay 0; and the first step takes a product of
+        // zeros
+        for (int i = tid; i < (EXACT ? 1 : 2) * kKeys * kPieces; i += kTileThreads) {
+            value_lds[EXACT ? 1 : 0][i] = u32x4{0, 0, 0, 0};
+            if constexpr (!EXACT) key_lds[0][i] = u32x4{0, 0, 0, 0};
         }
+        if (wave == 0)
+            for (int v = 0; v < 3 && v < count; ++v) {
+                lookup(v);
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                keep_lookup(v);
+            }
         __syncthreads();
-        load(0);
-        look_at(v_first);
-        store(0);
+        find(-1);
+        copy_keys(0);
+        // the queries are there before the first copies of the loop are under way
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) asm volatile("" : "+v"(q[k]));
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        for (int32_t v = v_first; v < v_end; ++v) {
-            const int buffer = (v - v_first) & 1;
-            const int32_t t0 = tiles.tile(v) * kKeys, t_last = t0 + kKeys - 1;
-            const uint64_t there = present[buffer];
-            int64_t at = -1;
-            if (v + 1 < v_end) load(buffer ^ 1);
-            if (wave == 0 && v + 2 < v_end) at = lookup(v + 2);
-            if (!idle && t0 <= wave_last) {
-                f32x16 sc[2];
+
+        // where this lane reads: keys of token 32 h + n, and columns of the values
+        const int key_at = n * kPieces, key_turn = key_exchange<kPieces>(n);
+        const int value_token = 4 * g + (lane & 15) / 4;
+        int value_at[kBlocks];          // bytes
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+        for (int j = 0; j < kBlocks; ++j) {
+            const int piece = (4 * j + 2 * (lane >> 4 & 1) + (lane & 3) / 2) ^ value_exchange<kPieces>(value_token);
+            value_at[j] = (value_token * kPieces + piece) * 16 + (lane & 1) * 8;
+        }
+        // the two products of a step
+        f32x16 sc[2];
+        u32x4 w[2][2];
+        // (the last step's first), operands read kAhead instructions ahead: left to
+        // itself the compiler saves registers and waits for every read
+        constexpr int kProducts = 4 * kBlocks;
+        static_assert(kProducts == 2 * kSteps);
+        constexpr int kAhead = DP > 128 ? 4 : 6;
+        auto multiply = [&](int32_t v) {
+            const unsigned char* const old_values = (const unsigned char*)value_lds[(v - 1) & 1];
+            const u32x4* const new_keys = key_lds[v & 1];
+            u32x4 a[kAhead];
+            auto read = [&](int i) {
+                if (i < kProducts) {
+                    const unsigned char* const p = old_values + value_at[i % kBlocks] + 16 * (i / kBlocks) * kPieces * 16;
+                    const uint2 lo = read_column4(p), hi = read_column4(p + 8 * kPieces * 16);
+                    a[i % kAhead] = u32x4{lo.x, lo.y, hi.x, hi.y};
+                } else if (i < 2 * kProducts) {
+                    const int k = (i - kProducts) / 2, h = (i - kProducts) % 2;
+                    a[i % kAhead] = new_keys[key_at + 32 * h * kPieces + ((2 * k + g) ^ key_turn)];
+                }
+            };
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) sc[h][i] = 0.0f;
+            for (int i = 0; i < kAhead; ++i) read(i);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int k = 0; k < kSteps; ++k)
+            for (int i = 0; i < 2 * kProducts; ++i) {
+                if (i < kProducts) {
+                    const int j = i % kBlocks, y = i / kBlocks;
+                    acc[j] = mfma32<F16>(a[i % kAhead], w[y / 2][y % 2], acc[j]);
+                } else {
+                    const int k = (i - kProducts) / 2, h = (i - kProducts) % 2;
+                    if (k == 0)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int t = 32 * h + n, piece = 2 * k + g;
-                        sc[h] = mfma32<F16>(key_lds[buffer][t * kPieces + (piece ^ (t & (kPieces - 1) & 15))], q[k], sc[h]);
-                    }
-                const bool full = there == ~0ull && t_last <= wave_first &&
+                        for (int e = 0; e < 16; ++e) sc[h][e] = 0.0f;
+                    sc[h] = mfma32<F16>(a[i % kAhead], q[k], sc[h]);
+                }
+                read(i + kAhead);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) w[h][y] = u32x4{0, 0, 0, 0};
+        find(0);
+        if (second) {
+            copy(0);
+            phase_end();
+        }
+        uint64_t seen = there;          // of the softmax's step
+        for (int32_t v = 0; v <= count; ++v) {
+            // ---- matrix phase
+            const bool looks = wave == (v & 3) && v + 3 < count;
+            seen = there;
+            if (second) {
+                find(v + 1);
+            } else {
+                if (looks) lookup(v + 3);
+                copy(v);
+            }
+            const int32_t t0 = tiles.tile(v_first + v) * kKeys, t_last = t0 + kKeys - 1;
+            // (once a step is past the wavefront's rows all later ones are)
+            const bool was_on = v == 0 || tiles.tile(v_first + v - 1) * kKeys <= wave_last;
+            const bool on = !idle && v < count && t0 <= wave_last;
+            if (!idle && was_on) {
+                multiply(v);
+            }
+            if (second) settle(v, seen);
+            phase_end();
+            // ---- softmax phase
+            if (second) copy(v + 1);
+            if (on) {
+                const bool full = seen == ~0ull && t_last <= wave_first &&
                                   (P.window == 0 || t0 > wave_last - P.window || t_last < P.sinks);
                 if (!full) {
+                    const uint64_t bits = (seen & seen_bits(P.window, P.sinks, pos, t0)) >> (4 * g);
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const int u = 32 * h + 8 * (i / 4) + 4 * g + i % 4;
-                            if (!(there >> u & 1) || !sees(P.window, P.sinks, pos, t0 + u)) sc[h][i] = -INFINITY;
+                            const uint32_t half = (uint32_t)(bits >> (32 * h));
+                            sc[h][i] = half & (1u << (8 * (i / 4) + i % 4)) ? sc[h][i] : -INFINITY;
                         }
                 }
-                float top = sc[0][0];
+                float tops[4];
 #pragma unroll
-                for (int i = 1; i < 32; ++i) top = fmaxf(top, sc[i / 16][i % 16]);
-                top = fmaxf(top, __shfl_xor(top, 32));
+                for (int u = 0; u < 4; ++u) {
+                    tops[u] = fmaxf(sc[0][u], sc[1][u]);
+#pragma unroll
+                    for (int i = u + 4; i < 16; i += 4) tops[u] = fmaxf(fmaxf(tops[u], sc[0][i]), sc[1][i]);
+                }
+                float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+                top = fmaxf(top, other_half(top));
                 // The sums are only scaled down when the maximum has grown by
                 // more than 2^8 for some row: weights up to 2^8 lose nothing.
                 const float m2 = fmaxf(m, top * F.score_scale);
@@ -256,7 +416,6 @@ __global__ __launch_bounds__(kTileThreads, DP > 128 ? 1 : 2) void tile_kernel(At
                         for (int i = 0; i < 16; ++i) acc[j][i] *= keep;
                 }
                 float sum[4] = {0, 0, 0, 0};
-                u32x4 w[2][2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -267,30 +426,21 @@ __global__ __launch_bounds__(kTileThreads, DP > 128 ? 1 : 2) void tile_kernel(At
                         w[h][i / 8][i % 8 / 2] = pack2<F16>(a, z);
                     }
                 l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-#pragma unroll
-                for (int y = 0; y < 4; ++y)
-#pragma unroll
-                    for (int j = 0; j < kBlocks; ++j) {
-                        const int d = 32 * j + n, piece = 2 * y + g;
-                        acc[j] = mfma32<F16>(value_lds[buffer][d * (kKeys / 8) + (piece ^ (d & 7) ^ (d >> 3 & 7))],
-                                             w[y / 2][y % 2], acc[j]);
-                    }
             }
-            if (v + 1 < v_end) {
-                look_at(v + 1);
-                store(buffer ^ 1);
+            if (!second) {
+                settle(v, seen);
+                find(v + 1);
             }
-            __syncthreads();
-            // where[buffer] was read in the step before
-            if (wave == 0 && v + 2 < v_end) keep_lookup(buffer, at);
-            __syncthreads();
+            if (looks) keep_lookup(v + 3);
+            phase_end();
         }
+        if (!second) phase_end();
         l += __shfl_xor(l, 32);
     }
 
     const int64_t to = (s.first + token) * P.n_heads + head;
     const bool split = F.parts.count > 1;
-    const int64_t slot0 = (tile * c.n_kv_heads + kvh) * kTileRows;       // of the parts' rows
+    const int64_t slot0 = (tile * c.n_kv_heads + kvh) * kTileRows;      // of the parts' rows
     if (__syncthreads_or(special)) {
         for (int r = 0; r < kWaveRows; ++r) {
             const int64_t rr = wave_row + r;
@@ -336,55 +486,56 @@ __global__ __launch_bounds__(kTileThreads, DP > 128 ? 1 : 2) void tile_kernel(At
     }
 }
 
-template <bool F16>
-__global__ __launch_bounds__(kTileThreads) void join_tiles_kernel(AttendLaunch F) {
+constexpr int kJoinWaves = 4, kJoinThreads = kJoinWaves * kWave;
+
+template <bool F16, int ROWS>
+__global__ __launch_bounds__(kJoinThreads) void join_tiles_kernel(AttendLaunch F) {
     const AttendParams& P = F.a;
-    const int64_t slot = (int64_t)blockIdx.x * kTileWaves + threadIdx.x / kWave;
-    int64_t x = slot / kTileRows;
+    const int64_t slot = (int64_t)blockIdx.x * kJoinWaves + threadIdx.x / kWave;
+    const int64_t x = slot / ROWS;
     const int32_t kvh = (int32_t)(x % P.c.n_kv_heads);
-    const int64_t tile = x / P.c.n_kv_heads, b = tile_seq(P, tile);
+    const int64_t tile = x / P.c.n_kv_heads, b = tile_seq<ROWS>(P, tile);
     const SeqRows s = seq_rows(P.c, b);
-    const int64_t rows = (int64_t)s.n * P.group, row = (tile - first_tile(P, b)) * kTileRows + slot % kTileRows;
+    const int64_t rows = (int64_t)s.n * P.group, row = (tile - first_tile<ROWS>(P, b)) * ROWS + slot % ROWS;
     if (rows <= kFewRows || row < 0 || row >= rows) return;
     const int64_t token = row / P.group;
     join_row<F16>(F, slot, (s.first + token) * P.n_heads + kvh * P.group + (row - token * P.group));
 }
 
+int rows_of(const AttendParams& p) { return tile_rows(p.c.head_dim); }
+
 template <bool F16, int DP>
-void launch_dim(const AttendLaunch& f, dim3 grid, hipStream_t stream) {
-    const dim3 block(kTileThreads);
+hipError_t launch_dim(const AttendLaunch& f, hipStream_t stream) {
+    const int64_t blocks = tile_blocks(f.a) * f.parts.count;
+    if (!grid_fits(blocks, tile_waves(DP) * kWave)) return hipErrorInvalidConfiguration;
+    const dim3 grid((unsigned)blocks), block(tile_waves(DP) * kWave);
     if (f.a.c.head_dim == DP) hipLaunchKernelGGL((tile_kernel<F16, DP, true>), grid, block, 0, stream, f);
     else hipLaunchKernelGGL((tile_kernel<F16, DP, false>), grid, block, 0, stream, f);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || f.parts.count == 1) return e;
+    const int64_t joins = tile_slots(f.a) / kJoinWaves;
+    if (!grid_fits(joins, kJoinThreads)) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((join_tiles_kernel<F16, tile_rows(DP)>), dim3((unsigned)joins), dim3(kJoinThreads), 0, stream, f);
+    return hipGetLastError();
 }
 
 template <bool F16>
-void launch_type(const AttendLaunch& f, dim3 grid, hipStream_t stream) {
-    if (f.a.c.head_dim <= 64) launch_dim<F16, 64>(f, grid, stream);
-    else if (f.a.c.head_dim <= 128) launch_dim<F16, 128>(f, grid, stream);
-    else launch_dim<F16, 256>(f, grid, stream);
+hipError_t launch_type(const AttendLaunch& f, hipStream_t stream) {
+    if (f.a.c.head_dim <= 64) return launch_dim<F16, 64>(f, stream);
+    if (f.a.c.head_dim <= 128) return launch_dim<F16, 128>(f, stream);
+    return launch_dim<F16, 256>(f, stream);
 }
 
 }  // namespace
 
 int64_t tile_blocks(const AttendParams& p) {
-    return (p.c.n_tokens * p.group / kTileRows + p.c.n_seqs) * p.c.n_kv_heads;
+    return (p.c.n_tokens * p.group / rows_of(p) + p.c.n_seqs) * p.c.n_kv_heads;
 }
 
-int64_t tile_slots(const AttendParams& p) { return tile_blocks(p) * kTileRows; }
+int64_t tile_slots(const AttendParams& p) { return tile_blocks(p) * rows_of(p); }
 
 hipError_t launch_tiles(const AttendLaunch& f, hipStream_t stream) {
-    const int64_t blocks = tile_blocks(f.a) * f.parts.count;
-    if (!grid_fits(blocks, kTileThreads)) return hipErrorInvalidConfiguration;
-    if (f.a.f16) launch_type<true>(f, dim3((unsigned)blocks), stream);
-    else launch_type<false>(f, dim3((unsigned)blocks), stream);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || f.parts.count == 1) return e;
-    const int64_t joins = tile_slots(f.a) / kTileWaves;
-    if (!grid_fits(joins, kTileThreads)) return hipErrorInvalidConfiguration;
-    const dim3 grid((unsigned)joins), block(kTileThreads);
-    if (f.a.f16) hipLaunchKernelGGL((join_tiles_kernel<true>), grid, block, 0, stream, f);
-    else hipLaunchKernelGGL((join_tiles_kernel<false>), grid, block, 0, stream, f);
-    return hipGetLastError();
+    return f.a.f16 ? launch_type<true>(f, stream) : launch_type<false>(f, stream);
 }
 
 }  // namespace tl
