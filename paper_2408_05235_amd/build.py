@@ -18,7 +18,7 @@ LIB_PATH = os.path.join(LIB_DIR, "libtl.so")
 SOURCES = ["api.cpp", "host_forest.cpp", "project.hip", "forest.hip", "column.hip", "small.hip", "lattice.hip", "select.hip",
            "cache_api.cpp", "pages.hip", "attend.hip", "attend_tiles.hip"]
 HEADERS = ["device_util.h", "tl_internal.h", "forest_walk.h", "record_format.h", "host_forest.h", "queue_tries.h",
-           "scratch.h", "status.h", "cache.h", "cache_rows.h", "attend_common.h"]
+           "scratch.h", "status.h", "cache.h", "cache_rows.h", "attend_common.h", "attend_few.h"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

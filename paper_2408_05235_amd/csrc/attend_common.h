@@ -120,19 +120,28 @@ struct Parts {
 // A launch of the attention's kernels.
 struct AttendLaunch {
     AttendParams a;
-    Parts parts;
     float score_scale;      // scale x log2 e
-    int32_t row_tiles;      // few_rows_kernel: of a sequence and head, without q_offset
+    Parts few;              // of sequences with few rows: a slot per row of a
+                            // sequence and KV head
+    int32_t row_tiles;      // ... row tiles of a sequence and head
+    int32_t slot_rows;      // ... slots of a sequence and head
+    Parts tiles;            // of the others: a slot per token and head
+    int64_t tile_count;     // row tiles, gaps included
 };
 
 // Sequences of up to so many rows (new tokens x query heads of a KV head) are
-// few_rows_kernel's, the others tile_kernel's.
+// few_rows', the others tile_rows'.
 constexpr int kFewRows = 16;
 
-hipError_t launch_tiles(const AttendLaunch& f, hipStream_t stream);
-// Workgroups of launch_tiles per part, and slots of its parts.
-int64_t tile_blocks(const AttendParams& p);
-int64_t tile_slots(const AttendParams& p);
+// A workgroup's wavefronts, and the rows that they have in tile_rows: two
+// wavefronts a SIMD where their registers allow it.
+constexpr int kWaveRows = 32;
+constexpr int tile_waves(int head_dim) { return head_dim > 128 ? 4 : 8; }
+constexpr int tile_rows_of(int head_dim) { return tile_waves(head_dim) * kWaveRows; }
+
+// Both kinds of sequences in one launch, few_blocks workgroups for those with
+// few rows.
+hipError_t launch_mixed(const AttendLaunch& f, int64_t few_blocks, hipStream_t stream);
 
 template <bool F16>
 __device__ __forceinline__ void load8(const uint16_t* p, float (&x)[8]) {
@@ -199,34 +208,48 @@ __device__ RowSums row_alone(const AttendParams& P, int64_t b, int64_t token, in
 }
 
 // A wavefront joins the parts of a slot, in their order, to output row `to`
-// (token x n_heads + head).
-template <bool F16>
-__device__ __forceinline__ void join_row(const AttendLaunch& F, int64_t slot, int64_t to) {
-    const AttendParams& P = F.a;
-    const int lane = lane_id(), n = F.parts.count, D = P.c.head_dim;
-    const float2* const st = (const float2*)F.parts.stats + slot * n;
+// (token x n_heads + head): one lane looks at each part's statistics, then
+// LANES lanes with 4 elements each take every (64 / LANES)th part.  Nothing
+// waits for the part before: a part without weight is read all the same and
+// left out by its factor of 0.
+template <bool F16, int LANES>
+__device__ __forceinline__ void join_row(const AttendParams& P, const Parts& parts, int64_t slot, int64_t to) {
+    constexpr int kGroups = kWave / LANES;
+    const int lane = lane_id(), n = parts.count, D = P.c.head_dim;
+    const float2* const st = (const float2*)parts.stats + slot * n;
+    const float* const sums = parts.sums + slot * n * D;
+    const int group = lane / LANES, d = lane % LANES * 4;
     float top = kNone;
-    for (int k = lane; k < n; k += kWave) top = fmaxf(top, st[k].x);
+    for (int k = lane; k < n; k += kWave) top = fmaxf(top, st[k].y == 0.0f ? kNone : st[k].x);
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-    const float* const sums = F.parts.sums + slot * n * D;
-    const int d = lane * 4;
     float all = 0.0f;
     f32x4 o = {0, 0, 0, 0};
-    for (int k = 0; k < n; ++k) {
-        const float2 y = st[k];
-        if (y.y == 0.0f) continue;      // an empty part: its sums are not written
-        const float f = exp2_fast(y.x - top);
+    for (int k0 = 0; k0 < n; k0 += kWave) {
+        const float2 y = k0 + lane < n ? st[k0 + lane] : make_float2(kNone, 0.0f);
+        const float f = y.y == 0.0f ? 0.0f : exp2_fast(y.x - top);
         all = fmaf(y.y, f, all);
-        if (d < D) {
-            const f32x4 v = *(const f32x4*)(sums + (int64_t)k * D + d);
+        const int m = min(n - k0, kWave);
+#pragma unroll 8
+        for (int k = 0; k < m; k += kGroups) {
+            const int part = min(k + group, m - 1);
+            const float there = __shfl(f, part), w = k + group < m ? there : 0.0f;
+            f32x4 v = {0, 0, 0, 0};
+            if (d < D) v = *(const f32x4*)(sums + (int64_t)(k0 + part) * D + d);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = fmaf(v[e], f, o[e]);
+            for (int e = 0; e < 4; ++e) o[e] = w == 0.0f ? o[e] : fmaf(v[e], w, o[e]);
         }
     }
+#pragma unroll
+    for (int s = 1; s < kWave; s <<= 1) all += __shfl_xor(all, s);
+#pragma unroll
+    for (int s = LANES; s < kWave; s <<= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], s);
     const float f = all == 0.0f ? 0.0f : 1.0f / all;
     if (all == 0.0f) o = f32x4{0, 0, 0, 0};
-    if (d < D) *(uint2*)(P.out + to * D + d) = make_uint2(pack2<F16>(o[0] * f, o[1] * f), pack2<F16>(o[2] * f, o[3] * f));
+    if (group == 0 && d < D)
+        *(uint2*)(P.out + to * D + d) = make_uint2(pack2<F16>(o[0] * f, o[1] * f), pack2<F16>(o[2] * f, o[3] * f));
     if (lane == 0 && P.lse) P.lse[to] = all == 0.0f ? -INFINITY : (top + log2f(all)) * kLn2;
 }
 

@@ -11,6 +11,7 @@
 #include <algorithm>
 
 #include "attend_common.h"
+#include "attend_few.h"
 #include "cache.h"
 #include "cache_rows.h"
 #include "device_util.h"
@@ -19,12 +20,7 @@
 namespace tl {
 namespace {
 
-constexpr int kWaveRows = 32;
 constexpr int kKeys = 64;               // cached tokens of a step
-// Wavefronts and rows of a workgroup: two wavefronts a SIMD where their
-// registers allow it.
-constexpr int tile_waves(int head_dim) { return head_dim > 128 ? 4 : 8; }
-constexpr int tile_rows(int head_dim) { return tile_waves(head_dim) * kWaveRows; }
 
 // Row tiles are numbered through the batch with gaps: sequence b's begin at
 // floor(q_offset[b] x group / ROWS) + b, which leaves room for all of them, and
@@ -121,14 +117,27 @@ __device__ __forceinline__ int value_exchange(int token) {
 // instructions run under the other's softmax.  Keys of the next step and this
 // one's values are copied meanwhile, and the step after is looked up in the page
 // table.
+template <int DP>
+struct TileLds {
+    // Steps in LDS: step v copies the keys of step v + kRing - 1 and the values
+    // of step v + kRing - 2, and looks up step v + kRing + 1.
+    static constexpr int kRing = DP > 128 ? 2 : 3;
+    u32x4 keys[kRing][kKeys * (DP / 8)];        // of step v in v % kRing
+    u32x4 values[kRing][kKeys * (DP / 8)];
+    int64_t where[8][kKeys];                    // of step v in v % 8
+    uint64_t present[8];
+    int32_t pages[4][kKeys];                    // of the steps that are looked up, a wavefront's each
+};
+
 template <bool F16, int DP, bool EXACT>
-__global__ __launch_bounds__(tile_waves(DP) * kWave, DP > 128 ? 1 : 2) void tile_kernel(AttendLaunch F) {
-    constexpr int kTileWaves = tile_waves(DP), kTileThreads = kTileWaves * kWave, kTileRows = tile_rows(DP);
+__device__ __forceinline__ void tile_rows(const AttendLaunch& F, int64_t block, TileLds<DP>& lds) {
+    constexpr int kTileWaves = tile_waves(DP), kTileThreads = kTileWaves * kWave, kTileRows = tile_rows_of(DP);
     constexpr int kSteps = DP / 16;                     // matrix instructions of a score
     constexpr int kBlocks = DP / 32;                    // of 32 elements of the output
     constexpr int kPieces = DP / 8;                     // 16-byte pieces of a row
     constexpr int kLoads = kKeys * kPieces / kTileThreads;          // pieces of keys, and of values, a thread stages
     constexpr int kTokenStep = kTileThreads / kPieces;              // from one to the next
+    constexpr int kRing = TileLds<DP>::kRing;
     const AttendParams& P = F.a;
     const CacheView& c = P.c;
     const int D = EXACT ? DP : c.head_dim;
@@ -136,19 +145,19 @@ __global__ __launch_bounds__(tile_waves(DP) * kWave, DP > 128 ? 1 : 2) void tile
     const int lane = lane_id(), n = lane & 31, g = lane >> 5;
     const bool second = wave >= 4;                      // the wavefronts that are a phase behind
 
-    __shared__ u32x4 key_lds[2][kKeys * kPieces];       // of step v in v % 2
-    __shared__ u32x4 value_lds[2][kKeys * kPieces];
-    __shared__ int64_t where[4][kKeys];                 // of step v in v % 4
-    __shared__ uint64_t present[4];
-    __shared__ int32_t pages[kKeys];                    // of the step that is looked up
+    auto& key_lds = lds.keys;
+    auto& value_lds = lds.values;
+    auto& where = lds.where;
+    auto& present = lds.present;
+    auto& pages = lds.pages;
 
     // KV head fastest, then the part, then the row tile, the last (longest) first
-    int64_t x = blockIdx.x;
+    int64_t x = block;
     const int32_t kvh = (int32_t)(x % c.n_kv_heads);
     x /= c.n_kv_heads;
-    const int32_t part = (int32_t)(x % F.parts.count);
-    x /= F.parts.count;
-    const int64_t tile = (int64_t)(gridDim.x / ((uint32_t)c.n_kv_heads * (uint32_t)F.parts.count)) - 1 - x;
+    const int32_t part = (int32_t)(x % F.tiles.count);
+    x /= F.tiles.count;
+    const int64_t tile = F.tile_count - 1 - x;
     const int64_t b = tile_seq<kTileRows>(P, tile);
     const SeqRows s = seq_rows(c, b);
     const int64_t rows = (int64_t)s.n * P.group;
@@ -170,7 +179,7 @@ __global__ __launch_bounds__(tile_waves(DP) * kWave, DP > 128 ? 1 : 2) void tile
     const int32_t wave_last = base + (int32_t)((min(wave_row + kWaveRows, rows) - 1) / P.group);
 
     const TileList tiles = visible_tiles<kKeys>(c, P.window, P.sinks, first_pos, last_pos);
-    const int32_t per = max(F.parts.tokens / kKeys, (tiles.count + F.parts.count - 1) / F.parts.count);
+    const int32_t per = max(F.tiles.tokens / kKeys, (tiles.count + F.tiles.count - 1) / F.tiles.count);
     const int32_t v_first = (int32_t)min((int64_t)tiles.count, (int64_t)part * per);
     const int32_t v_end = (int32_t)min((int64_t)tiles.count, (int64_t)(part + 1) * per);
     const int32_t count = v_end - v_first;              // steps, numbered from 0 below
@@ -209,60 +218,65 @@ __global__ __launch_bounds__(tile_waves(DP) * kWave, DP > 128 ? 1 : 2) void tile
 
         // The pages of step v's tokens, a token a lane; and, when they are here,
         // where the tokens lie.  (A token that no row sees, or without a page,
-        // copies some page's, which is not used.)
+        // copies some page's, which is not used; steps from `count` on copy the
+        // last one's again.)
+        const uint32_t end = (uint32_t)tiles.end;
         auto lookup = [&](int32_t v) {
-            const int64_t t = (int64_t)tiles.tile(v_first + v) * kKeys + lane;
-            copy_words(table_row + div_u32((uint32_t)min(t, tiles.end - 1), c.div_page), lds_address(pages));
+            const uint32_t t = min((uint32_t)(tiles.tile(v_first + v) * kKeys + lane), end - 1);
+            copy_words(table_row + div_u32(t, c.div_page), lds_address(pages[wave & 3]));
         };
         auto keep_lookup = [&](int32_t v) {
-            const int64_t t = (int64_t)tiles.tile(v_first + v) * kKeys + lane;
-            const bool seen = t < tiles.end && sees(P.window, P.sinks, max(first_pos, (int32_t)t), (int32_t)t);
-            const uint32_t u = (uint32_t)min(t, tiles.end - 1);
+            const uint32_t t = (uint32_t)(tiles.tile(v_first + v) * kKeys + lane), u = min(t, end - 1);
+            const bool seen = t < end && sees(P.window, P.sinks, max(first_pos, (int32_t)u), (int32_t)u);
             const uint32_t in_page = u - div_u32(u, c.div_page) * (uint32_t)c.page_tokens;
-            const int32_t page = pages[lane];
+            const int32_t page = pages[wave & 3][lane];
             const bool there = seen && page >= 0 && page < c.n_pages;
             const uint64_t mask = __ballot(there);
-            where[v & 3][lane] = there ? page * c.page_stride + (int64_t)in_page * c.token_stride : 0;
-            if (lane == 0) present[v & 3] = mask;
+            where[v & 7][lane] = there ? page * c.page_stride + (int64_t)in_page * c.token_stride : 0;
+            if (lane == 0) present[v & 7] = mask;
         };
-        // What is copied while step v runs: the next one's keys and this one's
-        // values.  `find` reads where they lie, a phase before `copy`.
+        // What is copied in step v.  `find` reads where it lies, a phase before.
         int64_t key_from[kLoads], value_from[kLoads];
         const uint32_t key_to = lds_address(key_lds) + wave * (kWave * 16), value_to = lds_address(value_lds) + wave * (kWave * 16);
         constexpr uint32_t kBufferBytes = kKeys * kPieces * 16, kLoadBytes = kTileThreads * 16;
-        uint64_t there = 0;             // tokens of the step that are copied
+        uint64_t there = 0;             // the tokens of step v that are copied
         auto find = [&](int32_t v) {
+            const int k = min(v + kRing - 1, count - 1) & 7, y = min(v + kRing - 2, count - 1) & 7;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-                key_from[i] = where[(v + 1) & 3][my_token + i * kTokenStep];
-                value_from[i] = where[v & 3][my_token + i * kTokenStep];
+                key_from[i] = where[k][my_token + i * kTokenStep];
+                value_from[i] = where[y][my_token + i * kTokenStep];
             }
-            there = present[v & 3];
+            there = present[min(v, count - 1) & 7];
         };
-        auto copy_keys = [&](int32_t v) {
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i)
-                if (key_in[i & 1])
-                    copy_piece(keys + (key_from[i] + (i & 1 ? odd_step : 0)),
-                               key_to + (v & 1) * kBufferBytes + i * kLoadBytes);
+        auto copy_key = [&](int buffer, int i) {
+            if (key_in[i & 1])
+                copy_piece(keys + (key_from[i] + (i & 1 ? odd_step : 0)), key_to + buffer * kBufferBytes + i * kLoadBytes);
         };
-        auto copy = [&](int32_t v) {
-            if (v + 1 < count) copy_keys(v + 1);
-            if (v >= count) return;
+        auto copy_value = [&](int buffer, int i) {
+            if (value_in) copy_piece(values + value_from[i], value_to + buffer * kBufferBytes + i * kLoadBytes);
+        };
+        auto copy_all = [&](int key_buffer, int value_buffer) {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i)
-                if (value_in) copy_piece(values + value_from[i], value_to + (v & 1) * kBufferBytes + i * kLoadBytes);
+            for (int i = 0; i < kLoads; ++i) {
+                copy_key(key_buffer, i);
+                copy_value(value_buffer, i);
+            }
         };
         // After the copies of step v: values of tokens that nobody sees are 0;
         // and whether one that some rows see and others do not is not finite,
         // which would reach the others as 0 x value.
-        auto settle = [&](int32_t v, uint64_t there) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        auto settle = [&](int32_t v, uint64_t there, int value_buffer) {
+            // (with three steps in LDS this step's own copies may still be under
+            // way: each wavefront issues 2 kLoads)
+            if constexpr (kRing == 3 && kLoads == 2) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+            else if constexpr (kRing == 3 && kLoads == 1) asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             const int32_t t0 = tiles.tile(v_first + v) * kKeys, t_last = t0 + kKeys - 1;
             const bool all = t_last <= first_pos && (P.window == 0 || t0 > last_pos - P.window || t_last < P.sinks);
             if (v >= count || (there == ~0ull && all)) return;
             for (int i = 0; i < kLoads; ++i) {
-                u32x4* const at = &value_lds[v & 1][tid + i * kTileThreads];
+                u32x4* const at = &value_lds[value_buffer][tid + i * kTileThreads];
                 if (!(there >> (my_token + i * kTokenStep) & 1)) {
                     *at = u32x4{0, 0, 0, 0};
                 } else if (!all) {
@@ -281,19 +295,23 @@ __global__ __launch_bounds__(tile_waves(DP) * kWave, DP > 128 ? 1 : 2) void tile
 
         // pieces beyond head_dim stay 0; and the first step takes a product of
         // zeros
-        for (int i = tid; i < (EXACT ? 1 : 2) * kKeys * kPieces; i += kTileThreads) {
-            value_lds[EXACT ? 1 : 0][i] = u32x4{0, 0, 0, 0};
+        for (int i = tid; i < kRing * kKeys * kPieces; i += kTileThreads) {
+            if (!EXACT || i >= (kRing - 1) * kKeys * kPieces) value_lds[0][i] = u32x4{0, 0, 0, 0};
             if constexpr (!EXACT) key_lds[0][i] = u32x4{0, 0, 0, 0};
         }
-        if (wave == 0)
-            for (int v = 0; v < 3 && v < count; ++v) {
-                lookup(v);
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                keep_lookup(v);
-            }
+        if (wave <= kRing && wave < count) lookup(wave);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (wave <= kRing && wave < count) keep_lookup(wave);
         __syncthreads();
-        find(-1);
-        copy_keys(0);
+        // what the steps before the first one copy: keys 0 .. kRing - 2, values
+        // 0 .. kRing - 3
+        if constexpr (kRing == 3) {
+            find(-1);
+            copy_all(1, 0);
+        }
+        find(1 - kRing);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) copy_key(0, i);
         // the queries are there before the first copies of the loop are under way
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) asm volatile("" : "+v"(q[k]));
@@ -316,10 +334,12 @@ __global__ __launch_bounds__(tile_waves(DP) * kWave, DP > 128 ? 1 : 2) void tile
         // itself the compiler saves registers and waits for every read
         constexpr int kProducts = 4 * kBlocks;
         static_assert(kProducts == 2 * kSteps);
-        constexpr int kAhead = DP > 128 ? 4 : 6;
-        auto multiply = [&](int32_t v) {
-            const unsigned char* const old_values = (const unsigned char*)value_lds[(v - 1) & 1];
-            const u32x4* const new_keys = key_lds[v & 1];
+        constexpr int kAhead = 4;
+        auto multiply = [&](int now, int before) {      // places of this step and the last one
+            const unsigned char* const old_values = (const unsigned char*)value_lds[before];
+            const u32x4* const new_keys = key_lds[now];
+            // (the copies' places are the ones that were read last)
+            const int key_buffer = before, value_buffer = kRing == 3 ? (now == 2 ? 0 : now + 1) : now;
             u32x4 a[kAhead];
             auto read = [&](int i) {
                 if (i < kProducts) {
@@ -347,6 +367,13 @@ __global__ __launch_bounds__(tile_waves(DP) * kWave, DP > 128 ? 1 : 2) void tile
                     sc[h] = mfma32<F16>(a[i % kAhead], q[k], sc[h]);
                 }
                 read(i + kAhead);
+                // the copies, one at a time
+                constexpr int kEvery = 2 * kProducts / (2 * kLoads);
+                if (i % kEvery == kEvery / 2) {
+                    const int y = i / kEvery;
+                    if (y < kLoads) copy_key(key_buffer, y);
+                    else copy_value(value_buffer, y - kLoads);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
@@ -355,32 +382,24 @@ __global__ __launch_bounds__(tile_waves(DP) * kWave, DP > 128 ? 1 : 2) void tile
 #pragma unroll
             for (int y = 0; y < 2; ++y) w[h][y] = u32x4{0, 0, 0, 0};
         find(0);
-        if (second) {
-            copy(0);
-            phase_end();
-        }
-        uint64_t seen = there;          // of the softmax's step
+        if (second) phase_end();
+        int now = 0;                    // v % kRing
         for (int32_t v = 0; v <= count; ++v) {
             // ---- matrix phase
-            const bool looks = wave == (v & 3) && v + 3 < count;
-            seen = there;
-            if (second) {
-                find(v + 1);
-            } else {
-                if (looks) lookup(v + 3);
-                copy(v);
-            }
+            const int before = now == 0 ? kRing - 1 : now - 1, after = now == kRing - 1 ? 0 : now + 1;
+            const bool looks = wave == (v & 3) && v + kRing + 1 < count;
+            const uint64_t seen = there;
+            if (looks) lookup(v + kRing + 1);
             const int32_t t0 = tiles.tile(v_first + v) * kKeys, t_last = t0 + kKeys - 1;
             // (once a step is past the wavefront's rows all later ones are)
             const bool was_on = v == 0 || tiles.tile(v_first + v - 1) * kKeys <= wave_last;
             const bool on = !idle && v < count && t0 <= wave_last;
-            if (!idle && was_on) {
-                multiply(v);
-            }
-            if (second) settle(v, seen);
+            if (!idle && was_on) multiply(now, before);
+            else copy_all(before, kRing == 3 ? after : now);
+            if (second) settle(v, seen, now);
             phase_end();
             // ---- softmax phase
-            if (second) copy(v + 1);
+            find(v + 1);
             if (on) {
                 const bool full = seen == ~0ull && t_last <= wave_first &&
                                   (P.window == 0 || t0 > wave_last - P.window || t_last < P.sinks);
@@ -427,44 +446,42 @@ __global__ __launch_bounds__(tile_waves(DP) * kWave, DP > 128 ? 1 : 2) void tile
                     }
                 l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
             }
-            if (!second) {
-                settle(v, seen);
-                find(v + 1);
-            }
-            if (looks) keep_lookup(v + 3);
+            if (!second) settle(v, seen, now);
+            if (looks) keep_lookup(v + kRing + 1);
             phase_end();
+            now = after;
         }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         if (!second) phase_end();
         l += __shfl_xor(l, 32);
     }
 
     const int64_t to = (s.first + token) * P.n_heads + head;
-    const bool split = F.parts.count > 1;
-    const int64_t slot0 = (tile * c.n_kv_heads + kvh) * kTileRows;      // of the parts' rows
+    const bool split = F.tiles.count > 1;
     if (__syncthreads_or(special)) {
         for (int r = 0; r < kWaveRows; ++r) {
             const int64_t rr = wave_row + r;
             if (rr >= rows) break;
             const int32_t tok = (int32_t)(rr / P.group), hd = kvh * P.group + (int32_t)(rr - (int64_t)tok * P.group);
             const RowSums y = row_alone<F16, kKeys>(P, b, s.first + tok, hd, base + tok, tiles, v_first, v_end, F.score_scale);
-            const int64_t out = (s.first + tok) * P.n_heads + hd, part_slot = (slot0 + rr - row0) * F.parts.count + part;
+            const int64_t out = (s.first + tok) * P.n_heads + hd, part_slot = out * F.tiles.count + part;
             const int d = (lane & 31) * 8;
             if (lane < 32 && d < D) {
                 const float f = y.l == 0.0f ? 0.0f : 1.0f / y.l;
                 for (int e = 0; e < 8; ++e) {
-                    if (split) F.parts.sums[part_slot * D + d + e] = y.acc[e];
+                    if (split) F.tiles.sums[part_slot * D + d + e] = y.acc[e];
                     else P.out[out * D + d + e] = from_float<F16>(y.l == 0.0f ? 0.0f : y.acc[e] * f);
                 }
             }
             if (lane == 0) {
-                if (split) *(float2*)(F.parts.stats + part_slot * 2) = make_float2(y.m, y.l);
+                if (split) *(float2*)(F.tiles.stats + part_slot * 2) = make_float2(y.m, y.l);
                 else if (P.lse) P.lse[out] = y.l == 0.0f ? -INFINITY : (y.m + log2f(y.l)) * kLn2;
             }
         }
         return;
     }
     if (!real) return;
-    const int64_t slot = (slot0 + row - row0) * F.parts.count + part;
+    const int64_t slot = to * F.tiles.count + part;
     const float f = split ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
     for (int j = 0; j < kBlocks; ++j)
@@ -474,68 +491,52 @@ __global__ __launch_bounds__(tile_waves(DP) * kWave, DP > 128 ? 1 : 2) void tile
             if (!EXACT && d >= D) continue;
             f32x4 o = {acc[j][i], acc[j][i + 1], acc[j][i + 2], acc[j][i + 3]};
             if (split) {
-                if (l != 0.0f) *(f32x4*)(F.parts.sums + slot * D + d) = o;
+                if (l != 0.0f) *(f32x4*)(F.tiles.sums + slot * D + d) = o;
             } else {
                 if (l == 0.0f) o = f32x4{0, 0, 0, 0};
                 *(uint2*)(P.out + to * D + d) = make_uint2(pack2<F16>(o[0] * f, o[1] * f), pack2<F16>(o[2] * f, o[3] * f));
             }
         }
     if (g == 0) {
-        if (split) *(float2*)(F.parts.stats + slot * 2) = make_float2(m, l);
+        if (split) *(float2*)(F.tiles.stats + slot * 2) = make_float2(m, l);
         else if (P.lse) P.lse[to] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
     }
 }
 
-constexpr int kJoinWaves = 4, kJoinThreads = kJoinWaves * kWave;
-
-template <bool F16, int ROWS>
-__global__ __launch_bounds__(kJoinThreads) void join_tiles_kernel(AttendLaunch F) {
-    const AttendParams& P = F.a;
-    const int64_t slot = (int64_t)blockIdx.x * kJoinWaves + threadIdx.x / kWave;
-    const int64_t x = slot / ROWS;
-    const int32_t kvh = (int32_t)(x % P.c.n_kv_heads);
-    const int64_t tile = x / P.c.n_kv_heads, b = tile_seq<ROWS>(P, tile);
-    const SeqRows s = seq_rows(P.c, b);
-    const int64_t rows = (int64_t)s.n * P.group, row = (tile - first_tile<ROWS>(P, b)) * ROWS + slot % ROWS;
-    if (rows <= kFewRows || row < 0 || row >= rows) return;
-    const int64_t token = row / P.group;
-    join_row<F16>(F, slot, (s.first + token) * P.n_heads + kvh * P.group + (row - token * P.group));
+// Workgroups of tile_rows first, then those of few_rows: compute on some CUs
+// and reading on the others.
+template <bool F16, int DP, bool EXACT>
+__global__ __launch_bounds__(tile_waves(DP) * kWave, DP > 128 ? 1 : 2) void mixed_kernel(AttendLaunch F) {
+    __shared__ union {
+        TileLds<DP> tile;
+        FewLds<tile_waves(DP), DP> few;
+    } lds;
+    const int64_t tiles = F.tile_count * F.a.c.n_kv_heads * F.tiles.count;
+    if (blockIdx.x < tiles) tile_rows<F16, DP, EXACT>(F, blockIdx.x, lds.tile);
+    else few_rows<F16, DP, EXACT, tile_waves(DP)>(F, blockIdx.x - tiles, lds.few);
 }
 
-int rows_of(const AttendParams& p) { return tile_rows(p.c.head_dim); }
-
 template <bool F16, int DP>
-hipError_t launch_dim(const AttendLaunch& f, hipStream_t stream) {
-    const int64_t blocks = tile_blocks(f.a) * f.parts.count;
+hipError_t launch_dim(const AttendLaunch& f, int64_t few_blocks, hipStream_t stream) {
+    const int64_t blocks = f.tile_count * f.a.c.n_kv_heads * f.tiles.count + few_blocks * f.few.count;
     if (!grid_fits(blocks, tile_waves(DP) * kWave)) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)blocks), block(tile_waves(DP) * kWave);
-    if (f.a.c.head_dim == DP) hipLaunchKernelGGL((tile_kernel<F16, DP, true>), grid, block, 0, stream, f);
-    else hipLaunchKernelGGL((tile_kernel<F16, DP, false>), grid, block, 0, stream, f);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || f.parts.count == 1) return e;
-    const int64_t joins = tile_slots(f.a) / kJoinWaves;
-    if (!grid_fits(joins, kJoinThreads)) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((join_tiles_kernel<F16, tile_rows(DP)>), dim3((unsigned)joins), dim3(kJoinThreads), 0, stream, f);
+    if (f.a.c.head_dim == DP) hipLaunchKernelGGL((mixed_kernel<F16, DP, true>), grid, block, 0, stream, f);
+    else hipLaunchKernelGGL((mixed_kernel<F16, DP, false>), grid, block, 0, stream, f);
     return hipGetLastError();
 }
 
 template <bool F16>
-hipError_t launch_type(const AttendLaunch& f, hipStream_t stream) {
-    if (f.a.c.head_dim <= 64) return launch_dim<F16, 64>(f, stream);
-    if (f.a.c.head_dim <= 128) return launch_dim<F16, 128>(f, stream);
-    return launch_dim<F16, 256>(f, stream);
+hipError_t launch_type(const AttendLaunch& f, int64_t few_blocks, hipStream_t stream) {
+    if (f.a.c.head_dim <= 64) return launch_dim<F16, 64>(f, few_blocks, stream);
+    if (f.a.c.head_dim <= 128) return launch_dim<F16, 128>(f, few_blocks, stream);
+    return launch_dim<F16, 256>(f, few_blocks, stream);
 }
 
 }  // namespace
 
-int64_t tile_blocks(const AttendParams& p) {
-    return (p.c.n_tokens * p.group / rows_of(p) + p.c.n_seqs) * p.c.n_kv_heads;
-}
-
-int64_t tile_slots(const AttendParams& p) { return tile_blocks(p) * rows_of(p); }
-
-hipError_t launch_tiles(const AttendLaunch& f, hipStream_t stream) {
-    return f.a.f16 ? launch_type<true>(f, stream) : launch_type<false>(f, stream);
+hipError_t launch_mixed(const AttendLaunch& f, int64_t few_blocks, hipStream_t stream) {
+    return f.a.f16 ? launch_type<true>(f, few_blocks, stream) : launch_type<false>(f, few_blocks, stream);
 }
 
 }  // namespace tl
