@@ -364,48 +364,56 @@ def tl_adjust_lengths(req_offset, generated, pred_len, scale_num, scale_den, max
 
 
 _KV_DTYPES = {torch.bfloat16: _lib.BF16, torch.float16: _lib.F16}
-_VIEW_SIZE = ctypes.sizeof(_lib.KvView)
+_VIEW_SIZE, _APPEND_SIZE = ctypes.sizeof(_lib.KvView), ctypes.sizeof(_lib.KvAppendArgs)
+_ATTEND_SIZE, _PAGES_SIZE = ctypes.sizeof(_lib.AttendArgs), ctypes.sizeof(_lib.Pages)
 
 
 def _strides(t):
     """Strides, 0 where there is nothing to step over."""
-    return [0 if n <= 1 else s for n, s in zip(t.shape, t.stride())]
+    return tuple([0 if n <= 1 else s for n, s in zip(t.shape, t.stride())])
 
 
 def _rows3(t, dtype, name, heads=None, dim=None, tokens=None):
-    """Packed rows [tokens, heads, dim] with any token and head strides (a
-    view into a layer's fused product, say)."""
+    """The strides of packed rows [tokens, heads, dim], whatever they are for
+    tokens and heads (a view into a layer's fused product, say)."""
+    shape, strides = t.shape, t.stride()
+    if (t.is_cuda and t.dtype == dtype and len(shape) == 3 and strides[2] == 1 and (heads is None or shape[1] == heads)
+            and shape[2] == dim and (tokens is None or shape[0] == tokens)):
+        return strides if shape[0] > 1 and shape[1] > 1 else _strides(t)
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+    if len(shape) != 3 or (shape[2] > 1 and strides[2] != 1):
         raise ValueError(f"{name} must be [tokens, heads, head_dim] with contiguous heads")
     want = (tokens, heads, dim)
-    if any(w is not None and w != g for w, g in zip(want, t.shape)):
-        raise ValueError(f"{name} must have shape {want}, got {tuple(t.shape)}")
-    return t
+    if any(w is not None and w != g for w, g in zip(want, shape)):
+        raise ValueError(f"{name} must have shape {want}, got {tuple(shape)}")
+    return _strides(t)
 
 
 def _kv_view(key_pages, value_pages, page_table, length):
-    if key_pages.dtype not in _KV_DTYPES:
-        raise ValueError(f"key_pages must be bfloat16 or float16, got {key_pages.dtype}")
+    shape, strides, dtype = key_pages.shape, key_pages.stride(), key_pages.dtype
+    kind = _KV_DTYPES.get(dtype)
+    if kind is None:
+        raise ValueError(f"key_pages must be bfloat16 or float16, got {dtype}")
     if not key_pages.is_cuda or not value_pages.is_cuda:
         raise ValueError("pages must be device tensors")
-    if key_pages.dim() != 4 or key_pages.shape != value_pages.shape or key_pages.dtype != value_pages.dtype:
+    if len(shape) != 4 or shape != value_pages.shape or dtype != value_pages.dtype:
         raise ValueError("key_pages and value_pages must be [n_pages, n_kv_heads, page_tokens, head_dim] alike")
-    strides = _strides(key_pages)
-    if strides != _strides(value_pages) or strides[3] > 1:
-        raise ValueError("key_pages and value_pages must have the same strides and contiguous heads")
+    n_pages, heads, tokens, dim = shape
+    if value_pages.stride() != strides or strides[3] != 1 or n_pages == 1 or heads == 1 or tokens == 1:
+        strides = _strides(key_pages)
+        if strides != _strides(value_pages) or strides[3] > 1:
+            raise ValueError("key_pages and value_pages must have the same strides and contiguous heads")
     if page_table.dim() != 2:
         raise ValueError("page_table must be [n_seqs, table_width]")
-    n_pages, heads, tokens, dim = key_pages.shape
     n_seqs, width = page_table.shape
     _need(page_table, torch.int32, "page_table")
     _need(length, torch.int32, "length", (n_seqs,))
-    return _lib.KvView(_VIEW_SIZE, _KV_DTYPES[key_pages.dtype], heads, dim, tokens, width, n_pages, n_seqs,
-                       strides[0], strides[1], strides[2], key_pages.data_ptr(), value_pages.data_ptr(),
-                       page_table.data_ptr(), length.data_ptr())
+    return _lib.KvView(_VIEW_SIZE, kind, heads, dim, tokens, width, n_pages, n_seqs, strides[0], strides[1],
+                       strides[2], key_pages.data_ptr(), value_pages.data_ptr(), page_table.data_ptr(),
+                       length.data_ptr())
 
 
 def tl_kv_append(key, value, key_pages, value_pages, page_table, length, q_offset=None):
@@ -415,13 +423,12 @@ def tl_kv_append(key, value, key_pages, value_pages, page_table, length, q_offse
     [B, width] and length [B] int32, length with the new tokens; q_offset
     [B + 1] int64, or None for one token per sequence."""
     v = _kv_view(key_pages, value_pages, page_table, length)
-    T = key.shape[0]
-    _rows3(key, key_pages.dtype, "key", v.n_kv_heads, v.head_dim)
-    _rows3(value, key_pages.dtype, "value", v.n_kv_heads, v.head_dim, T)
-    _opt(q_offset, torch.int64, "q_offset", (v.n_seqs + 1,))
-    ks, vs = _strides(key), _strides(value)
-    a = _lib.KvAppendArgs(ctypes.sizeof(_lib.KvAppendArgs), 0, v, T, _p(q_offset), key.data_ptr(), value.data_ptr(),
-                          ks[0], ks[1], vs[0], vs[1])
+    dtype, (_, heads, _, dim), T = key_pages.dtype, key_pages.shape, key.shape[0]
+    ks, vs = _rows3(key, dtype, "key", heads, dim), _rows3(value, dtype, "value", heads, dim, T)
+    if q_offset is not None:
+        _need(q_offset, torch.int64, "q_offset", (page_table.shape[0] + 1,))
+    a = _lib.KvAppendArgs(_APPEND_SIZE, 0, v, T, _p(q_offset), key.data_ptr(), value.data_ptr(), ks[0], ks[1], vs[0],
+                          vs[1])
     check(lib().tl_kv_append(ctypes.byref(a), _stream()))
 
 
@@ -436,26 +443,29 @@ def tl_attend(query, key_pages, value_pages, page_table, length, q_offset=None, 
     use are allocated when None).  Returns out [T, n_heads, head_dim], and the
     log-sums [T, n_heads] fp32 too with ``want_lse``."""
     v = _kv_view(key_pages, value_pages, page_table, length)
-    _rows3(query, key_pages.dtype, "query", None, v.head_dim)
-    T, heads, dim = query.shape
-    _opt(q_offset, torch.int64, "q_offset", (v.n_seqs + 1,))
+    dtype, shape, device = key_pages.dtype, query.shape, query.device
+    qs = _rows3(query, dtype, "query", None, key_pages.shape[3])
+    T, heads, dim = shape
+    if q_offset is not None:
+        _need(q_offset, torch.int64, "q_offset", (page_table.shape[0] + 1,))
     if out is None:
-        out = torch.empty((T, heads, dim), dtype=query.dtype, device=query.device)
-    _need(out, query.dtype, "out", (T, heads, dim))
-    lse = torch.empty((T, heads), dtype=torch.float32, device=query.device) if want_lse else None
-    qs = _strides(query)
-    a = _lib.AttendArgs(ctypes.sizeof(_lib.AttendArgs), heads, v, T, _p(q_offset), query.data_ptr(), qs[0], qs[1],
+        out = torch.empty(shape, dtype=dtype, device=device)
+    else:
+        _need(out, dtype, "out", shape)
+    lse = torch.empty((T, heads), dtype=torch.float32, device=device) if want_lse else None
+    a = _lib.AttendArgs(_ATTEND_SIZE, heads, v, T, _p(q_offset), query.data_ptr(), qs[0], qs[1],
                         dim ** -0.5 if scale is None else float(scale), int(window), int(sinks), int(max_length),
                         out.data_ptr(), _p(lse), None, 0)
+    L, ref = lib(), ctypes.byref(a)
     if workspace is None:
-        n = lib().tl_attend_workspace_bytes(ctypes.byref(a))
+        n = L.tl_attend_workspace_bytes(ref)
         if n:
-            workspace = torch.empty(n, dtype=torch.uint8, device=query.device)
+            workspace = torch.empty(n, dtype=torch.uint8, device=device)
     elif workspace.dtype != torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous uint8 device tensor")
     if workspace is not None:
         a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
-    check(lib().tl_attend(ctypes.byref(a), _stream()))
+    check(L.tl_attend(ref, _stream()))
     return (out, lse) if want_lse else out
 
 
@@ -466,7 +476,7 @@ def _pages(ref, page_table, length, page_tokens, work):
         raise ValueError("ref must be [n_pages] and page_table [n_slots, table_width]")
     n_slots, width = page_table.shape
     _need(length, torch.int32, "length", (n_slots,))
-    g = _lib.Pages(ctypes.sizeof(_lib.Pages), int(page_tokens), ref.numel(), n_slots, width, 0, _p(ref),
+    g = _lib.Pages(_PAGES_SIZE, int(page_tokens), ref.numel(), n_slots, width, 0, _p(ref),
                    _p(page_table), _p(length))
     if work is None:
         work = torch.empty(lib().tl_pages_work_words(ctypes.byref(g)), dtype=torch.int32, device=ref.device)
@@ -497,7 +507,8 @@ def tl_pages_fork(ref, page_table, length, parent, child, page_tokens, work=None
     F = parent.numel()
     _need(parent, torch.int32, "parent", (F,))
     _need(child, torch.int32, "child", (F,))
-    src, dst, status = torch.empty((3, F), dtype=torch.int32, device=ref.device).unbind(0)
+    three = torch.empty((3, F), dtype=torch.int32, device=ref.device)
+    src, dst, status = three[0], three[1], three[2]
     check(lib().tl_pages_fork(ctypes.byref(g), F, _p(parent), _p(child), _p(src), _p(dst), _p(status), _p(work),
                               _stream()))
     return src, dst, status
@@ -510,7 +521,7 @@ def tl_pages_free(ref, page_table, length, slots, page_tokens):
     _need(page_table, torch.int32, "page_table")
     n_slots, width = page_table.shape
     _need(length, torch.int32, "length", (n_slots,))
-    g = _lib.Pages(ctypes.sizeof(_lib.Pages), int(page_tokens), ref.numel(), n_slots, width, 0, _p(ref),
+    g = _lib.Pages(_PAGES_SIZE, int(page_tokens), ref.numel(), n_slots, width, 0, _p(ref),
                    _p(page_table), _p(length))
     check(lib().tl_pages_free(ctypes.byref(g), slots.numel(), _p(slots), _stream()))
 
@@ -571,7 +582,7 @@ class KVCache:
         self.ref = torch.zeros(n_pages, **i32)
         self.page_table = torch.full((n_slots, width), -1, **i32)
         self.length = torch.zeros(n_slots, **i32)
-        g = _lib.Pages(ctypes.sizeof(_lib.Pages), self.page_tokens, n_pages, n_slots, width, 0, _p(self.ref),
+        g = _lib.Pages(_PAGES_SIZE, self.page_tokens, n_pages, n_slots, width, 0, _p(self.ref),
                        _p(self.page_table), _p(self.length))
         self.work = torch.empty(lib().tl_pages_work_words(ctypes.byref(g)), **i32)
 

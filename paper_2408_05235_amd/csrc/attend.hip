@@ -106,7 +106,12 @@ int64_t wanted_parts(const AttendParams& p, const SplitRule& rule, int64_t block
     int64_t tokens = (int64_t)p.c.table_width * p.c.page_tokens;
     if (p.max_length > 0) tokens = std::min<int64_t>(tokens, p.max_length);
     if (p.window > 0) tokens = std::min<int64_t>(tokens, (int64_t)p.window + p.sinks);
-    const int64_t fill = std::min((rule.fill + blocks - 1) / blocks, (tokens + rule.least - 1) / rule.least);
+    // A join costs 4 to 5 us with its launch.  It does not pay for two parts'
+    // tokens (8 heads of 250: 10.0 us in one, 14.1 in two), nor for short sequences
+    // that nearly fill the chip (512 workgroups of 600: 29.9 and 34.8 us; of 16
+    // to 1280, 48.9 and 46.3).
+    int64_t fill = std::min((rule.fill + blocks - 1) / blocks, (tokens + rule.least - 1) / rule.least);
+    if (tokens <= 2 * rule.least || (3 * blocks >= 2 * rule.fill && tokens < 8 * rule.least)) fill = 1;
     const int64_t n = std::max(fill, tokens / rule.most + (tokens % rule.most != 0));
     return std::max<int64_t>(1, std::min(n, kMostParts));
 }

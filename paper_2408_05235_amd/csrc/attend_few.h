@@ -98,7 +98,7 @@ __device__ __forceinline__ void few_rows(const AttendLaunch& F, int64_t block, F
                 const uint16_t* const p = keys + shuffle64(at0, 16 * h + n) + 8 * g;
 #pragma unroll
                 for (int e = 0; e < kSteps; ++e) {
-                    if (EXACT || 32 * e + 8 * g < D) k[h][e] = *(const u32x4*)(p + 32 * e);
+                    if (EXACT || 32 * e + 8 * g < D) k[h][e] = __builtin_nontemporal_load((const u32x4*)(p + 32 * e));
                     else k[h][e] = u32x4{0, 0, 0, 0};
                 }
             }
@@ -115,7 +115,7 @@ __device__ __forceinline__ void few_rows(const AttendLaunch& F, int64_t block, F
                         w[e][1] = z.y;
                     } else {
                         u32x4 z = {0, 0, 0, 0};
-                        if (EXACT || kPer * n + y < D) z = *(const u32x4*)(p + y);
+                        if (EXACT || kPer * n + y < D) z = __builtin_nontemporal_load((const u32x4*)(p + y));
 #pragma unroll
                         for (int u = 0; u < 4; ++u) w[e][y / 2 + u] = z[u];
                     }

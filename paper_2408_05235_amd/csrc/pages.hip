@@ -17,6 +17,8 @@
 namespace tl {
 namespace {
 
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+
 constexpr int kAppendThreads = 256;
 constexpr int kAppendTokens = 16;       // most tokens of a workgroup
 
@@ -45,10 +47,10 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendParams P, 
         const int64_t at = dst[r];
         if (at < 0) continue;
         const int64_t to = at + (int64_t)h * c.head_stride + d;
-        const uint4 k = *(const uint4*)(P.src[0] + (first + r) * P.token_stride[0] + h * P.head_stride[0] + d);
-        const uint4 v = *(const uint4*)(P.src[1] + (first + r) * P.token_stride[1] + h * P.head_stride[1] + d);
-        *(uint4*)(c.key + to) = k;
-        *(uint4*)(c.value + to) = v;
+        const u32x4 k = *(const u32x4*)(P.src[0] + (first + r) * P.token_stride[0] + h * P.head_stride[0] + d);
+        const u32x4 v = *(const u32x4*)(P.src[1] + (first + r) * P.token_stride[1] + h * P.head_stride[1] + d);
+        *(u32x4*)(c.key + to) = k;
+        *(u32x4*)(c.value + to) = v;
     }
 }
 
@@ -57,32 +59,53 @@ constexpr int kPoolWaves = kPoolThreads / kWave;
 constexpr int kBallots = 16;            // of 64 pages, per wavefront and step
 
 // Words of `work`: for the slots, what the calls note (three arrays), then for
-// the pages two arrays and the counts of blocks of 4096.
+// the pages one array and a half and the counts of blocks of 4096.
 __host__ __device__ inline int64_t work_list(const PagesParams& p) { return 3 * p.n_slots; }
+
+// What one workgroup decides about few slots stays in LDS, and with many in
+// the work array.
+constexpr int kLdsSlots = 4096, kLdsList = 4096;
+struct PoolLds {
+    int32_t starts[kLdsSlots];
+    int32_t notes[kLdsSlots];
+    int32_t list[kLdsList];
+};
+
+// The counts of kPoolThreads x kBallots consecutive pages, kBallots a lane:
+// a wavefront's ballots cover 1024 of them.
+struct PageCounts {
+    int32_t r[kBallots];
+    // `none` for pages past the last one
+    __device__ __forceinline__ void load(const PagesParams& P, int64_t base, int32_t none = 1) {
+        const int64_t w0 = base + (int64_t)(threadIdx.x / kWave) * kBallots * kWave + lane_id();
+#pragma unroll
+        for (int i = 0; i < kBallots; ++i) {
+            const int64_t p = w0 + i * kWave;
+            r[i] = p < P.n_pages ? P.ref[p] : none;
+        }
+    }
+};
 
 // The first `want` free pages in ascending order, to list[]; returns how many
 // free pages were seen (at least min(want, all)).  One workgroup of
-// kPoolThreads; each wavefront's ballots cover 1024 consecutive pages.
-__device__ int64_t list_free(const PagesParams& P, int64_t want, int32_t* list) {
+// kPoolThreads; `c` holds the counts of the first pages (their loads are under way
+// while the caller finds out what it wants).
+__device__ int64_t list_free(const PagesParams& P, PageCounts& c, int64_t want, int32_t* list) {
     __shared__ int32_t counts[2][kPoolWaves];
+    constexpr int64_t kStep = (int64_t)kPoolThreads * kBallots;
     const int wave = threadIdx.x / kWave, lane = lane_id();
     int64_t found = 0;
     int parity = 0;
-    for (int64_t base = 0; base < P.n_pages && found < want; base += kPoolWaves * kBallots * kWave, parity ^= 1) {
+    for (int64_t base = 0; base < P.n_pages && found < want; base += kStep, parity ^= 1) {
         const int64_t w0 = base + (int64_t)wave * kBallots * kWave;
-        int32_t r[kBallots];
-#pragma unroll
-        for (int i = 0; i < kBallots; ++i) {
-            const int64_t p = w0 + i * kWave + lane;
-            r[i] = p < P.n_pages ? P.ref[p] : 1;
-        }
         uint64_t bits[kBallots];
         int32_t n = 0;
 #pragma unroll
         for (int i = 0; i < kBallots; ++i) {
-            bits[i] = __ballot(r[i] == 0);
+            bits[i] = __ballot(c.r[i] == 0);
             n += __popcll(bits[i]);
         }
+        if (base + kStep < P.n_pages) c.load(P, base + kStep);
         if (lane == 0) counts[parity][wave] = n;
         __syncthreads();
         int32_t before = 0, all = 0;
@@ -124,46 +147,65 @@ __device__ int64_t running_sum(int64_t x, int64_t* carry) {
 
 __device__ __forceinline__ int32_t saturate(int64_t x) { return (int32_t)min(x, (int64_t)INT32_MAX); }
 
-// What slot b asks for: its pages now and after, and the status that does not
-// depend on the pool.
+// Full pages of `tokens` (0 .. 2^31 - 1), and pages with the last one.
+__device__ __forceinline__ int32_t full_pages(const PagesParams& P, int32_t tokens) {
+    return (int32_t)div_u32((uint32_t)tokens, P.div_page);
+}
+__device__ __forceinline__ bool partly(const PagesParams& P, int32_t tokens) {
+    return (int64_t)full_pages(P, tokens) * P.page_tokens != tokens;
+}
+__device__ __forceinline__ int32_t pages_of(const PagesParams& P, int32_t tokens) {
+    return full_pages(P, tokens) + partly(P, tokens);
+}
+
+// What a slot asks for: its pages now and the further ones, and the status
+// that does not depend on the pool.
 struct Wish {
-    int64_t old_len, new_len;
-    int32_t have, need;
-    int32_t status;
+    int32_t new_len, have, need, status;
 };
 
 __device__ __forceinline__ Wish wish(const PagesParams& P, int32_t length, int32_t add) {
-    Wish w;
-    w.old_len = length;
-    w.new_len = (int64_t)length + add;
-    w.status = TL_PAGES_OK;
-    w.have = w.need = 0;
-    const int64_t room = (int64_t)P.table_width * P.page_tokens;
+    Wish w = {0, 0, 0, TL_PAGES_OK};
+    const int64_t new_len = (int64_t)length + add, room = (int64_t)P.table_width * P.page_tokens;
     if (length < 0 || add < 0) w.status = TL_PAGES_BAD;
-    else if (w.new_len > room || w.new_len > INT32_MAX) w.status = TL_PAGES_TABLE_FULL;
+    else if (new_len > room || new_len > INT32_MAX) w.status = TL_PAGES_TABLE_FULL;
     else {
-        w.have = (int32_t)((w.old_len + P.page_tokens - 1) / P.page_tokens);
-        w.need = (int32_t)((w.new_len + P.page_tokens - 1) / P.page_tokens) - w.have;
+        w.new_len = (int32_t)new_len;
+        w.have = pages_of(P, length);
+        w.need = pages_of(P, w.new_len) - w.have;
     }
     return w;
 }
 
 // One workgroup: (1) where each slot's pages begin among the free ones, (2)
 // the free pages, (3) page k to the slot that it falls to (found in the starts,
-// which are sorted), (4) lengths and statuses.
+// which are sorted), (4) lengths and statuses.  A chain of memory round
+// trips, not work: 64 slots of a pool of 131072 pages take 6 us.
 __global__ __launch_bounds__(kPoolThreads) void extend_kernel(PagesParams P, const int32_t* add, int32_t* status,
                                                               int32_t* work) {
-    int32_t* const starts = work;
-    int32_t* const list = work + work_list(P);
+    __shared__ PoolLds lds;
+    const bool small = P.n_slots <= kLdsSlots;
+    int32_t* const starts = small ? lds.starts : work;
+    int32_t* const have = small ? lds.notes : work + P.n_slots;
+    PageCounts counts;
+    counts.load(P, 0);
     int64_t total = 0;
+    Wish mine = {};                     // of slot threadIdx.x
     for (int64_t b0 = 0; b0 < P.n_slots; b0 += kPoolThreads) {
         const int64_t b = b0 + threadIdx.x;
-        const int64_t n = b < P.n_slots ? wish(P, P.length[b], add[b]).need : 0;
-        const int64_t at = running_sum(n, &total);
-        if (b < P.n_slots) starts[b] = saturate(at);
+        Wish w = {};
+        if (b < P.n_slots) w = wish(P, P.length[b], add[b]);
+        const int64_t at = running_sum(w.need, &total);
+        if (b < P.n_slots) {
+            starts[b] = saturate(at);
+            have[b] = w.have;
+        }
+        if (b0 == 0) mine = w;
     }
     const int64_t want = min(total, P.n_pages);
-    const int64_t found = min(list_free(P, want, list), P.n_pages);
+    int32_t* const list = want <= kLdsList ? lds.list : work + work_list(P);
+    __syncthreads();
+    const int64_t found = min(list_free(P, counts, want, list), P.n_pages);
     for (int64_t k = threadIdx.x; k < min(want, found); k += kPoolThreads) {
         int64_t lo = 0, hi = P.n_slots;     // starts[lo] <= k < starts[hi]
         while (hi - lo > 1) {
@@ -171,65 +213,81 @@ __global__ __launch_bounds__(kPoolThreads) void extend_kernel(PagesParams P, con
             if (starts[mid] <= k) lo = mid;
             else hi = mid;
         }
-        const Wish w = wish(P, P.length[lo], add[lo]);
-        if (starts[lo] + (int64_t)w.need > found) continue;
+        if ((lo + 1 < P.n_slots ? (int64_t)starts[lo + 1] : total) > found) continue;
         const int32_t page = list[k];
-        P.table[lo * P.table_width + w.have + (k - starts[lo])] = page;
+        P.table[lo * P.table_width + have[lo] + (k - starts[lo])] = page;
         P.ref[page] = 1;
     }
-    __syncthreads();
     for (int64_t b = threadIdx.x; b < P.n_slots; b += kPoolThreads) {
-        const Wish w = wish(P, P.length[b], add[b]);
+        const Wish w = b < kPoolThreads ? mine : wish(P, P.length[b], add[b]);
         const bool fits = w.need == 0 || starts[b] + (int64_t)w.need <= found;
         status[b] = w.status != TL_PAGES_OK ? w.status : fits ? TL_PAGES_OK : TL_PAGES_NONE_FREE;
-        if (w.status == TL_PAGES_OK && fits) P.length[b] = (int32_t)w.new_len;
+        if (w.status == TL_PAGES_OK && fits) P.length[b] = w.new_len;
     }
 }
 
 // One workgroup decides the forks: validity (of several with one child the
-// first counts), which need a page, and which page that is.  lens[f]: the
-// child's length, -1 where the fork is not served.
+// first counts), which need a page, and which page that is.  work[n_slots + f]:
+// the child's length, -1 where the fork is not served.
 __global__ __launch_bounds__(kPoolThreads) void fork_kernel(PagesParams P, int64_t n_forks, const int32_t* parent,
                                                             const int32_t* child, int32_t* copy_src,
                                                             int32_t* copy_dst, int32_t* status, int32_t* work) {
-    int32_t* const claim = work;
+    __shared__ PoolLds lds;
+    const bool small = P.n_slots <= kLdsSlots;
+    int32_t* const claim = small ? lds.notes : work;
     int32_t* const lens = work + P.n_slots;
-    int32_t* const starts = work + 2 * P.n_slots;
-    int32_t* const list = work + work_list(P);
+    int32_t* const starts = small ? lds.starts : work + 2 * P.n_slots;
     const int64_t room = (int64_t)P.table_width * P.page_tokens;
     auto in_range = [&](int32_t s) { return s >= 0 && s < P.n_slots; };
+    PageCounts counts;
+    counts.load(P, 0);
+    // fork threadIdx.x's slots and length stay in registers
+    const bool any = threadIdx.x < n_forks;
+    const int32_t my_parent = any ? parent[threadIdx.x] : -1, my_child = any ? child[threadIdx.x] : -1;
+    const int32_t parent_len = in_range(my_parent) ? P.length[my_parent] : -1;
+    const int32_t child_len = in_range(my_child) ? P.length[my_child] : -1;
+    int32_t my_len = -1;
+    auto child_of = [&](int64_t f) { return f < kPoolThreads ? my_child : child[f]; };
     for (int64_t f = threadIdx.x; f < n_forks; f += kPoolThreads)
-        if (in_range(child[f])) claim[child[f]] = INT32_MAX;
-    __threadfence();
+        if (in_range(child_of(f))) claim[child_of(f)] = INT32_MAX;
+    if (!small) __threadfence();
     __syncthreads();
     for (int64_t f = threadIdx.x; f < n_forks; f += kPoolThreads)
-        if (in_range(child[f])) atomicMin(&claim[child[f]], (int32_t)f);
-    __threadfence();
+        if (in_range(child_of(f))) atomicMin(&claim[child_of(f)], (int32_t)f);
+    if (!small) __threadfence();
     __syncthreads();
     int64_t total = 0;
     for (int64_t f0 = 0; f0 < n_forks; f0 += kPoolThreads) {
         const int64_t f = f0 + threadIdx.x;
         int32_t len = -1;
-        if (f < n_forks && in_range(child[f]) && in_range(parent[f])) {
-            const int32_t first = __hip_atomic_load(&claim[child[f]], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            len = P.length[parent[f]];
-            if (first != f || P.length[child[f]] != 0 || len > room) len = -1;
+        if (f < n_forks && in_range(child_of(f))) {
+            const int32_t first = __hip_atomic_load(&claim[child_of(f)], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            const int32_t from = f0 == 0 ? my_parent : parent[f];
+            len = f0 == 0 ? parent_len : in_range(from) ? P.length[from] : -1;
+            if (first != f || (f0 == 0 ? child_len : P.length[child[f]]) != 0 || len > room) len = -1;
         }
-        const bool part = len > 0 && len % P.page_tokens != 0;
-        const int64_t at = running_sum(part, &total);
+        len = max(len, -1);
+        const int64_t at = running_sum(len > 0 && partly(P, len), &total);
         if (f < n_forks) {
-            lens[f] = max(len, -1);
+            lens[f] = len;
             starts[f] = saturate(at);
         }
+        if (f0 == 0) my_len = len;
     }
     const int64_t want = min(total, P.n_pages);
-    const int64_t found = list_free(P, want, list);
+    int32_t* const list = want <= kLdsList ? lds.list : work + work_list(P);
+    // (the page to copy is looked up while the free ones are listed)
+    auto last_page = [&](int32_t from, int32_t len) {
+        return len > 0 && partly(P, len) ? P.table[(int64_t)from * P.table_width + full_pages(P, len)] : -1;
+    };
+    const int32_t my_src = last_page(my_parent, my_len);
+    const int64_t found = list_free(P, counts, want, list);
     for (int64_t f = threadIdx.x; f < n_forks; f += kPoolThreads) {
-        const int32_t len = lens[f];
+        const int32_t len = f < kPoolThreads ? my_len : lens[f];
         int32_t src = -1, dst = -1, st = len < 0 ? TL_PAGES_BAD : TL_PAGES_OK;
-        if (len > 0 && len % P.page_tokens != 0) {
+        if (len > 0 && partly(P, len)) {
             if (starts[f] < min(found, want)) {
-                src = P.table[(int64_t)parent[f] * P.table_width + len / P.page_tokens];
+                src = f < kPoolThreads ? my_src : last_page(parent[f], len);
                 dst = list[starts[f]];
                 P.ref[dst] = 1;
             } else {
@@ -249,7 +307,7 @@ __global__ __launch_bounds__(256) void fork_rows_kernel(PagesParams P, const int
     const int64_t f = blockIdx.x + first;
     const int32_t len = work[P.n_slots + f];
     if (len < 0) return;
-    const int32_t full = len / P.page_tokens;
+    const int32_t full = full_pages(P, len);
     const int32_t* const from = P.table + (int64_t)parent[f] * P.table_width;
     int32_t* const to = P.table + (int64_t)child[f] * P.table_width;
     for (int32_t i = threadIdx.x; i < full; i += 256) {
@@ -258,7 +316,7 @@ __global__ __launch_bounds__(256) void fork_rows_kernel(PagesParams P, const int
         if (page >= 0 && page < P.n_pages) atomicAdd(&P.ref[page], 1);
     }
     if (threadIdx.x == 0) {
-        if (len % P.page_tokens != 0) to[full] = copy_dst[f];
+        if (partly(P, len)) to[full] = copy_dst[f];
         P.length[child[f]] = len;
     }
 }
@@ -271,7 +329,7 @@ __global__ __launch_bounds__(256) void free_kernel(PagesParams P, const int32_t*
     if (slot < 0 || slot >= P.n_slots) return;
     if (threadIdx.x == 0) taken = atomicExch(&P.length[slot], 0);
     __syncthreads();
-    const int64_t have = min(((int64_t)max(taken, 0) + P.page_tokens - 1) / P.page_tokens, (int64_t)P.table_width);
+    const int64_t have = min(pages_of(P, max(taken, 0)), P.table_width);
     const int32_t* const row = P.table + (int64_t)slot * P.table_width;
     for (int64_t i = threadIdx.x; i < have; i += 256) {
         const int32_t page = row[i];
@@ -316,12 +374,12 @@ __device__ int64_t block_sum(int64_t x) {
     return (int64_t)all;
 }
 
-__device__ __forceinline__ bool live(const PagesParams& P, int64_t p) { return p < P.n_pages && P.ref[p] > 0; }
-
 __global__ __launch_bounds__(256) void count_live_kernel(PagesParams P, int32_t* counts) {
-    const int64_t base = (int64_t)blockIdx.x * kBlockPages;
+    PageCounts c;
+    c.load(P, (int64_t)blockIdx.x * kBlockPages, 0);
     int64_t n = 0;
-    for (int i = threadIdx.x; i < kBlockPages; i += 256) n += live(P, base + i);
+#pragma unroll
+    for (int i = 0; i < kBallots; ++i) n += c.r[i] > 0;
     n = block_sum(n);
     if (threadIdx.x == 0) counts[blockIdx.x] = (int32_t)n;
 }
@@ -332,6 +390,8 @@ __global__ __launch_bounds__(256) void count_live_kernel(PagesParams P, int32_t*
 __global__ __launch_bounds__(256) void plan_moves_kernel(PagesParams P, CompactWork W, int32_t* copy_src,
                                                          int32_t* copy_dst, int32_t* n_copies) {
     const int64_t blocks = page_blocks(P), mine = blockIdx.x;
+    PageCounts c;
+    c.load(P, mine * kBlockPages, 0);
     int64_t n = 0, mine_before = 0;
     for (int64_t k = threadIdx.x; k < blocks; k += 256) {
         n += W.counts[k];
@@ -342,7 +402,11 @@ __global__ __launch_bounds__(256) void plan_moves_kernel(PagesParams P, CompactW
     const int64_t edge = n_live / kBlockPages;
     int64_t low = 0;
     for (int64_t k = threadIdx.x; k < edge; k += 256) low += W.counts[k];
-    for (int64_t p = edge * kBlockPages + threadIdx.x; p < n_live; p += 256) low += live(P, p);
+    PageCounts e;
+    e.load(P, edge * kBlockPages, 0);
+#pragma unroll
+    for (int i = 0; i < kBallots; ++i)
+        low += e.r[i] > 0 && edge * kBlockPages + ((int64_t)(threadIdx.x / kWave) * kBallots + i) * kWave + lane_id() < n_live;
     low = block_sum(low);
     if (mine == 0 && threadIdx.x == 0) {
         *n_copies = (int32_t)(n_live - low);
@@ -354,14 +418,16 @@ __global__ __launch_bounds__(256) void plan_moves_kernel(PagesParams P, CompactW
     const int64_t w0 = mine * kBlockPages + (int64_t)wave * kBallots * kWave;
     uint64_t bits[kBallots];
     int32_t own = 0;
+#pragma unroll
     for (int i = 0; i < kBallots; ++i) {
-        bits[i] = __ballot(live(P, w0 + i * kWave + lane));
+        bits[i] = __ballot(c.r[i] > 0);
         own += __popcll(bits[i]);
     }
     if (lane == 0) counts[wave] = own;
     __syncthreads();
     int64_t before = mine_before;
     for (int w = 0; w < wave; ++w) before += counts[w];
+#pragma unroll
     for (int i = 0; i < kBallots; ++i) {
         const int64_t p = w0 + i * kWave + lane;
         const bool is_live = bits[i] >> lane & 1;
@@ -372,7 +438,7 @@ __global__ __launch_bounds__(256) void plan_moves_kernel(PagesParams P, CompactW
         if (is_live && p >= n_live) {
             fate = (int32_t)(at - low);
             copy_src[fate] = (int32_t)p;
-            W.moved_ref[fate] = P.ref[p];
+            W.moved_ref[fate] = c.r[i];
         } else if (!is_live && p < n_live) {
             fate = (int32_t)(p - at);
             copy_dst[fate] = (int32_t)p;
@@ -418,16 +484,16 @@ __global__ __launch_bounds__(kCopyThreads) void copy_kernel(CopyParams P) {
         const int32_t s = P.src[pair], d = P.dst[pair];
         if (s < 0 || s >= P.n_pages || d < 0 || d >= P.n_pages || s == d) continue;
         unsigned char* const base = P.pages + plane * P.plane_stride;
-        const uint4* const from = (const uint4*)(base + s * P.page_stride);
-        uint4* const to = (uint4*)(base + d * P.page_stride);
+        const u32x4* const from = (const u32x4*)(base + s * P.page_stride);
+        u32x4* const to = (u32x4*)(base + d * P.page_stride);
         for (int64_t i = threadIdx.x; i < n; i += 4 * kCopyThreads) {
-            uint4 x[4];
+            u32x4 x[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                if (i + q * kCopyThreads < n) x[q] = from[i + q * kCopyThreads];
+                if (i + q * kCopyThreads < n) x[q] = __builtin_nontemporal_load(&from[i + q * kCopyThreads]);
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                if (i + q * kCopyThreads < n) to[i + q * kCopyThreads] = x[q];
+                if (i + q * kCopyThreads < n) __builtin_nontemporal_store(x[q], &to[i + q * kCopyThreads]);
         }
     }
 }
