@@ -28,7 +28,7 @@ constexpr int kFewWaves = 4, kFewThreads = kFewWaves * kWave;
 template <bool F16, int DP, bool EXACT>
 __global__ __launch_bounds__(kFewThreads, DP > 128 ? 1 : 3) void few_rows_kernel(AttendLaunch F) {
     __shared__ FewLds<kFewWaves, DP> lds;
-    few_rows<F16, DP, EXACT, kFewWaves>(F, blockIdx.x, lds);
+    few_rows<F16, DP, EXACT, kFewWaves, true>(F, blockIdx.x, lds);
 }
 
 // A wavefront per slot: first those of few_rows, then those of tile_rows.

@@ -513,7 +513,7 @@ __global__ __launch_bounds__(tile_waves(DP) * kWave, DP > 128 ? 1 : 2) void mixe
     } lds;
     const int64_t tiles = F.tile_count * F.a.c.n_kv_heads * F.tiles.count;
     if (blockIdx.x < tiles) tile_rows<F16, DP, EXACT>(F, blockIdx.x, lds.tile);
-    else few_rows<F16, DP, EXACT, tile_waves(DP)>(F, blockIdx.x - tiles, lds.few);
+    else few_rows<F16, DP, EXACT, tile_waves(DP), false>(F, blockIdx.x - tiles, lds.few);
 }
 
 template <bool F16, int DP>
