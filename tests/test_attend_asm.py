@@ -5,20 +5,32 @@ kernel keeps registers in memory."""
 import os
 import re
 import shutil
+import subprocess
 
 import pytest
 
 from paper_2408_05235_amd import build
-from test_asm_m0 import IMPLICIT_M0, INSTR, _device_asm
 from test_kernel_resources import _resources
+
+IMPLICIT_M0 = re.compile(r"^\s*(s_sendmsg\w*|s_movrel\w*|v_movrel\w*|s_set_gpr_idx\w*|ds_gws\w*|v_interp\w*)\b")
+INSTR = re.compile(r"^\s+[a-z_][a-z0-9_]*(\s|$)")
 
 needs_hipcc = pytest.mark.skipif(shutil.which("hipcc") is None and not os.path.exists("/opt/rocm/bin/hipcc"),
                                  reason="no hipcc")
 
 
+def _device_asm(tmp_path, name):
+    flags = [f for f in build.HIPCC_FLAGS if f not in ("-shared", "-fPIC")]
+    out = str(tmp_path / "out.s")
+    cmd = [build.hipcc(), *flags, "--cuda-device-only", "-S", "-I", build.INCLUDE, "-I", build.CSRC, "-x", "hip",
+           os.path.join(build.CSRC, name), "-o", out]
+    subprocess.run(cmd, check=True, capture_output=True, text=True)
+    return open(out).read().splitlines()
+
+
 @needs_hipcc
 def test_tiles_in_assembly(tmp_path):
-    lines = _device_asm(tmp_path, os.path.join(build.CSRC, "attend_tiles.hip"))
+    lines = _device_asm(tmp_path, "attend_tiles.hip")
     instrs = [ln.split(";")[0].rstrip() for ln in lines if INSTR.match(ln) and not ln.lstrip().startswith(".")]
     writes = 0
     for i, ins in enumerate(instrs):
