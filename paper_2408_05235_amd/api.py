@@ -469,28 +469,32 @@ def tl_attend(query, key_pages, value_pages, page_table, length, q_offset=None, 
     return (out, lse) if want_lse else out
 
 
-def _pages(ref, page_table, length, page_tokens, work):
+def _pages(ref, page_table, length, page_tokens):
     _need(ref, torch.int32, "ref")
     _need(page_table, torch.int32, "page_table")
     if ref.dim() != 1 or page_table.dim() != 2:
         raise ValueError("ref must be [n_pages] and page_table [n_slots, table_width]")
     n_slots, width = page_table.shape
     _need(length, torch.int32, "length", (n_slots,))
-    g = _lib.Pages(_PAGES_SIZE, int(page_tokens), ref.numel(), n_slots, width, 0, _p(ref),
-                   _p(page_table), _p(length))
+    return _lib.Pages(_PAGES_SIZE, int(page_tokens), ref.shape[0], n_slots, width, 0, ref.data_ptr(),
+                      page_table.data_ptr(), length.data_ptr())
+
+
+def _pages_work(g, ref, work):
+    """`work` for the pool's calls on ``g``, checked or allocated."""
+    words = lib().tl_pages_work_words(ctypes.byref(g))
     if work is None:
-        work = torch.empty(lib().tl_pages_work_words(ctypes.byref(g)), dtype=torch.int32, device=ref.device)
-    else:
-        _need(work, torch.int32, "work")
-        if work.numel() < lib().tl_pages_work_words(ctypes.byref(g)):
-            raise ValueError("work is too small (tl_pages_work_words)")
-    return g, work
+        return torch.empty(words, dtype=torch.int32, device=ref.device)
+    if _need(work, torch.int32, "work").numel() < words:
+        raise ValueError("work is too small (tl_pages_work_words)")
+    return work
 
 
 def tl_pages_extend(ref, page_table, length, add, page_tokens, status=None, work=None):
     """Room for ``add`` [n_slots] int32 more tokens in every slot, in place
     (tl_pages_extend).  Returns status [n_slots] int32 (PAGES_* codes)."""
-    g, work = _pages(ref, page_table, length, page_tokens, work)
+    g = _pages(ref, page_table, length, page_tokens)
+    work = _pages_work(g, ref, work)
     _need(add, torch.int32, "add", (g.n_slots,))
     if status is None:
         status = torch.empty(g.n_slots, dtype=torch.int32, device=ref.device)
@@ -503,7 +507,8 @@ def tl_pages_fork(ref, page_table, length, parent, child, page_tokens, work=None
     """Empty slots ``child`` become copies of slots ``parent`` (int32 [F]), in
     place (tl_pages_fork).  Returns (copy_src, copy_dst, status) int32 [F]; the
     pages still have to be copied (tl_pages_copy)."""
-    g, work = _pages(ref, page_table, length, page_tokens, work)
+    g = _pages(ref, page_table, length, page_tokens)
+    work = _pages_work(g, ref, work)
     F = parent.numel()
     _need(parent, torch.int32, "parent", (F,))
     _need(child, torch.int32, "child", (F,))
@@ -516,13 +521,8 @@ def tl_pages_fork(ref, page_table, length, parent, child, page_tokens, work=None
 
 def tl_pages_free(ref, page_table, length, slots, page_tokens):
     """The sequences in ``slots`` (int32) leave, in place (tl_pages_free)."""
+    g = _pages(ref, page_table, length, page_tokens)
     _need(slots, torch.int32, "slots")
-    _need(ref, torch.int32, "ref")
-    _need(page_table, torch.int32, "page_table")
-    n_slots, width = page_table.shape
-    _need(length, torch.int32, "length", (n_slots,))
-    g = _lib.Pages(_PAGES_SIZE, int(page_tokens), ref.numel(), n_slots, width, 0, _p(ref),
-                   _p(page_table), _p(length))
     check(lib().tl_pages_free(ctypes.byref(g), slots.numel(), _p(slots), _stream()))
 
 
@@ -531,7 +531,8 @@ def tl_pages_compact(ref, page_table, length, page_tokens, out=None, work=None):
     dict with the state after it (ref, page_table; taken from ``out``, which may
     hold the arguments themselves, or allocated) and the moves (copy_src,
     copy_dst, n_copies [1], all int32), which tl_pages_copy has to make."""
-    g, work = _pages(ref, page_table, length, page_tokens, work)
+    g = _pages(ref, page_table, length, page_tokens)
+    work = _pages_work(g, ref, work)
     o = out or {}
 
     def buf(name, shape):

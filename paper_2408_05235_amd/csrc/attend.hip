@@ -24,11 +24,12 @@ namespace {
 constexpr int kFewWaves = 4, kFewThreads = kFewWaves * kWave;
 
 // Three wavefronts a SIMD (12 steps of 16 KB on their way in a CU): 105 us
-// with them and 113 us with two for 4 sequences of 20011 to 36864 tokens.
-template <bool F16, int DP, bool EXACT>
-__global__ __launch_bounds__(kFewThreads, DP > 128 ? 1 : 3) void few_rows_kernel(AttendLaunch F) {
-    __shared__ FewLds<kFewWaves, DP> lds;
-    few_rows<F16, DP, EXACT, kFewWaves, true>(F, blockIdx.x, lds);
+// with them and 113 us with two for 4 sequences of 20011 to 36864 tokens.  (Two
+// of a workgroup of eight: wide_few.)
+template <bool F16, int DP, bool EXACT, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave, DP > 128 ? 1 : WAVES > 4 ? 2 : 3) void few_rows_kernel(AttendLaunch F) {
+    __shared__ FewLds<WAVES, DP> lds;
+    few_rows<F16, DP, EXACT, WAVES, true>(F, blockIdx.x, lds);
 }
 
 // A wavefront per slot: first those of few_rows, then those of tile_rows.
@@ -56,13 +57,20 @@ __global__ __launch_bounds__(kFewThreads) void join_kernel(AttendLaunch F, int64
     join_row<F16, LANES>(P, F.tiles, to, to);
 }
 
+template <bool F16, int DP, int WAVES>
+hipError_t launch_waves(const AttendLaunch& f, int64_t blocks, hipStream_t stream) {
+    if (!grid_fits(blocks * f.few.count, WAVES * kWave)) return hipErrorInvalidConfiguration;
+    const dim3 grid((unsigned)(blocks * f.few.count)), block(WAVES * kWave);
+    if (f.a.c.head_dim == DP) hipLaunchKernelGGL((few_rows_kernel<F16, DP, true, WAVES>), grid, block, 0, stream, f);
+    else hipLaunchKernelGGL((few_rows_kernel<F16, DP, false, WAVES>), grid, block, 0, stream, f);
+    return hipGetLastError();
+}
+
 template <bool F16, int DP>
 hipError_t launch_few(const AttendLaunch& f, int64_t blocks, hipStream_t stream) {
-    if (!grid_fits(blocks * f.few.count, kFewThreads)) return hipErrorInvalidConfiguration;
-    const dim3 grid((unsigned)(blocks * f.few.count)), block(kFewThreads);
-    if (f.a.c.head_dim == DP) hipLaunchKernelGGL((few_rows_kernel<F16, DP, true>), grid, block, 0, stream, f);
-    else hipLaunchKernelGGL((few_rows_kernel<F16, DP, false>), grid, block, 0, stream, f);
-    return hipGetLastError();
+    if constexpr (DP <= 128)
+        if (f.wide) return launch_waves<F16, DP, 2 * kFewWaves>(f, blocks, stream);
+    return launch_waves<F16, DP, kFewWaves>(f, blocks, stream);
 }
 
 template <bool F16, int DP>
@@ -99,13 +107,30 @@ constexpr SplitRule kSplitMixed = {512, 8 * kFewTile, 8192};
 // tile_rows: a workgroup a CU; of half the CUs in a batch of more sequences
 // than row tiles, whose other sequences have few rows and read meanwhile (two
 // chunks of 512 tokens with 62 single tokens: 721 us so, 874 us on all CUs).
-constexpr SplitRule kSplitTiles = {256, 512, INT64_MAX}, kSplitHalf = {128, 512, INT64_MAX};
+constexpr SplitRule kSplitTiles = {256, 256, INT64_MAX}, kSplitHalf = {128, 256, INT64_MAX};
 constexpr int64_t kMostParts = 256;
 
-int64_t wanted_parts(const AttendParams& p, const SplitRule& rule, int64_t blocks) {
+// Tokens that a sequence's rows see at most, from what the host knows.
+int64_t most_tokens(const AttendParams& p) {
     int64_t tokens = (int64_t)p.c.table_width * p.c.page_tokens;
     if (p.max_length > 0) tokens = std::min<int64_t>(tokens, p.max_length);
     if (p.window > 0) tokens = std::min<int64_t>(tokens, (int64_t)p.window + p.sinks);
+    return tokens;
+}
+
+// Whether few_rows takes each sequence in one part with eight wavefronts: up
+// to three of their steps, on up to a workgroup a CU.  8 heads of 500 tokens:
+// 10.1 us so, 13.3 in four parts and a join; of 700 12.1 and 13.2, of 1000 16.8 and
+// 13.2; 256 of 500 15.4 and 19.8.  Heads of more than 128 elements leave no
+// registers for two steps a SIMD (8 of 400 tokens 21.4 and 14.0).
+bool wide_few(const AttendParams& p) {
+    const int64_t tokens = most_tokens(p);
+    return !needs_tiles(p) && p.c.head_dim <= 128 && few_blocks(p) <= 256 && tokens > 2 * kFewWaves * kFewTile &&
+           tokens <= 6 * kFewWaves * kFewTile;
+}
+
+int64_t wanted_parts(const AttendParams& p, const SplitRule& rule, int64_t blocks) {
+    const int64_t tokens = most_tokens(p);
     // A join costs 4 to 5 us with its launch.  It does not pay for two parts'
     // tokens (8 heads of 250: 10.0 us in one, 14.1 in two), nor for short sequences
     // that nearly fill the chip (512 workgroups of 600: 29.9 and 34.8 us; of 16
@@ -116,7 +141,9 @@ int64_t wanted_parts(const AttendParams& p, const SplitRule& rule, int64_t block
     return std::max<int64_t>(1, std::min(n, kMostParts));
 }
 const SplitRule& few_rule(const AttendParams& p) { return needs_tiles(p) ? kSplitMixed : kSplitFew; }
-int64_t few_parts(const AttendParams& p) { return needs_few(p) ? wanted_parts(p, few_rule(p), few_blocks(p)) : 1; }
+int64_t few_parts(const AttendParams& p) {
+    return !needs_few(p) || wide_few(p) ? 1 : wanted_parts(p, few_rule(p), few_blocks(p));
+}
 // (workgroups without those that a ragged batch adds: too many parts cost
 // less than too few)
 int64_t tile_parts(const AttendParams& p) {
@@ -178,6 +205,7 @@ hipError_t launch_attend(const AttendParams& p, hipStream_t stream) {
     f.score_scale = p.scale * kLog2e;
     f.row_tiles = few_row_tiles(p);
     f.slot_rows = few_slot_rows(p);
+    f.wide = wide_few(p);
     f.few = take_parts(&f.a, few_rule(p).least, few_slots(p), few_parts(p));
     f.tiles = take_parts(&f.a, kSplitTiles.least, tile_slots(p), tile_parts(p));
     f.tile_count = p.c.n_tokens * p.group / tile_rows_of(p.c.head_dim) + p.c.n_seqs;

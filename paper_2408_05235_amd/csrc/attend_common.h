@@ -125,6 +125,7 @@ struct AttendLaunch {
                             // sequence and KV head
     int32_t row_tiles;      // ... row tiles of a sequence and head
     int32_t slot_rows;      // ... slots of a sequence and head
+    bool wide;              // ... with eight wavefronts a workgroup
     Parts tiles;            // of the others: a slot per token and head
     int64_t tile_count;     // row tiles, gaps included
 };
