@@ -512,8 +512,7 @@ def tl_pages_fork(ref, page_table, length, parent, child, page_tokens, work=None
     F = parent.numel()
     _need(parent, torch.int32, "parent", (F,))
     _need(child, torch.int32, "child", (F,))
-    three = torch.empty((3, F), dtype=torch.int32, device=ref.device)
-    src, dst, status = three[0], three[1], three[2]
+    src, dst, status = torch.empty((3, F), dtype=torch.int32, device=ref.device).unbind(0)
     check(lib().tl_pages_fork(ctypes.byref(g), F, _p(parent), _p(child), _p(src), _p(dst), _p(status), _p(work),
                               _stream()))
     return src, dst, status
@@ -532,16 +531,21 @@ def tl_pages_compact(ref, page_table, length, page_tokens, out=None, work=None):
     hold the arguments themselves, or allocated) and the moves (copy_src,
     copy_dst, n_copies [1], all int32), which tl_pages_copy has to make."""
     g = _pages(ref, page_table, length, page_tokens)
-    work = _pages_work(g, ref, work)
-    o = out or {}
+    o, half = out or {}, ref.shape[0] // 2
+    # what is not given comes in as few allocations as can be
+    sizes = [half, half, 1, lib().tl_pages_work_words(ctypes.byref(g)) if work is None else 0]
+    moves = list(torch.empty(sum(sizes), dtype=torch.int32, device=ref.device).split(sizes))
+    work = moves.pop() if work is None else _pages_work(g, ref, work)
 
-    def buf(name, shape):
-        t = o.get(name) if o.get(name) is not None else torch.empty(shape, dtype=torch.int32, device=ref.device)
+    def buf(name, shape, default=None):
+        t = o.get(name)
+        if t is None:
+            return torch.empty(shape, dtype=torch.int32, device=ref.device) if default is None else default
         return _need(t, torch.int32, name, shape)
 
-    half = ref.numel() // 2
-    r = dict(ref=buf("ref", (ref.numel(),)), page_table=buf("page_table", tuple(page_table.shape)),
-             copy_src=buf("copy_src", (half,)), copy_dst=buf("copy_dst", (half,)), n_copies=buf("n_copies", (1,)))
+    r = dict(ref=buf("ref", ref.shape), page_table=buf("page_table", page_table.shape),
+             copy_src=buf("copy_src", (half,), moves[0]), copy_dst=buf("copy_dst", (half,), moves[1]),
+             n_copies=buf("n_copies", (1,), moves[2]))
     check(lib().tl_pages_compact(ctypes.byref(g), _p(r["ref"]), _p(r["page_table"]), _p(r["copy_src"]),
                                  _p(r["copy_dst"]), _p(r["n_copies"]), _p(work), _stream()))
     return r

@@ -81,7 +81,7 @@ tl_status attend_params(const tl_attend_args* a, const char* who, tl::AttendPara
     if (a->n_heads < 1 || a->n_heads % a->cache.n_kv_heads != 0)
         return fail(TL_EINVAL, "%s: n_heads %d is not a positive multiple of n_kv_heads %d", who, a->n_heads,
                     a->cache.n_kv_heads);
-    if (!(a->scale > 0.0f) || !std::isfinite(a->scale))
+    if (!(a->scale > 0.0f) || !std::isfinite(a->scale * 2.0f))      // (x log2 e below)
         return fail(TL_EINVAL, "%s: scale must be finite and positive", who);
     if (a->window < 0 || a->sinks < 0) return fail(TL_EINVAL, "%s: window or sinks < 0", who);
     if (a->max_length < 0) return fail(TL_EINVAL, "%s: max_length %d < 0", who, a->max_length);

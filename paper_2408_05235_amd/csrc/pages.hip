@@ -22,7 +22,9 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 constexpr int kAppendThreads = 256;
 constexpr int kAppendTokens = 16;       // most tokens of a workgroup
 
-// One workgroup moves `tokens` consecutive rows, 16 bytes per lane.
+// One workgroup moves `tokens` consecutive rows, 16 bytes per lane.  Bound by
+// memory: 65415 tokens of 8 heads of 128 (536 MB) take 111 us, 4.8 TB/s; 64
+// tokens 3 us, a launch and four round trips.
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendParams P, int tokens) {
     const CacheView& c = P.c;
     __shared__ int64_t dst[kAppendTokens];
@@ -180,7 +182,7 @@ __device__ __forceinline__ Wish wish(const PagesParams& P, int32_t length, int32
 // One workgroup: (1) where each slot's pages begin among the free ones, (2)
 // the free pages, (3) page k to the slot that it falls to (found in the starts,
 // which are sorted), (4) lengths and statuses.  A chain of memory round
-// trips, not work: 64 slots of a pool of 131072 pages take 6 us.
+// trips, not work: 80 slots of a pool of 131072 pages take 7.8 us.
 __global__ __launch_bounds__(kPoolThreads) void extend_kernel(PagesParams P, const int32_t* add, int32_t* status,
                                                               int32_t* work) {
     __shared__ PoolLds lds;
@@ -228,7 +230,8 @@ __global__ __launch_bounds__(kPoolThreads) void extend_kernel(PagesParams P, con
 
 // One workgroup decides the forks: validity (of several with one child the
 // first counts), which need a page, and which page that is.  work[n_slots + f]:
-// the child's length, -1 where the fork is not served.
+// the child's length, -1 where the fork is not served.  Latency: 64 forks
+// 7.3 us, their rows in a launch of their own 2.8 (17.8 in this one).
 __global__ __launch_bounds__(kPoolThreads) void fork_kernel(PagesParams P, int64_t n_forks, const int32_t* parent,
                                                             const int32_t* child, int32_t* copy_src,
                                                             int32_t* copy_dst, int32_t* status, int32_t* work) {
@@ -473,7 +476,9 @@ __global__ __launch_bounds__(256) void remap_kernel(PagesParams P, CompactWork W
 constexpr int kCopyThreads = 256;
 
 // A workgroup copies whole pages, 64 bytes per lane and step: four loads are
-// under way before the first store waits.
+// under way before the first store waits.  Past the caches, which would only lose
+// what others read: 13286 pages of 8 KB in 8 planes (1.7 GB) 0.31 ms, 5.3 TB/s
+// (0.33 ms through them).
 __global__ __launch_bounds__(kCopyThreads) void copy_kernel(CopyParams P) {
     int64_t pairs = P.n_pairs;
     if (P.n_live) pairs = min(pairs, (int64_t)max(*P.n_live, 0));
