@@ -514,7 +514,9 @@ tl_status tl_kv_append(const tl_kv_append_args* args, void* stream);
  * -inf.  What lies in pages beyond the visible tokens, infinities and NaN
  * included, is not used.  Rows that belong to no sequence are left alone.
  *
- * Scores, the softmax's maximum and sum and the output's sums are fp32.
+ * Scores, the softmax's maximum and sum and the output's sums are fp32.  The
+ * weights are rounded to the cache's type for the product with the values (in f16
+ * scaled up, so that small ones do not vanish), the output once at the end.
  * workspace: device memory of the caller, 16-byte aligned, for the parts of
  * sequences that are split over their length and joined;
  * tl_attend_workspace_bytes(args) says how much a call can use.  With less, or

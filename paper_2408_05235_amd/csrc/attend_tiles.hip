@@ -432,7 +432,7 @@ __device__ __forceinline__ void tile_rows(const AttendLaunch& F, int64_t block, 
                 top = fmaxf(top, other_half(top));
                 // The sums are only scaled down when the maximum has grown by
                 // more than 2^8 for some row: weights up to 2^8 lose nothing.
-                const float m2 = fmaxf(m, top * F.score_scale);
+                const float m2 = fmaxf(m, reference<F16, kLiftTiles>(top, F.score_scale));
                 if (__any(m2 > m + 8.0f)) {
                     const float keep = exp2_fast(m - m2);
                     l *= keep;

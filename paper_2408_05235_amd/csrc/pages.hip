@@ -65,7 +65,7 @@ constexpr int kBallots = 16;            // of 64 pages, per wavefront and step
 __host__ __device__ inline int64_t work_list(const PagesParams& p) { return 3 * p.n_slots; }
 
 // What one workgroup decides about few slots stays in LDS, and with many in
-// the work array.
+// the work array: 4096 slots 22 us so, 34 there.
 constexpr int kLdsSlots = 4096, kLdsList = 4096;
 struct PoolLds {
     int32_t starts[kLdsSlots];
@@ -506,7 +506,8 @@ __global__ __launch_bounds__(kCopyThreads) void copy_kernel(CopyParams P) {
 }  // namespace
 
 hipError_t launch_append(const AppendParams& p, hipStream_t stream) {
-    // few tokens: one a workgroup, so that they are spread over the chip
+    // few tokens: one a workgroup, so that they are spread over the chip (4095
+    // 8.0 us so, 8.5 with 16); many: 16, which saves workgroups (65415 112 us, 152)
     const int tokens = p.c.n_tokens < 4096 ? 1 : kAppendTokens;
     const int64_t blocks = (p.c.n_tokens + tokens - 1) / tokens;
     if (!grid_fits(blocks, kAppendThreads)) return hipErrorInvalidConfiguration;

@@ -110,6 +110,33 @@ def test_peaked_and_low_scores(gpu):
     cc.check(c, *run(c))
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("new", [1, 20])
+def test_many_small_weights(gpu, dtype, new):
+    """One token outweighs each of 32768 others by e^18 (2^26), and its value
+    is 0: what is left of the output is the others'.  A weight may be off by 2^-8 of
+    itself (bf16; 2^-11 in f16), and in f16 by 2^-31 of the largest, the output by
+    2^-8 (2^-11) of itself."""
+    L, dim = 32768, 64
+    c = cc.make(17, dtype, 2, 1, dim, 16, [L], [new])
+    c["q"] = torch.zeros(new, 2, dim, dtype=cc.DTYPES[dtype], device="cuda")
+    c["q"][:, :, 3] = 1.0
+    c["k"].zero_()
+    c["v"].fill_(1.0)
+    at = 700
+    page = int(c["table"][0, at // 16])
+    c["k"][page, 0, at % 16, 3] = 18.0
+    c["v"][page, 0, at % 16] = 0.0
+    out, lse = run(c, scale=1.0)
+    others = torch.arange(L, L + new, device="cuda").double()[:, None, None]
+    all = math.exp(18.0) + others
+    exact = others / all
+    u = 2.0 ** -11 if dtype == "f16" else 2.0 ** -8
+    tol = exact * (2.1 * u + 2.0 ** -14) + (2.0 ** -31 * others if dtype == "f16" else 0)
+    assert bool(((out.double() - exact).abs() <= tol).all()), (float(out[0, 0, 0]), float(exact[0, 0, 0]))
+    assert bool(((lse.double() - torch.log(all)[:, :, 0]).abs() <= 2.0 ** -17).all())
+
+
 def test_scale(gpu):
     c = cc.make(8, "f16", 4, 2, 64, 16, [100, 0], [1, 70])
     cc.check(c, *run(c, scale=0.7), scale=0.7)
