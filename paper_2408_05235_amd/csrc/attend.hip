@@ -35,13 +35,17 @@ __global__ __launch_bounds__(WAVES * kWave, DP > 128 ? 1 : WAVES > 4 ? 2 : 3) vo
     few_rows<F16, DP, EXACT, WAVES, true>(F, blockIdx.x, lds);
 }
 
-// A wavefront per slot: first those of few_rows, then those of tile_rows.  4 us
-// with its launch where there is little to join, 7.5 us for 256 rows of 24 parts.
-template <bool F16, int LANES>
+// Four wavefronts per slot where there are many parts, else one: first the
+// slots of few_rows, then those of tile_rows.  4 us with its launch where there is
+// little to join.  With four: 8 heads of 36864 tokens, 96 parts, attention and
+// join 37.3 us, 47.9 with one; 1 head of 131072, 229 parts, 32.8 and 61.2.  Of a few parts
+// each one is better (384 rows of 2: 76.9 and 78.3 us; 1024 of 9, with tile_rows: 19.2 and
+// 20.6).
+template <bool F16, int LANES, int WAVES>
 __global__ __launch_bounds__(kFewThreads) void join_kernel(AttendLaunch F, int64_t few_slots) {
     const AttendParams& P = F.a;
     const CacheView& c = P.c;
-    const int64_t slot = (int64_t)blockIdx.x * kFewWaves + threadIdx.x / kWave;
+    const int64_t slot = WAVES > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * kFewWaves + threadIdx.x / kWave;
     if (slot < few_slots) {
         const int64_t x = slot / F.slot_rows, row = slot % F.slot_rows;
         const int32_t kvh = (int32_t)(x % c.n_kv_heads);
@@ -50,7 +54,7 @@ __global__ __launch_bounds__(kFewThreads) void join_kernel(AttendLaunch F, int64
         const int64_t rows = (int64_t)s.n * P.group;
         if ((c.q_offset && rows > kFewRows) || row >= rows) return;
         const int64_t token = row / P.group;
-        join_row<F16, LANES>(P, F.few, slot, (s.first + token) * P.n_heads + kvh * P.group + (row - token * P.group));
+        join_row<F16, LANES, WAVES>(P, F.few, slot, (s.first + token) * P.n_heads + kvh * P.group + (row - token * P.group));
         return;
     }
     const int64_t to = slot - few_slots, i = to / P.n_heads;
@@ -58,7 +62,7 @@ __global__ __launch_bounds__(kFewThreads) void join_kernel(AttendLaunch F, int64
     if (i >= c.n_tokens || !find_seq(c, i, &b)) return;
     const SeqRows s = seq_rows(c, b);
     if (i < s.first || i - s.first >= s.n || (int64_t)s.n * P.group <= kFewRows) return;
-    join_row<F16, LANES>(P, F.tiles, to, to);
+    join_row<F16, LANES, WAVES>(P, F.tiles, to, to);
 }
 
 template <bool F16, int DP, int WAVES>
@@ -79,9 +83,16 @@ hipError_t launch_few(const AttendLaunch& f, int64_t blocks, hipStream_t stream)
 
 template <bool F16, int DP>
 hipError_t launch_join(const AttendLaunch& f, int64_t few_slots, int64_t tile_slots, hipStream_t stream) {
-    const int64_t blocks = (few_slots + tile_slots + kFewWaves - 1) / kFewWaves;
+    const int64_t slots = few_slots + tile_slots;
+    if (std::max(f.few.count, f.tiles.count) > 16) {
+        if (!grid_fits(slots, kFewThreads)) return hipErrorInvalidConfiguration;
+        hipLaunchKernelGGL((join_kernel<F16, DP / 4, kFewWaves>), dim3((unsigned)slots), dim3(kFewThreads), 0, stream, f,
+                           few_slots);
+        return hipGetLastError();
+    }
+    const int64_t blocks = (slots + kFewWaves - 1) / kFewWaves;
     if (!grid_fits(blocks, kFewThreads)) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((join_kernel<F16, DP / 4>), dim3((unsigned)blocks), dim3(kFewThreads), 0, stream, f, few_slots);
+    hipLaunchKernelGGL((join_kernel<F16, DP / 4, 1>), dim3((unsigned)blocks), dim3(kFewThreads), 0, stream, f, few_slots);
     return hipGetLastError();
 }
 
@@ -103,8 +114,10 @@ bool needs_tiles(const AttendParams& p) { return p.c.q_offset && p.c.n_tokens * 
 struct SplitRule {
     int64_t fill, least, most;
 };
-// few_rows: three workgroups a CU; a step of each wavefront; and parts
-// short enough that a long sequence does not end alone.
+// few_rows: three workgroups a CU (4 sequences of 20011 to 36864 tokens, 8
+// heads: 96 us; with 512 workgroups 116, with 384 131); a step of each wavefront; and
+// parts short enough that a long sequence does not end alone (96 of 16 to 36864
+// tokens: 1.19 ms, unsplit 1.46).
 constexpr SplitRule kSplitFew = {768, kFewWaves * kFewTile, 8192};
 // few_rows beside tile_rows: a workgroup of up to 8 wavefronts a CU.
 constexpr SplitRule kSplitMixed = {512, 8 * kFewTile, 8192};
@@ -141,6 +154,11 @@ int64_t wanted_parts(const AttendParams& p, const SplitRule& rule, int64_t block
     // to 1280, 48.9 and 46.3).
     int64_t fill = std::min((rule.fill + blocks - 1) / blocks, (tokens + rule.least - 1) / rule.least);
     if (tokens <= 2 * rule.least || (3 * blocks >= 2 * rule.fill && tokens < 8 * rule.least)) fill = 1;
+    // Each further part makes the join longer by as much as it takes off the
+    // parts when there are sqrt(0.4 tokens): 1 head of 20000 tokens in 64, 128 and
+    // 157 parts 15.4, 16.3 and 17.2 us; 2 of 36864 in 64, 128 and 256 22.9, 20.6 and 24.9;
+    // 1 of 131072 53.0, 36.3 and 32.8.
+    while (fill > 1 && 5 * fill * fill > 2 * tokens) --fill;
     const int64_t n = std::max(fill, tokens / rule.most + (tokens % rule.most != 0));
     return std::max<int64_t>(1, std::min(n, kMostParts));
 }
@@ -150,12 +168,24 @@ int64_t few_parts(const AttendParams& p) {
     if (!needs_few(p) || wide_few(p) || (needs_tiles(p) && p.c.n_seqs == 1)) return 1;
     return wanted_parts(p, few_rule(p), few_blocks(p));
 }
-// (workgroups without those that a ragged batch adds: too many parts cost
-// less than too few)
+// (Workgroups without those that a ragged batch adds: too many parts cost
+// less than too few.)  Rows are many here, and so are the parts' sums, which are
+// written and read in 32 bits: as many parts as make their time, 26 ns a token,
+// and that of the join least.  A prompt of 1000 tokens, 32 heads on 8: 37 us
+// in one part, 55 in three; 512 new tokens behind 16384: 153 us in four, 439 in one;
+// 64: 41 us in 32, 423 in one.
 int64_t tile_parts(const AttendParams& p) {
     if (!needs_tiles(p)) return 1;
     const int64_t tiles = std::max<int64_t>(1, p.c.n_tokens * p.group / tile_rows_of(p.c.head_dim));
-    return wanted_parts(p, p.c.n_seqs > tiles ? kSplitHalf : kSplitTiles, tiles * p.c.n_kv_heads);
+    const int64_t most = wanted_parts(p, p.c.n_seqs > tiles ? kSplitHalf : kSplitTiles, tiles * p.c.n_kv_heads);
+    const int64_t sums = tile_slots(p) * p.c.head_dim * 2 * (int64_t)sizeof(float);     // bytes, of a part
+    auto cost = [&](int64_t parts) {                                                    // ns, at 4.5 TB/s
+        return most_tokens(p) * 26 / parts + (parts > 1 ? 5000 + sums * parts / 4500 : 0);
+    };
+    int64_t best = 1;
+    for (int64_t n = 2; n <= most; ++n)
+        if (cost(n) < cost(best)) best = n;
+    return best;
 }
 
 constexpr int64_t kAlign = 256;

@@ -226,14 +226,17 @@ __device__ RowSums row_alone(const AttendParams& P, int64_t b, int64_t token, in
     return r;
 }
 
-// A wavefront joins the parts of a slot, in their order, to output row `to`
-// (token x n_heads + head): one lane looks at each part's statistics, then
-// LANES lanes with 4 elements each take every (64 / LANES)th part.  Nothing
-// waits for the part before: a part without weight is read all the same and
-// left out by its factor of 0.
-template <bool F16, int LANES>
+// WAVES wavefronts join the parts of a slot, in an order that the parts' number
+// gives, to output row `to` (token x n_heads + head): each looks at all parts'
+// statistics, a part a lane; then LANES lanes with 4 elements each take every
+// (WAVES x 64 / LANES)th part.  Nothing waits for the part before: a part without
+// weight is read all the same and left out by its factor of 0.  With WAVES > 1 the
+// whole workgroup works on one slot.
+template <bool F16, int LANES, int WAVES>
 __device__ __forceinline__ void join_row(const AttendParams& P, const Parts& parts, int64_t slot, int64_t to) {
     constexpr int kGroups = kWave / LANES;
+    __shared__ f32x4 sums_of[WAVES > 1 ? WAVES - 1 : 1][LANES];
+    const int wave = WAVES > 1 ? threadIdx.x / kWave : 0;
     const int lane = lane_id(), n = parts.count, D = P.c.head_dim;
     const float2* const st = (const float2*)parts.stats + slot * n;
     const float* const sums = parts.sums + slot * n * D;
@@ -250,7 +253,7 @@ __device__ __forceinline__ void join_row(const AttendParams& P, const Parts& par
         all = fmaf(y.y, f, all);
         const int m = min(n - k0, kWave);
 #pragma unroll 8
-        for (int k = 0; k < m; k += kGroups) {
+        for (int k = wave * kGroups; k < m; k += WAVES * kGroups) {
             const int part = min(k + group, m - 1);
             const float there = __shfl(f, part), w = k + group < m ? there : 0.0f;
             f32x4 v = {0, 0, 0, 0};
@@ -265,6 +268,17 @@ __device__ __forceinline__ void join_row(const AttendParams& P, const Parts& par
     for (int s = LANES; s < kWave; s <<= 1)
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], s);
+    if constexpr (WAVES > 1) {
+        if (wave > 0 && group == 0) sums_of[wave - 1][lane] = o;
+        __syncthreads();
+        if (wave > 0) return;
+#pragma unroll
+        for (int w = 0; w < WAVES - 1; ++w) {
+            const f32x4 y = sums_of[w][lane % LANES];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += y[e];
+        }
+    }
     const float f = all == 0.0f ? 0.0f : 1.0f / all;
     if (all == 0.0f) o = f32x4{0, 0, 0, 0};
     if (group == 0 && d < D)
