@@ -441,7 +441,7 @@ def tl_attend(query, key_pages, value_pages, page_table, length, q_offset=None, 
     given; ``max_length`` is an upper bound of ``length`` where the caller
     knows one.  ``workspace`` is an uint8 tensor (as many bytes as the call can
     use are allocated when None).  Returns out [T, n_heads, head_dim], and the
-    log-sums [T, n_heads] fp32 too with ``want_lse``."""
+    log-sums [T, n_heads] fp32 too with ``want_lse``.  For serving: no gradients."""
     v = _kv_view(key_pages, value_pages, page_table, length)
     dtype, shape, device = key_pages.dtype, query.shape, query.device
     qs = _rows3(query, dtype, "query", None, key_pages.shape[3])

@@ -26,9 +26,9 @@ constexpr int kFewWaves = 4, kFewThreads = kFewWaves * kWave;
 
 // Bound by reading: 256 sequences of up to 4352 tokens, 20 heads with their
 // own keys, take 0.90 ms, 6.3 TB/s (a copy of 2 GiB reaches 4.95).  Three
-// wavefronts a SIMD (12 steps of 16 KB on their way in a CU): 105 us
-// with them and 113 us with two for 4 sequences of 20011 to 36864 tokens.  (Two
-// of a workgroup of eight: wide_few.)
+// wavefronts a SIMD (12 steps of 16 KB on their way in a CU): 0.93 ms with two, and
+// 97 and 108 us for 4 sequences of 20011 to 36864 tokens.  (Two of a workgroup of
+// eight: wide_few.)
 template <bool F16, int DP, bool EXACT, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave, DP > 128 ? 1 : WAVES > 4 ? 2 : 3) void few_rows_kernel(AttendLaunch F) {
     __shared__ FewLds<WAVES, DP> lds;
@@ -123,7 +123,7 @@ constexpr SplitRule kSplitFew = {768, kFewWaves * kFewTile, 8192};
 constexpr SplitRule kSplitMixed = {512, 8 * kFewTile, 8192};
 // tile_rows: a workgroup a CU; of half the CUs in a batch of more sequences
 // than row tiles, whose other sequences have few rows and read meanwhile (two
-// chunks of 512 tokens with 62 single tokens: 721 us so, 874 us on all CUs).
+// chunks of 512 tokens with 62 single tokens: 712 us so, 869 us on all CUs).
 constexpr SplitRule kSplitTiles = {256, 256, INT64_MAX}, kSplitHalf = {128, 256, INT64_MAX};
 constexpr int64_t kMostParts = 256;
 

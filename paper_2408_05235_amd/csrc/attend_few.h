@@ -40,7 +40,7 @@ struct FewLds {
 // tokens, 20 heads of 128: 0.90 ms, 0.93 with them; a prompt of 8192 in tile_rows, 8
 // heads of 256: 0.36 and 0.39).
 // STREAM: keys and values are read once and not kept in the caches (256
-// requests 901 us, 968 without; but 780 and 717 us beside tile_rows).
+// requests 902 us, 968 without; but 780 and 717 us beside tile_rows).
 template <bool F16, int DP, bool EXACT, int WAVES, bool STREAM>
 __device__ __forceinline__ void few_rows(const AttendLaunch& F, int64_t block, FewLds<WAVES, DP>& lds) {
     constexpr int kThreads = WAVES * kWave;

@@ -118,8 +118,8 @@ __device__ __forceinline__ int value_exchange(int token) {
 // registers hold one wavefront, which takes the phases in turn.)  Copies of later
 // steps are issued between the matrix instructions, one at a time.
 //
-// 32768 tokens through a window of 4096, 8 heads on one KV head: 0.56 ms, 918
-// TFLOP/s; 8 ragged prompts of up to 4096 tokens, 32 heads on 8: 0.55 ms, 800
+// 32768 tokens through a window of 4096, 8 heads on one KV head: 0.57 ms, 909
+// TFLOP/s; 8 ragged prompts of up to 4096 tokens, 32 heads on 8: 0.55 ms, 795
 // (a 16384^3 product of the library: 1363).  What bounds it is the power budget:
 // the clock falls to 1.7 to 1.9 GHz, and a step takes 4040 cycles of which the matrix
 // units are busy 2048.  A wavefront gets 32 bytes a cycle from LDS, just what its
@@ -513,7 +513,7 @@ __device__ __forceinline__ void tile_rows(const AttendLaunch& F, int64_t block, 
 
 // Workgroups of tile_rows first, then those of few_rows: compute on some CUs
 // and reading on the others.  Two chunks of 512 tokens and 62 single tokens over
-// 9001 to 16384 cached ones: 0.72 ms, 1.00 in two launches.
+// 9001 to 16384 cached ones: 0.71 ms, 1.00 in two launches.
 template <bool F16, int DP, bool EXACT>
 __global__ __launch_bounds__(tile_waves(DP) * kWave, DP > 128 ? 1 : 2) void mixed_kernel(AttendLaunch F) {
     __shared__ union {
