@@ -126,6 +126,7 @@ constexpr SplitRule kSplitMixed = {512, 8 * kFewTile, 8192};
 // chunks of 512 tokens with 62 single tokens: 712 us so, 869 us on all CUs).
 constexpr SplitRule kSplitTiles = {256, 256, INT64_MAX}, kSplitHalf = {128, 256, INT64_MAX};
 constexpr int64_t kMostParts = 256;
+constexpr int64_t kApartBytes = 192 << 20;
 
 // Tokens that a sequence's rows see at most, from what the host knows.
 int64_t most_tokens(const AttendParams& p) {
@@ -146,6 +147,16 @@ bool wide_few(const AttendParams& p) {
            tokens <= 6 * kFewWaves * kFewTile;
 }
 
+// Whether the sequences with few rows get a launch of their own before the
+// others': where most can be such (as when every sequence has one token and the
+// caller gives offsets all the same) and there is much to read.  In one launch
+// tile_rows' LDS leaves them two wavefronts a SIMD: 32 sequences of 2000 tokens, 8
+// heads (262 MB) take 55 us so and 61 in one launch, 64 of 500 (131 MB) 28.6 and 27.8.
+bool apart(const AttendParams& p) {
+    return needs_few(p) && needs_tiles(p) && p.c.n_tokens * p.group <= kFewRows * p.c.n_seqs &&
+           most_tokens(p) * p.c.n_seqs * p.c.n_kv_heads * p.c.head_dim * 4 >= kApartBytes;
+}
+
 int64_t wanted_parts(const AttendParams& p, const SplitRule& rule, int64_t blocks) {
     const int64_t tokens = most_tokens(p);
     // A join costs 4 to 5 us with its launch.  It does not pay for two parts'
@@ -162,12 +173,31 @@ int64_t wanted_parts(const AttendParams& p, const SplitRule& rule, int64_t block
     const int64_t n = std::max(fill, tokens / rule.most + (tokens % rule.most != 0));
     return std::max<int64_t>(1, std::min(n, kMostParts));
 }
-const SplitRule& few_rule(const AttendParams& p) { return needs_tiles(p) ? kSplitMixed : kSplitFew; }
+const SplitRule& few_rule(const AttendParams& p) {
+    return needs_tiles(p) && !apart(p) ? kSplitMixed : kSplitFew;
+}
 // (a lone sequence with many rows leaves none to few_rows)
 int64_t few_parts(const AttendParams& p) {
     if (!needs_few(p) || wide_few(p) || (needs_tiles(p) && p.c.n_seqs == 1)) return 1;
     return wanted_parts(p, few_rule(p), few_blocks(p));
 }
+// How row tiles are numbered.  A sequence of r rows has ceil(r / ROWS), which
+// is at most floor(r / ROWS) + 1, and none if r <= kFewRows, so at most
+// floor(r / (kFewRows + 1)).  A number without a tile is a workgroup that finds out
+// and ends, but holds a CU's LDS for it: 256 sequences with one new token each,
+// 20 heads: 1.18 ms with 257 numbers a head, 0.99 with 15.
+struct TileNumbers {
+    int64_t count;
+    int32_t per;
+    bool each;
+};
+TileNumbers number_tiles(const AttendParams& p) {
+    const int64_t rows = p.c.n_tokens * p.group;
+    const int32_t tile = tile_rows_of(p.c.head_dim), few = kFewRows + 1;
+    if (rows / few < rows / tile + p.c.n_seqs) return {rows / few, few, false};
+    return {rows / tile + p.c.n_seqs, tile, true};
+}
+
 // (Workgroups without those that a ragged batch adds: too many parts cost
 // less than too few.)  Rows are many here, and so are the parts' sums, which are
 // written and read in 32 bits: as many parts as make their time, 26 ns a token,
@@ -177,13 +207,15 @@ int64_t few_parts(const AttendParams& p) {
 int64_t tile_parts(const AttendParams& p) {
     if (!needs_tiles(p)) return 1;
     const int64_t tiles = std::max<int64_t>(1, p.c.n_tokens * p.group / tile_rows_of(p.c.head_dim));
-    const int64_t most = wanted_parts(p, p.c.n_seqs > tiles ? kSplitHalf : kSplitTiles, tiles * p.c.n_kv_heads);
+    const int64_t most = wanted_parts(p, p.c.n_seqs > tiles && !apart(p) ? kSplitHalf : kSplitTiles, tiles * p.c.n_kv_heads);
     const int64_t sums = tile_slots(p) * p.c.head_dim * 2 * (int64_t)sizeof(float);     // bytes, of a part
     auto cost = [&](int64_t parts) {                                                    // ns, at 4.5 TB/s
         return most_tokens(p) * 26 / parts + (parts > 1 ? 5000 + sums * parts / 4500 : 0);
     };
     int64_t best = 1;
-    for (int64_t n = 2; n <= most; ++n)
+    // (numbers without a tile are not split further than over the chip's CUs)
+    const int64_t limit = std::min(most, 1024 / (number_tiles(p).count * p.c.n_kv_heads));
+    for (int64_t n = 2; n <= limit; ++n)
         if (cost(n) < cost(best)) best = n;
     return best;
 }
@@ -215,7 +247,10 @@ template <bool F16, int DP>
 hipError_t launch_dim(const AttendLaunch& f, hipStream_t stream) {
     const AttendParams& p = f.a;
     const int64_t blocks = needs_few(p) ? few_blocks(p) : 0;
-    hipError_t e = needs_tiles(p) ? launch_mixed(f, blocks, stream) : launch_few<F16, DP>(f, blocks, stream);
+    hipError_t e = hipSuccess;
+    const bool alone = apart(p) || !needs_tiles(p);
+    if (alone) e = launch_few<F16, DP>(f, blocks, stream);
+    if (e == hipSuccess && needs_tiles(p)) e = launch_mixed(f, alone ? 0 : blocks, stream);
     const int64_t few = f.few.count > 1 ? few_slots(p) : 0, tiles = f.tiles.count > 1 ? tile_slots(p) : 0;
     if (e == hipSuccess && few + tiles > 0) e = launch_join<F16, DP>(f, few, tiles, stream);
     return e;
@@ -244,7 +279,10 @@ hipError_t launch_attend(const AttendParams& p, hipStream_t stream) {
     f.wide = wide_few(p);
     f.few = take_parts(&f.a, few_rule(p).least, few_slots(p), few_parts(p));
     f.tiles = take_parts(&f.a, kSplitTiles.least, tile_slots(p), tile_parts(p));
-    f.tile_count = p.c.n_tokens * p.group / tile_rows_of(p.c.head_dim) + p.c.n_seqs;
+    const TileNumbers t = number_tiles(p);
+    f.tile_count = t.count;
+    f.tile_per = t.per;
+    f.tile_each = t.each;
     return p.f16 ? launch_type<true>(f, stream) : launch_type<false>(f, stream);
 }
 

@@ -144,6 +144,8 @@ struct AttendLaunch {
     bool wide;              // ... with eight wavefronts a workgroup
     Parts tiles;            // of the others: a slot per token and head
     int64_t tile_count;     // row tiles, gaps included
+    int32_t tile_per;       // ... a number for so many rows
+    bool tile_each;         // ... and one for each sequence
 };
 
 // Sequences of up to so many rows (new tokens x query heads of a KV head) are

@@ -22,21 +22,21 @@ namespace {
 
 constexpr int kKeys = 64;               // cached tokens of a step
 
-// Row tiles are numbered through the batch with gaps: sequence b's begin at
-// floor(q_offset[b] x group / ROWS) + b, which leaves room for all of them, and
-// needs no sum over the batch.
-template <int ROWS>
-__device__ __forceinline__ int64_t first_tile(const AttendParams& P, int64_t b) {
-    return clamp_offset(P.c, P.c.q_offset[b]) * P.group / ROWS + b;
+// Row tiles are numbered through the batch with gaps, which needs no sum over
+// the batch: sequence b's begin at floor(rows before it / ROWS) + b, or, in a batch of
+// mostly few rows, at floor(rows before it / (kFewRows + 1)); both leave room for
+// all of them (number_tiles).
+__device__ __forceinline__ int64_t first_tile(const AttendLaunch& F, int64_t b) {
+    const AttendParams& P = F.a;
+    return clamp_offset(P.c, P.c.q_offset[b]) * P.group / F.tile_per + (F.tile_each ? b : 0);
 }
 
 // The last sequence whose first tile is at most `tile`: 64 ways at a time.
-template <int ROWS>
-__device__ __forceinline__ int64_t tile_seq(const AttendParams& P, int64_t tile) {
-    int64_t lo = 0, hi = P.c.n_seqs;
+__device__ __forceinline__ int64_t tile_seq(const AttendLaunch& F, int64_t tile) {
+    int64_t lo = 0, hi = F.a.c.n_seqs;
     while (hi - lo > 1) {
         const int64_t step = (hi - lo + kWave - 1) / kWave, at = lo + lane_id() * step;
-        const bool below = at < hi && first_tile<ROWS>(P, at) <= tile;
+        const bool below = at < hi && first_tile(F, at) <= tile;
         const int k = max(__popcll(__ballot(below)) - 1, 0);
         lo += k * step;
         hi = min(lo + step, hi);
@@ -166,10 +166,10 @@ __device__ __forceinline__ void tile_rows(const AttendLaunch& F, int64_t block, 
     const int32_t part = (int32_t)(x % F.tiles.count);
     x /= F.tiles.count;
     const int64_t tile = F.tile_count - 1 - x;
-    const int64_t b = tile_seq<kTileRows>(P, tile);
+    const int64_t b = tile_seq(F, tile);
     const SeqRows s = seq_rows(c, b);
     const int64_t rows = (int64_t)s.n * P.group;
-    const int64_t row0 = (tile - first_tile<kTileRows>(P, b)) * kTileRows;
+    const int64_t row0 = (tile - first_tile(F, b)) * kTileRows;
     if (rows <= kFewRows || row0 < 0 || row0 >= rows) return;
 
     const int32_t base = s.length - s.n;                // position of the first new token

@@ -102,6 +102,27 @@ def test_random(gpu, seed):
     cc.check(c, *run(c))
 
 
+@pytest.mark.parametrize("dtype,dim,group,page", [("bf16", 128, 2, 16), ("f16", 64, 1, 16), ("bf16", 256, 2, 24),
+                                                  ("f16", 80, 3, 7)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (90, 3)])
+def test_a_few_long_among_many_single(gpu, dtype, dim, group, page, window, sinks):
+    """Offsets where nearly all sequences have one new token: those with more are
+    found, whatever comes between; with a table so wide that the call may have much to
+    read, and one that has no room for that."""
+    r = np.random.RandomState(dim)
+    new = np.ones(64, np.int64)
+    new[[5, 6, 20, 33, 40, 63]] = 40, 17, 0, 19, 0, 33
+    before = r.randint(0, 200, 64)
+    before[7], before[40] = 0, 50
+    c = cc.make(18, dtype, 8 * group, 8, dim, page, before, new, window, sinks)
+    cc.check(c, *run(c))
+    wide = torch.full((64, 200 * 16 // page), -1, dtype=torch.int32, device="cuda")
+    wide[:, :c["table"].shape[1]] = c["table"]
+    c["table"] = wide
+    cc.check(c, *run(c))
+    cc.check(c, *run(c, max_length=int(c["length"].max())))
+
+
 def test_peaked_and_low_scores(gpu):
     # wide scores: most weights vanish, the largest comes late or early
     c = cc.make(6, "bf16", 8, 2, 128, 16, [600, 0, 3000], [1, 200, 33], spread=6.0)
