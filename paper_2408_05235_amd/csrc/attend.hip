@@ -213,7 +213,7 @@ int64_t tile_parts(const AttendParams& p) {
         return most_tokens(p) * 26 / parts + (parts > 1 ? 5000 + sums * parts / 4500 : 0);
     };
     int64_t best = 1;
-    // (numbers without a tile are not split further than over the chip's CUs)
+    // (at most four workgroups a CU, those of numbers without a tile among them)
     const int64_t limit = std::min(most, 1024 / (number_tiles(p).count * p.c.n_kv_heads));
     for (int64_t n = 2; n <= limit; ++n)
         if (cost(n) < cost(best)) best = n;
