@@ -201,21 +201,24 @@ TileNumbers number_tiles(const AttendParams& p) {
 // (Workgroups without those that a ragged batch adds: too many parts cost
 // less than too few.)  Rows are many here, and so are the parts' sums, which are
 // written and read in 32 bits: as many parts as make their time, 26 ns a token,
-// and that of the join least.  A prompt of 1000 tokens, 32 heads on 8: 37 us
-// in one part, 55 in three; 512 new tokens behind 16384: 153 us in four, 439 in one;
-// 64: 41 us in 32, 423 in one.
+// and that of the join least.  A prompt of 1000 tokens, 32 heads on 8: 37 us in
+// one part, 55 in three; 8 of up to 1916, 4 heads on one: 63 us in one, 75 in
+// three; 512 new tokens behind 16384: 155 us in four, 439 in one; 64: 41 us in 32, 423
+// in one.
 int64_t tile_parts(const AttendParams& p) {
     if (!needs_tiles(p)) return 1;
     const int64_t tiles = std::max<int64_t>(1, p.c.n_tokens * p.group / tile_rows_of(p.c.head_dim));
     const int64_t most = wanted_parts(p, p.c.n_seqs > tiles && !apart(p) ? kSplitHalf : kSplitTiles, tiles * p.c.n_kv_heads);
     const int64_t sums = tile_slots(p) * p.c.head_dim * 2 * (int64_t)sizeof(float);     // bytes, of a part
-    auto cost = [&](int64_t parts) {                                                    // ns, at 4.5 TB/s
-        return most_tokens(p) * 26 / parts + (parts > 1 ? 5000 + sums * parts / 4500 : 0);
+    // (ns: a round of a workgroup a CU takes 8 us to begin and end; the sums at
+    // 4.5 TB/s; a number without a tile holds a CU for 1.5 us)
+    const int64_t wgs = tiles * p.c.n_kv_heads, empty = std::max<int64_t>(number_tiles(p).count * p.c.n_kv_heads - wgs, 0);
+    auto cost = [&](int64_t parts) {
+        return (wgs * parts + 255) / 256 * (8000 + most_tokens(p) * 26 / parts) + empty * parts * 6 +
+               (parts > 1 ? 5000 + sums * parts / 4500 : 0);
     };
     int64_t best = 1;
-    // (at most four workgroups a CU, those of numbers without a tile among them)
-    const int64_t limit = std::min(most, 1024 / (number_tiles(p).count * p.c.n_kv_heads));
-    for (int64_t n = 2; n <= limit; ++n)
+    for (int64_t n = 2; n <= most; ++n)
         if (cost(n) < cost(best)) best = n;
     return best;
 }
