@@ -73,12 +73,14 @@ __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 acc) {
                                                        acc, 0, 0, 0);
 }
 
-// What weights are relative to before any score (then the maximum, or a little
-// less): finite, so that no difference of two is NaN; a score below it is -inf,
-// whose weight is 0.
+// What weights are relative to before any score (then the largest score so
+// far, or a little less, before scaling): finite, so that no difference of two is NaN; a
+// score below it is -inf, whose weight is 0.
 constexpr float kNone = -FLT_MAX;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Weights are rounded to the 16-bit type for the product with the values: the
 // matrix units take no more, and the output has no more (each is off by up to
@@ -88,13 +90,16 @@ constexpr float kLn2 = 0.69314718055994530942f;
 // weights are relative to 2^-LIFT times the largest and at most 2^15 (tile_rows
 // lets them grow by 2^8): those of 2^-29 (few_rows) and 2^-21 (tile_rows) of the
 // largest are still normal.  bf16 has the exponents of 32 bits.
-constexpr int kLiftFew = 15, kLiftTiles = 7;
-template <bool F16, int LIFT>
-__device__ __forceinline__ float reference(float top, float score_scale) {
-    return F16 ? fmaf(top, score_scale, -(float)LIFT) : top * score_scale;
-}
+template <bool F16>
+constexpr float kLiftFew = F16 ? 15.0f : 0.0f;
+template <bool F16>
+constexpr float kLiftTiles = F16 ? 7.0f : 0.0f;
 
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+// 2^(scaled difference of two scores): the difference first, which is exact for
+// near scores however large they are.
+__device__ __forceinline__ float weight(float score, float than, float score_scale, float lift = 0.0f) {
+    return exp2_fast(fmaf(score - than, score_scale, lift));
+}
 
 // The tokens that rows at positions first .. last see, as a list of tiles of TILE
 // tokens: `sink` tiles from 0, the others from tile `from`; tokens are below `end`.
@@ -123,8 +128,8 @@ __device__ __forceinline__ bool sees(int32_t window, int32_t sinks, int32_t p, i
 }
 
 // Where the parts of a split call go: per slot (a row of a workgroup) and
-// part, first all sums [slots][parts][D], then (what weights are relative to, in
-// log2, and their sum)
+// part, first all sums [slots][parts][D], then (the score that weights are
+// relative to, their sum)
 // [slots][parts][2].
 struct Parts {
     int32_t count;          // 1 = not split
@@ -175,13 +180,17 @@ __device__ __forceinline__ void load8(const uint16_t* p, float (&x)[8]) {
     }
 }
 
+__device__ __forceinline__ float log_sum(float top, float all, float score_scale) {
+    return all == 0.0f ? -INFINITY : fmaf(top, score_scale, log2f(all)) * kLn2;
+}
+
 // One row by itself over the tokens of tiles v0 .. v1 - 1, as the definition
 // has it: a wavefront's halves take a token each in turn, 8 elements a lane.
 // The way of rows whose step holds values that are not finite and that only
 // some of its rows see, and where speed does not matter.
 struct RowSums {
     float acc[8];           // of elements 8 (lane % 32) ..
-    float m, l;             // the maximum in log2 and the sum of weights
+    float m, l;             // the largest score, not scaled, and the sum of weights
 };
 
 template <bool F16, int TILE>
@@ -209,9 +218,8 @@ __device__ RowSums row_alone(const AttendParams& P, int64_t b, int64_t token, in
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor(dot, o);
             if (at < 0) continue;
-            const float sc = dot * score_scale;
-            const float m2 = fmaxf(r.m, sc);
-            const float keep = exp2_fast(r.m - m2), w = exp2_fast(sc - m2);
+            const float m2 = fmaxf(r.m, dot);
+            const float keep = weight(r.m, m2, score_scale), w = weight(dot, m2, score_scale);
             r.l = fmaf(r.l, keep, w);
             if (in) load8<F16>(c.value + at + at0, x);
 #pragma unroll
@@ -220,7 +228,7 @@ __device__ RowSums row_alone(const AttendParams& P, int64_t b, int64_t token, in
         }
     }
     const float mo = __shfl_xor(r.m, 32), lo = __shfl_xor(r.l, 32);
-    const float m2 = fmaxf(r.m, mo), a = exp2_fast(r.m - m2), z = exp2_fast(mo - m2);
+    const float m2 = fmaxf(r.m, mo), a = weight(r.m, m2, score_scale), z = weight(mo, m2, score_scale);
     r.l = r.l * a + lo * z;
 #pragma unroll
     for (int e = 0; e < 8; ++e) r.acc[e] = r.acc[e] * a + __shfl_xor(r.acc[e], 32) * z;
@@ -235,7 +243,8 @@ __device__ RowSums row_alone(const AttendParams& P, int64_t b, int64_t token, in
 // weight is read all the same and left out by its factor of 0.  With WAVES > 1 the
 // whole workgroup works on one slot.
 template <bool F16, int LANES, int WAVES>
-__device__ __forceinline__ void join_row(const AttendParams& P, const Parts& parts, int64_t slot, int64_t to) {
+__device__ __forceinline__ void join_row(const AttendLaunch& F, const Parts& parts, int64_t slot, int64_t to) {
+    const AttendParams& P = F.a;
     constexpr int kGroups = kWave / LANES;
     __shared__ f32x4 sums_of[WAVES > 1 ? WAVES - 1 : 1][LANES];
     const int wave = WAVES > 1 ? threadIdx.x / kWave : 0;
@@ -251,7 +260,7 @@ __device__ __forceinline__ void join_row(const AttendParams& P, const Parts& par
     f32x4 o = {0, 0, 0, 0};
     for (int k0 = 0; k0 < n; k0 += kWave) {
         const float2 y = k0 + lane < n ? st[k0 + lane] : make_float2(kNone, 0.0f);
-        const float f = y.y == 0.0f ? 0.0f : exp2_fast(y.x - top);
+        const float f = y.y == 0.0f ? 0.0f : weight(y.x, top, F.score_scale);
         all = fmaf(y.y, f, all);
         const int m = min(n - k0, kWave);
 #pragma unroll 8
@@ -285,7 +294,7 @@ __device__ __forceinline__ void join_row(const AttendParams& P, const Parts& par
     if (all == 0.0f) o = f32x4{0, 0, 0, 0};
     if (group == 0 && d < D)
         *(uint2*)(P.out + to * D + d) = make_uint2(pack2<F16>(o[0] * f, o[1] * f), pack2<F16>(o[2] * f, o[3] * f));
-    if (lane == 0 && P.lse) P.lse[to] = all == 0.0f ? -INFINITY : (top + log2f(all)) * kLn2;
+    if (lane == 0 && P.lse) P.lse[to] = log_sum(top, all, F.score_scale);
 }
 
 }  // namespace tl

@@ -181,12 +181,12 @@ __device__ __forceinline__ void few_rows(const AttendLaunch& F, int64_t block, F
                               fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            const float m2 = fmaxf(m, reference<F16, kLiftFew>(top, F.score_scale));
-            const float keep = exp2_fast(m - m2);
+            const float m2 = fmaxf(m, top);
+            const float keep = weight(m, m2, F.score_scale);
             m = m2;
             float p[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) p[e] = exp2_fast(fmaf(sc[e / 4][e % 4], F.score_scale, -m));
+            for (int e = 0; e < 8; ++e) p[e] = weight(sc[e / 4][e % 4], m, F.score_scale, kLiftFew<F16>);
             float sum = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
             l = fmaf(l, keep, sum);     // of this lane's tokens
             const u32x4 pw = {pack2<F16>(p[0], p[1]), pack2<F16>(p[2], p[3]), pack2<F16>(p[4], p[5]),
@@ -204,6 +204,12 @@ __device__ __forceinline__ void few_rows(const AttendLaunch& F, int64_t block, F
         }
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);
+        if constexpr (F16) {
+            constexpr float kBack = 1.0f / 32768.0f;        // 2^-lift
+            l *= kBack;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) acc[j] *= kBack;
+        }
     }
 
     // join the wavefronts: acc[j][i] is element kPer * (4 g + i) + j of row n
@@ -250,7 +256,7 @@ __device__ __forceinline__ void few_rows(const AttendLaunch& F, int64_t block, F
         f32x4 o = {0, 0, 0, 0};
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            const float f = exp2_fast(stats[w][r][0] - top);
+            const float f = weight(stats[w][r][0], top, F.score_scale);
             all = fmaf(stats[w][r][1], f, all);
             const f32x4 y = *(const f32x4*)&sums[w][r][d];
 #pragma unroll
@@ -267,7 +273,7 @@ __device__ __forceinline__ void few_rows(const AttendLaunch& F, int64_t block, F
             if (all == 0.0f) o = f32x4{0, 0, 0, 0};
             if (d < D)
                 *(uint2*)(P.out + to * D + d) = make_uint2(pack2<F16>(o[0] * f, o[1] * f), pack2<F16>(o[2] * f, o[3] * f));
-            if (d == 0 && P.lse) P.lse[to] = all == 0.0f ? -INFINITY : (top + log2f(all)) * kLn2;
+            if (d == 0 && P.lse) P.lse[to] = log_sum(top, all, F.score_scale);
         }
     }
 }

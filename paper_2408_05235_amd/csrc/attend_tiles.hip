@@ -432,9 +432,8 @@ __device__ __forceinline__ void tile_rows(const AttendLaunch& F, int64_t block, 
                 top = fmaxf(top, other_half(top));
                 // The sums are only scaled down when the maximum has grown by
                 // more than 2^8 for some row: weights up to 2^8 lose nothing.
-                const float m2 = fmaxf(m, reference<F16, kLiftTiles>(top, F.score_scale));
-                if (__any(m2 > m + 8.0f)) {
-                    const float keep = exp2_fast(m - m2);
+                if (__any((top - m) * F.score_scale > 8.0f || (m == kNone && top > kNone))) {
+                    const float m2 = fmaxf(m, top), keep = weight(m, m2, F.score_scale);
                     l *= keep;
                     m = m2;
 #pragma unroll
@@ -442,13 +441,23 @@ __device__ __forceinline__ void tile_rows(const AttendLaunch& F, int64_t block, 
 #pragma unroll
                         for (int i = 0; i < 16; ++i) acc[j][i] *= keep;
                 }
+                // (the difference of scores first only where they are so large
+                // that it matters: 32 instructions)
+                float back = m == kNone ? kLiftTiles<F16> : fmaf(-m, F.score_scale, kLiftTiles<F16>);
+                if (__any(fabsf(back) > 65536.0f)) {
+                    back = kLiftTiles<F16>;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sc[h][i] -= m;
+                }
                 float sum[4] = {0, 0, 0, 0};
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int i = 0; i < 16; i += 2) {
-                        const float a = exp2_fast(fmaf(sc[h][i], F.score_scale, -m));
-                        const float z = exp2_fast(fmaf(sc[h][i + 1], F.score_scale, -m));
+                        const float a = exp2_fast(fmaf(sc[h][i], F.score_scale, back));
+                        const float z = exp2_fast(fmaf(sc[h][i + 1], F.score_scale, back));
                         sum[i / 2 % 4] += a + z;
                         w[h][i / 8][i % 8 / 2] = pack2<F16>(a, z);
                     }
@@ -462,6 +471,14 @@ __device__ __forceinline__ void tile_rows(const AttendLaunch& F, int64_t block, 
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         if (!second) phase_end();
         l += __shfl_xor(l, 32);
+        if constexpr (F16) {
+            constexpr float kBack = 1.0f / 128.0f;          // 2^-lift
+            l *= kBack;
+#pragma unroll
+            for (int j = 0; j < kBlocks; ++j)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[j][i] *= kBack;
+        }
     }
 
     const int64_t to = (s.first + token) * P.n_heads + head;
@@ -483,7 +500,7 @@ __device__ __forceinline__ void tile_rows(const AttendLaunch& F, int64_t block, 
             }
             if (lane == 0) {
                 if (split) *(float2*)(F.tiles.stats + part_slot * 2) = make_float2(y.m, y.l);
-                else if (P.lse) P.lse[out] = y.l == 0.0f ? -INFINITY : (y.m + log2f(y.l)) * kLn2;
+                else if (P.lse) P.lse[out] = log_sum(y.m, y.l, F.score_scale);
             }
         }
         return;
@@ -507,7 +524,7 @@ __device__ __forceinline__ void tile_rows(const AttendLaunch& F, int64_t block, 
         }
     if (g == 0) {
         if (split) *(float2*)(F.tiles.stats + slot * 2) = make_float2(m, l);
-        else if (P.lse) P.lse[to] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
+        else if (P.lse) P.lse[to] = log_sum(m, l, F.score_scale);
     }
 }
 

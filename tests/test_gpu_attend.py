@@ -158,6 +158,39 @@ def test_many_small_weights(gpu, dtype, new):
     assert bool(((lse.double() - torch.log(all)[:, :, 0]).abs() <= 2.0 ** -17).all())
 
 
+@pytest.mark.parametrize("dtype,q,k", [("f16", 60000.0, 60000.0), ("f16", 30000.0, 2000.0), ("bf16", 1e14, 1e15),
+                                       ("bf16", 1e4, 1e4), ("f16", -60000.0, 60000.0), ("bf16", -1e14, 1e15)])
+@pytest.mark.parametrize("new", [1, 20])
+@pytest.mark.parametrize("rising", [False, True])
+def test_large_scores(gpu, dtype, q, k, new, rising):
+    """Scores so large that their distances are all that counts: the output is
+    the value of the token with the largest one, exactly, and lse that score (2^-20 of
+    itself: its product, the scale and the logarithm's factor, each rounded to 24 bits)."""
+    L, dim = 3000, 64
+    c = cc.make(19, dtype, 2, 1, dim, 16, [L], [new])
+    t = torch.arange(L + new, device="cuda")
+    steps = (t // 12 if rising else (L + new - 1 - t) // 12).float()       # 12 tokens each have the same score
+    top = steps == steps.max() if q > 0 else steps == 0
+    keys = (k * (0.5 + steps / 1024)).to(cc.DTYPES[dtype])
+    top = keys == (keys.max() if q > 0 else keys.min())
+    values = torch.where(top, 3.0, -5.0).to(cc.DTYPES[dtype])
+    page = c["table"][0].long()[t // 16]
+    c["k"].zero_()
+    c["q"] = torch.zeros(new, 2, dim, dtype=cc.DTYPES[dtype], device="cuda")
+    c["q"][:, :, 3] = q
+    c["k"][page, 0, t % 16, 3] = keys
+    c["v"][page, 0, t % 16] = values[:, None]
+    out, lse = run(c, scale=1.0)
+    q1 = float(c["q"][0, 0, 3])
+    for i in range(new):
+        seen = keys[: L + i + 1].double() * q1
+        best = seen == seen.max()
+        assert bool((values[: L + i + 1][best] == values[: L + i + 1][best][0]).all())
+        assert bool((out[i] == values[: L + i + 1][best][0]).all()), (i, float(out[i, 0, 0]))
+        want = float(seen.max()) + math.log(int(best.sum()))
+        assert bool(((lse[i].double() - want).abs() <= 2.0 ** -20 * abs(want) + 2.0 ** -18).all())
+
+
 def test_scale(gpu):
     c = cc.make(8, "f16", 4, 2, 64, 16, [100, 0], [1, 70])
     cc.check(c, *run(c, scale=0.7), scale=0.7)
