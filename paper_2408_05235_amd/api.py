@@ -595,7 +595,9 @@ class KVCache:
         return self.ref, self.page_table, self.length
 
     def extend(self, add, status=None):
-        """Room for ``add`` [n_slots] new tokens; returns the statuses."""
+        """Room for ``add`` [n_slots] new tokens; returns the statuses.  A slot
+        that got none keeps its length: its new tokens stay out of append and
+        attend, which place them by the length."""
         return tl_pages_extend(*self._state(), add, self.page_tokens, status, self.work)
 
     def append(self, layer, key, value, q_offset=None):
