@@ -50,13 +50,15 @@ __device__ __forceinline__ int64_t tile_seq(const AttendLaunch& F, int64_t tile)
 // it; `settle` waits for the copies (vmcnt) before a barrier hands them over.
 __device__ __forceinline__ void copy_piece(const uint16_t* src, uint32_t lds) {
     const uint32_t to = __builtin_amdgcn_readfirstlane(lds);
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(src) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\t" TL_M0_WAIT "\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(src)
+                 : "memory", "m0");
 }
 
 // The same for 4 bytes a lane.
 __device__ __forceinline__ void copy_words(const int32_t* src, uint32_t lds) {
     const uint32_t to = __builtin_amdgcn_readfirstlane(lds);
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(src) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\t" TL_M0_WAIT "\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(src)
+                 : "memory", "m0");
 }
 
 __device__ __forceinline__ uint32_t lds_address(const void* p) {

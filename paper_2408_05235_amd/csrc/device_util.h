@@ -35,6 +35,12 @@ __device__ __forceinline__ uint32_t ceil_div_u32(uint32_t x, DivU32 q) {
     return div_u32(x + q.d - 1, q);   // caller keeps x + d - 1 < 2^31
 }
 
+// The wait state that a load to LDS needs behind the scalar write of M0 that it
+// reads, which the compiler puts between its own but not into inline assembly.
+// s_nop 0 by its encoding: in a listing of the instructions a copy stays next to
+// the write that feeds it, which is how the listings are checked for other uses of M0.
+#define TL_M0_WAIT ".long 0xbf800000"
+
 __device__ __forceinline__ int lane_id() { return (int)(threadIdx.x & (kWave - 1)); }
 
 // Wavefront scans by DPP (data movement inside the VALU, no LDS round
