@@ -135,7 +135,8 @@ __device__ __forceinline__ int32_t block_count(const RankDev& D, const TreeBlock
 // in flight inside its block loop.
 __device__ __forceinline__ void stage_piece(const uint4* src, uint32_t lds) {
     const uint32_t base = __builtin_amdgcn_readfirstlane(lds);   // wavefront-uniform by construction
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(base), "v"(src) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\t" TL_M0_WAIT "\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(base), "v"(src)
+                 : "memory", "m0");
 }
 
 // Bytes of a staged tree: the whole record, or (HALF) its nodes and leaf

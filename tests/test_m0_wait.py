@@ -18,7 +18,7 @@ OBJDUMP = "/opt/rocm/llvm/bin/llvm-objdump"
 
 @pytest.mark.skipif((shutil.which("hipcc") is None and not os.path.exists("/opt/rocm/bin/hipcc"))
                     or not os.path.exists(OBJDUMP), reason="no hipcc or no llvm-objdump")
-@pytest.mark.parametrize("name", ["attend_tiles.hip"])
+@pytest.mark.parametrize("name", ["attend_tiles.hip", "forest.hip", "column.hip"])
 def test_a_wait_state_between_m0_and_the_copy(tmp_path, name):
     flags = [f for f in build.HIPCC_FLAGS if f not in ("-shared", "-fPIC")]
     obj = str(tmp_path / "out.o")
