@@ -485,10 +485,17 @@ typedef struct tl_kv_view {
     const int32_t* length;         /* [B] */
 } tl_kv_view;
 
+/* A sequence whose tokens got no room has rows all the same, and a length that
+ * does not count them: taken for its last tokens they would be written over
+ * those that it, or a sequence that shares the page, has.  `granted` [n_seqs + 1]
+ * (tl_pages_extend's; nullable) says what each got since the last append; a sequence
+ * with more rows than that has no position for any of them: they are not written
+ * and, where it was refused, see nothing. */
+
 /* New keys and values to their pages: row i of key and value (strides in
  * elements between tokens and heads, multiples of 8) to its sequence's
  * position.  A page that two rows write (a shared page: fork copies those) gets
- * one of them. */
+ * one of them.  Sets granted[n_seqs]. */
 typedef struct tl_kv_append_args {
     uint32_t struct_size;          /* sizeof(tl_kv_append_args) */
     uint32_t reserved;
@@ -499,6 +506,7 @@ typedef struct tl_kv_append_args {
     const void* value;
     int64_t key_token_stride, key_head_stride;
     int64_t value_token_stride, value_head_stride;
+    int32_t* granted;              /* [n_seqs + 1], nullable (absent: a struct_size without it) */
 } tl_kv_append_args;
 
 tl_status tl_kv_append(const tl_kv_append_args* args, void* stream);
@@ -541,6 +549,7 @@ typedef struct tl_attend_args {
     float* lse;                    /* [T][n_heads]; NULL = not wanted */
     void* workspace;               /* nullable */
     uint64_t workspace_bytes;
+    const int32_t* granted;        /* [n_seqs + 1], nullable (absent: a struct_size without it) */
 } tl_attend_args;
 
 tl_status tl_attend(const tl_attend_args* args, void* stream);
@@ -573,6 +582,7 @@ typedef struct tl_pages {
     int32_t* ref;                  /* [n_pages] */
     int32_t* page_table;           /* [n_slots][table_width] */
     int32_t* length;               /* [n_slots] */
+    int32_t* granted;              /* [n_slots + 1], nullable (absent: a struct_size without it) */
 } tl_pages;
 
 /* int32 words that `work` of the calls below has to hold. */
@@ -580,7 +590,10 @@ uint64_t tl_pages_work_words(const tl_pages* pages);
 
 /* Room for add[b] more tokens in every slot b, in slot order: the pages
  * behind its last one, ref 1, and length[b] += add[b].  TL_PAGES_BAD: add < 0
- * or length < 0.  Slots that are not served keep their length. */
+ * or length < 0.  Slots that are not served keep their length.
+ * granted[b]: the tokens that slot b got since the last append, g, or -1 - g when
+ * it was refused after that.  granted[n_slots]: 0 from here until tl_kv_append has
+ * placed them (non-zero at first). */
 tl_status tl_pages_extend(const tl_pages* pages, const int32_t* add, int32_t* status, int32_t* work, void* stream);
 
 /* Fork i makes the empty slot child[i] a copy of parent[i]: it shares the full
@@ -589,7 +602,7 @@ tl_status tl_pages_extend(const tl_pages* pages, const int32_t* add, int32_t* st
  * is nothing to copy).  So a page with room is only ever one sequence's.
  * Lengths are those before the call.  TL_PAGES_BAD: a slot out of range or of
  * negative length, child not empty, or an earlier fork's child; the child stays
- * empty then, as with TL_PAGES_NONE_FREE. */
+ * empty then, as with TL_PAGES_NONE_FREE.  granted[child[i]] becomes 0 with the fork. */
 tl_status tl_pages_fork(const tl_pages* pages, int64_t n_forks, const int32_t* parent, const int32_t* child,
                         int32_t* copy_src, int32_t* copy_dst, int32_t* status, int32_t* work, void* stream);
 

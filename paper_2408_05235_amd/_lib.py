@@ -63,7 +63,7 @@ class KvAppendArgs(ctypes.Structure):
     _fields_ = [
         ("struct_size", u32), ("reserved", u32), ("cache", KvView), ("n_tokens", i64), ("q_offset", P), ("key", P),
         ("value", P), ("key_token_stride", i64), ("key_head_stride", i64), ("value_token_stride", i64),
-        ("value_head_stride", i64),
+        ("value_head_stride", i64), ("granted", P),
     ]
 
 
@@ -72,13 +72,14 @@ class AttendArgs(ctypes.Structure):
         ("struct_size", u32), ("n_heads", i32), ("cache", KvView), ("n_tokens", i64), ("q_offset", P), ("query", P),
         ("query_token_stride", i64), ("query_head_stride", i64), ("scale", f32), ("window", i32), ("sinks", i32),
         ("max_length", i32), ("out", P), ("lse", P), ("workspace", P), ("workspace_bytes", ctypes.c_uint64),
+        ("granted", P),
     ]
 
 
 class Pages(ctypes.Structure):
     _fields_ = [
         ("struct_size", u32), ("page_tokens", i32), ("n_pages", i64), ("n_slots", i64), ("table_width", i32),
-        ("reserved", i32), ("ref", P), ("page_table", P), ("length", P),
+        ("reserved", i32), ("ref", P), ("page_table", P), ("length", P), ("granted", P),
     ]
 
 

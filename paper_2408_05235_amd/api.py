@@ -416,32 +416,41 @@ def _kv_view(key_pages, value_pages, page_table, length):
                        length.data_ptr())
 
 
-def tl_kv_append(key, value, key_pages, value_pages, page_table, length, q_offset=None):
+def _granted(t, n):
+    return None if t is None else _need(t, torch.int32, "granted", (n + 1,)).data_ptr()
+
+
+def tl_kv_append(key, value, key_pages, value_pages, page_table, length, q_offset=None, granted=None):
     """New keys and values [T, n_kv_heads, head_dim] to their pages
     (tl_kv_append).  Pages are [n_pages, n_kv_heads, page_tokens, head_dim]
     with any strides (``x.transpose(1, 2)`` of token-major pages); page_table
     [B, width] and length [B] int32, length with the new tokens; q_offset
-    [B + 1] int64, or None for one token per sequence."""
+    [B + 1] int64, or None for one token per sequence.  ``granted`` [B + 1] int32
+    is what tl_pages_extend gave the sequences: with it the rows of one that
+    got less than it has rows (none, where it was refused) are not written; without,
+    they are its last ``length`` tokens', whatever those are."""
     v = _kv_view(key_pages, value_pages, page_table, length)
     dtype, (_, heads, _, dim), T = key_pages.dtype, key_pages.shape, key.shape[0]
     ks, vs = _rows3(key, dtype, "key", heads, dim), _rows3(value, dtype, "value", heads, dim, T)
     if q_offset is not None:
         _need(q_offset, torch.int64, "q_offset", (page_table.shape[0] + 1,))
     a = _lib.KvAppendArgs(_APPEND_SIZE, 0, v, T, _p(q_offset), key.data_ptr(), value.data_ptr(), ks[0], ks[1], vs[0],
-                          vs[1])
+                          vs[1], None if granted is None else _granted(granted, page_table.shape[0]))
     check(lib().tl_kv_append(ctypes.byref(a), _stream()))
 
 
 def tl_attend(query, key_pages, value_pages, page_table, length, q_offset=None, window=0, sinks=0, scale=None,
-              max_length=0, out=None, want_lse=False, workspace=None):
+              max_length=0, out=None, want_lse=False, workspace=None, granted=None):
     """Attention of the new tokens' queries [T, n_heads, head_dim] over the
     paged cache (tl_attend); the cache as in tl_kv_append, with the new tokens
     already in it.  ``window`` 0 sees every earlier token, else the last
     ``window`` and the first ``sinks``; ``scale`` is head_dim ** -0.5 unless
     given; ``max_length`` is an upper bound of ``length`` where the caller
     knows one.  ``workspace`` is an uint8 tensor (as many bytes as the call can
-    use are allocated when None).  Returns out [T, n_heads, head_dim], and the
-    log-sums [T, n_heads] fp32 too with ``want_lse``.  For serving: no gradients."""
+    use are allocated when None).  Rows of a sequence that ``granted`` ([B + 1]
+    int32, tl_pages_extend's) says was refused see nothing.  Returns out [T, n_heads,
+    head_dim], and the log-sums [T, n_heads] fp32 too with ``want_lse``.  For serving:
+    no gradients."""
     v = _kv_view(key_pages, value_pages, page_table, length)
     dtype, shape, device = key_pages.dtype, query.shape, query.device
     qs = _rows3(query, dtype, "query", None, key_pages.shape[3])
@@ -455,7 +464,8 @@ def tl_attend(query, key_pages, value_pages, page_table, length, q_offset=None, 
     lse = torch.empty((T, heads), dtype=torch.float32, device=device) if want_lse else None
     a = _lib.AttendArgs(_ATTEND_SIZE, heads, v, T, _p(q_offset), query.data_ptr(), qs[0], qs[1],
                         dim ** -0.5 if scale is None else float(scale), int(window), int(sinks), int(max_length),
-                        out.data_ptr(), _p(lse), None, 0)
+                        out.data_ptr(), _p(lse), None, 0,
+                        _granted(granted, page_table.shape[0]))
     L, ref = lib(), ctypes.byref(a)
     if workspace is None:
         n = L.tl_attend_workspace_bytes(ref)
@@ -469,7 +479,7 @@ def tl_attend(query, key_pages, value_pages, page_table, length, q_offset=None, 
     return (out, lse) if want_lse else out
 
 
-def _pages(ref, page_table, length, page_tokens):
+def _pages(ref, page_table, length, page_tokens, granted=None):
     _need(ref, torch.int32, "ref")
     _need(page_table, torch.int32, "page_table")
     if ref.dim() != 1 or page_table.dim() != 2:
@@ -477,7 +487,7 @@ def _pages(ref, page_table, length, page_tokens):
     n_slots, width = page_table.shape
     _need(length, torch.int32, "length", (n_slots,))
     return _lib.Pages(_PAGES_SIZE, int(page_tokens), ref.shape[0], n_slots, width, 0, ref.data_ptr(),
-                      page_table.data_ptr(), length.data_ptr())
+                      page_table.data_ptr(), length.data_ptr(), _granted(granted, n_slots))
 
 
 def _pages_work(g, ref, work):
@@ -490,10 +500,12 @@ def _pages_work(g, ref, work):
     return work
 
 
-def tl_pages_extend(ref, page_table, length, add, page_tokens, status=None, work=None):
+def tl_pages_extend(ref, page_table, length, add, page_tokens, status=None, work=None, granted=None):
     """Room for ``add`` [n_slots] int32 more tokens in every slot, in place
-    (tl_pages_extend).  Returns status [n_slots] int32 (PAGES_* codes)."""
-    g = _pages(ref, page_table, length, page_tokens)
+    (tl_pages_extend).  Returns status [n_slots] int32 (PAGES_* codes).
+    ``granted`` [n_slots + 1] int32 (its last word not 0 at first) keeps what
+    each slot got since the last append, for tl_kv_append and tl_attend."""
+    g = _pages(ref, page_table, length, page_tokens, granted)
     work = _pages_work(g, ref, work)
     _need(add, torch.int32, "add", (g.n_slots,))
     if status is None:
@@ -503,11 +515,11 @@ def tl_pages_extend(ref, page_table, length, add, page_tokens, status=None, work
     return status
 
 
-def tl_pages_fork(ref, page_table, length, parent, child, page_tokens, work=None):
+def tl_pages_fork(ref, page_table, length, parent, child, page_tokens, work=None, granted=None):
     """Empty slots ``child`` become copies of slots ``parent`` (int32 [F]), in
-    place (tl_pages_fork).  Returns (copy_src, copy_dst, status) int32 [F]; the
-    pages still have to be copied (tl_pages_copy)."""
-    g = _pages(ref, page_table, length, page_tokens)
+    place (tl_pages_fork; ``granted`` as in tl_pages_extend).  Returns (copy_src,
+    copy_dst, status) int32 [F]; the pages still have to be copied (tl_pages_copy)."""
+    g = _pages(ref, page_table, length, page_tokens, granted)
     work = _pages_work(g, ref, work)
     F = parent.numel()
     _need(parent, torch.int32, "parent", (F,))
@@ -574,7 +586,9 @@ class KVCache:
     pages of ``page_tokens`` tokens, the page table, the lengths and the pages'
     counts, all on the device.  One iteration of an engine extends the slots
     by their new tokens, then appends and attends in every layer; finished
-    sequences are freed.  Nothing here waits for the device."""
+    sequences are freed.  Where the pool has no room for a slot, nothing of what
+    the others do depends on it, and its cached tokens stay as they are.  Nothing here
+    waits for the device."""
 
     def __init__(self, n_layers, n_pages, n_kv_heads, page_tokens, head_dim, n_slots, max_tokens,
                  dtype=torch.bfloat16, device="cuda"):
@@ -587,6 +601,8 @@ class KVCache:
         self.ref = torch.zeros(n_pages, **i32)
         self.page_table = torch.full((n_slots, width), -1, **i32)
         self.length = torch.zeros(n_slots, **i32)
+        # what extend gave since the last append (before the first one: no limit)
+        self.granted = torch.full((n_slots + 1,), 2 ** 31 - 1, **i32)
         g = _lib.Pages(_PAGES_SIZE, self.page_tokens, n_pages, n_slots, width, 0, _p(self.ref),
                        _p(self.page_table), _p(self.length))
         self.work = torch.empty(lib().tl_pages_work_words(ctypes.byref(g)), **i32)
@@ -596,24 +612,27 @@ class KVCache:
 
     def extend(self, add, status=None):
         """Room for ``add`` [n_slots] new tokens; returns the statuses.  A slot
-        that got none keeps its length: its new tokens stay out of append and
-        attend, which place them by the length."""
-        return tl_pages_extend(*self._state(), add, self.page_tokens, status, self.work)
+        that is refused keeps its length and its tokens: rows that it has in append
+        all the same are not written, and in attend they give zeros."""
+        return tl_pages_extend(*self._state(), add, self.page_tokens, status, self.work, self.granted)
 
     def append(self, layer, key, value, q_offset=None):
-        """The new tokens' keys and values (after extend) into one layer."""
+        """The new tokens' keys and values (after extend) into one layer.  Slots
+        with more rows than tokens that they got since the last append (refused ones,
+        and without ``q_offset`` those that asked for none) are left as they are."""
         k, v = self.pages[layer]
-        tl_kv_append(key, value, k, v, self.page_table, self.length, q_offset)
+        tl_kv_append(key, value, k, v, self.page_table, self.length, q_offset, self.granted)
 
     def attend(self, layer, query, q_offset=None, **kw):
-        """The new tokens' attention over one layer (after append)."""
+        """The new tokens' attention over one layer (after append); zeros for
+        tokens that extend refused."""
         k, v = self.pages[layer]
-        return tl_attend(query, k, v, self.page_table, self.length, q_offset, **kw)
+        return tl_attend(query, k, v, self.page_table, self.length, q_offset, granted=self.granted, **kw)
 
     def fork(self, parent, child):
         """Empty slots ``child`` become copies of ``parent``; returns the
         statuses."""
-        src, dst, status = tl_pages_fork(*self._state(), parent, child, self.page_tokens, self.work)
+        src, dst, status = tl_pages_fork(*self._state(), parent, child, self.page_tokens, self.work, self.granted)
         tl_pages_copy(self.pages, src, dst)
         return status
 

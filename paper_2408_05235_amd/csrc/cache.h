@@ -21,10 +21,13 @@ struct CacheView {
     const int32_t* length;          // [n_seqs]
     int64_t n_tokens;
     const int64_t* q_offset;        // [n_seqs + 1]; NULL = one token each
+    const int32_t* granted;         // [n_seqs + 1], nullable: tokens that the sequences got
+    bool refused_only;              // ... which count only where a sequence was refused
 };
 
 struct AppendParams {
     CacheView c;
+    int32_t* appended;              // c.granted's last word
     const uint16_t* src[2];         // key, value
     int64_t token_stride[2], head_stride[2];
 };
@@ -50,6 +53,7 @@ struct PagesParams {
     int32_t* ref;
     int32_t* table;
     int32_t* length;
+    int32_t* granted;               // nullable
     DivU32 div_page;
 };
 

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <cstddef>
 
 #include "cache.h"
 #include "status.h"
@@ -17,6 +18,11 @@ using tl::ok;
 constexpr int64_t kMaxCount = 0x7fffffffll;
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+
+// Sizes of the structs without `granted`, which is NULL there.
+constexpr size_t kAppendSize = offsetof(tl_kv_append_args, granted);
+constexpr size_t kAttendSize = offsetof(tl_attend_args, granted);
+constexpr size_t kPagesSize = offsetof(tl_pages, granted);
 
 // Checks of a cache view and the packed rows that go with it, and their
 // translation; `who` prefixes messages.
@@ -73,8 +79,8 @@ tl_status view_params(const tl_kv_view* v, int64_t n_tokens, const int64_t* q_of
 }
 
 tl_status attend_params(const tl_attend_args* a, const char* who, tl::AttendParams* p) {
-    if (a->struct_size < sizeof(tl_attend_args))
-        return fail(TL_EINVAL, "%s: struct_size %u < %zu", who, a->struct_size, sizeof(tl_attend_args));
+    if (a->struct_size < kAttendSize)
+        return fail(TL_EINVAL, "%s: struct_size %u < %zu", who, a->struct_size, kAttendSize);
     *p = tl::AttendParams{};
     const tl_status st = view_params(&a->cache, a->n_tokens, a->q_offset, who, &p->c);
     if (st != TL_OK) return st;
@@ -107,6 +113,8 @@ tl_status attend_params(const tl_attend_args* a, const char* who, tl::AttendPara
     p->max_length = a->max_length;
     p->workspace = a->workspace;
     p->workspace_bytes = a->workspace ? a->workspace_bytes : 0;
+    p->c.granted = a->struct_size >= sizeof(tl_attend_args) ? a->granted : nullptr;
+    p->c.refused_only = true;
     if (p->c.n_pages == 0) p->c.table_width = 0;    // nothing is in the cache
     return TL_OK;
 }
@@ -115,8 +123,8 @@ tl_status attend_params(const tl_attend_args* a, const char* who, tl::AttendPara
 // slots does not).
 tl_status pages_params(const tl_pages* g, const char* who, tl::PagesParams* p) {
     if (!g) return fail(TL_EINVAL, "%s: pages is NULL", who);
-    if (g->struct_size < sizeof(tl_pages))
-        return fail(TL_EINVAL, "%s: struct_size %u < %zu", who, g->struct_size, sizeof(tl_pages));
+    if (g->struct_size < kPagesSize)
+        return fail(TL_EINVAL, "%s: struct_size %u < %zu", who, g->struct_size, kPagesSize);
     if (g->page_tokens < 1 || g->page_tokens > TL_MAX_BLOCK_TOKENS)
         return fail(TL_EINVAL, "%s: page_tokens %d outside [1, %d]", who, g->page_tokens, TL_MAX_BLOCK_TOKENS);
     if (g->n_pages < 0 || g->n_pages > kMaxCount)
@@ -135,6 +143,7 @@ tl_status pages_params(const tl_pages* g, const char* who, tl::PagesParams* p) {
     p->ref = g->ref;
     p->table = g->page_table;
     p->length = g->length;
+    p->granted = g->struct_size >= sizeof(tl_pages) ? g->granted : nullptr;
     p->div_page = tl::make_divu32((uint32_t)g->page_tokens);
     return TL_OK;
 }
@@ -146,8 +155,8 @@ extern "C" {
 tl_status tl_kv_append(const tl_kv_append_args* a, void* stream) {
     const char* const who = "tl_kv_append";
     if (!a) return fail(TL_EINVAL, "%s: args is NULL", who);
-    if (a->struct_size < sizeof(tl_kv_append_args))
-        return fail(TL_EINVAL, "%s: struct_size %u < %zu", who, a->struct_size, sizeof(tl_kv_append_args));
+    if (a->struct_size < kAppendSize)
+        return fail(TL_EINVAL, "%s: struct_size %u < %zu", who, a->struct_size, kAppendSize);
     tl::AppendParams p{};
     const tl_status st = view_params(&a->cache, a->n_tokens, a->q_offset, who, &p.c);
     if (st != TL_OK) return st;
@@ -164,6 +173,10 @@ tl_status tl_kv_append(const tl_kv_append_args* a, void* stream) {
     p.token_stride[1] = a->value_token_stride;
     p.head_stride[0] = a->key_head_stride;
     p.head_stride[1] = a->value_head_stride;
+    if (a->struct_size >= sizeof(tl_kv_append_args) && a->granted) {
+        p.c.granted = a->granted;
+        p.appended = a->granted + p.c.n_seqs;
+    }
     if (a->n_tokens == 0 || p.c.n_seqs == 0 || p.c.n_pages == 0 || p.c.table_width == 0) return ok();
     return from_hip(tl::launch_append(p, (hipStream_t)stream), "tl_kv_append: launch");
 }

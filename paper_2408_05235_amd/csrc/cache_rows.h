@@ -6,8 +6,11 @@
 
 namespace tl {
 
+// The tokens of an entry of `granted`: g, or refused (-1 - g) when it had got g.
+__device__ __forceinline__ int32_t tokens_granted(int32_t granted) { return granted < 0 ? ~granted : granted; }
+
 // The rows of sequence b: first and count (0 for malformed offsets), and the
-// number of its cached tokens that exist.
+// number of its cached tokens that exist (0 where its rows have no position).
 struct SeqRows {
     int64_t first;
     int32_t n, length;
@@ -34,6 +37,10 @@ __device__ __forceinline__ SeqRows seq_rows(const CacheView& c, int64_t b) {
         s.n = 1;
     }
     s.length = given_length(c, b);
+    if (c.granted) {
+        const int32_t got = c.granted[b];
+        if ((got < 0 || !c.refused_only) && s.n > tokens_granted(got)) s.length = 0;
+    }
     return s;
 }
 

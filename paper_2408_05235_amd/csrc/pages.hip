@@ -29,6 +29,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendParams P, 
     const CacheView& c = P.c;
     __shared__ int64_t dst[kAppendTokens];
     const int64_t first = (int64_t)blockIdx.x * tokens;
+    if (P.appended && first == 0 && threadIdx.x == 0) *P.appended = 1;
     if ((int)threadIdx.x < tokens) {
         const int64_t i = first + threadIdx.x;
         int64_t at = -1, b;
@@ -193,6 +194,8 @@ __global__ __launch_bounds__(kPoolThreads) void extend_kernel(PagesParams P, con
     counts.load(P, 0);
     int64_t total = 0;
     Wish mine = {};                     // of slot threadIdx.x
+    // tokens granted before stand beside these until an append has placed them
+    const bool keep = P.granted && P.granted[P.n_slots] == 0;
     for (int64_t b0 = 0; b0 < P.n_slots; b0 += kPoolThreads) {
         const int64_t b = b0 + threadIdx.x;
         Wish w = {};
@@ -224,8 +227,14 @@ __global__ __launch_bounds__(kPoolThreads) void extend_kernel(PagesParams P, con
         const Wish w = b < kPoolThreads ? mine : wish(P, P.length[b], add[b]);
         const bool fits = w.need == 0 || starts[b] + (int64_t)w.need <= found;
         status[b] = w.status != TL_PAGES_OK ? w.status : fits ? TL_PAGES_OK : TL_PAGES_NONE_FREE;
+        if (P.granted) {
+            const int32_t entry = keep ? P.granted[b] : 0, had = tokens_granted(entry);
+            const bool served = w.status == TL_PAGES_OK && fits;
+            P.granted[b] = !served ? ~had : add[b] > 0 ? saturate((int64_t)had + add[b]) : entry;
+        }
         if (w.status == TL_PAGES_OK && fits) P.length[b] = w.new_len;
     }
+    if (P.granted && threadIdx.x == 0) P.granted[P.n_slots] = 0;    // (read before the barriers above)
 }
 
 // One workgroup decides the forks: validity (of several with one child the
@@ -321,6 +330,7 @@ __global__ __launch_bounds__(256) void fork_rows_kernel(PagesParams P, const int
     if (threadIdx.x == 0) {
         if (partly(P, len)) to[full] = copy_dst[f];
         P.length[child[f]] = len;
+        if (P.granted) P.granted[child[f]] = 0;
     }
 }
 
