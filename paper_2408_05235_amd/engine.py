@@ -8,7 +8,8 @@ are in the batch at every future iteration; the performance model (Sec. 4.3.1) i
 trained on what the engine does at such points.  ``Engine`` serves one scenario's
 in-flight requests through attention layers over a ``api.KVCache``: their
 prompts first, then one token per request and iteration, finished requests
-leaving.  The pages in use are the projection's blocks, iteration by iteration.
+leaving.  The pages in use are the projection's blocks, iteration by iteration; a
+request that the pool has no room for stops where it is (``Engine.stopped``).
 The layers are random; the times are those of the attention part alone.
 """
 from __future__ import annotations
@@ -18,7 +19,7 @@ import argparse
 import numpy as np
 import torch
 
-from . import api, configs, synth
+from . import _lib, api, configs, synth
 
 
 class Engine:
@@ -43,7 +44,14 @@ class Engine:
         self.proj = [weight(width, width) for _ in range(n_layers)]
         self.inputs = lambda n: torch.randn(n, width, generator=g, device=device).to(dtype)
         self.left = torch.from_numpy(self.remaining).to(device, torch.int32)
+        self.stopped = torch.zeros(len(self.tokens), dtype=torch.bool, device=device)
         self.iteration = 0
+
+    def _extend(self, add):
+        """Room for ``add`` tokens.  A request that is refused keeps the pages and
+        tokens that it has until its time is over, and asks for no more: the tokens
+        behind a missing one would not be its own."""
+        self.stopped |= self.cache.extend(add) != _lib.PAGES_OK
 
     def forward(self, x, q_offset=None):
         """The new tokens' hidden states [T, n_heads * head_dim] through the
@@ -58,21 +66,22 @@ class Engine:
         return x
 
     def prefill(self):
-        """Iteration 0: every request's prompt and what it has generated."""
+        """Iteration 0: every request's prompt and what it has generated.  Rows
+        of a request that has stopped are no token's."""
         dev = self.left.device
-        add = torch.from_numpy(self.tokens).to(dev, torch.int32)
-        self.cache.extend(add)
+        self._extend(torch.from_numpy(self.tokens).to(dev, torch.int32))
         off = torch.from_numpy(np.concatenate([[0], np.cumsum(self.tokens)])).to(dev)
         return self.forward(self.inputs(int(self.tokens.sum())), off)
 
     def step(self):
         """The next iteration: finished requests leave, the others get a
-        token.  Returns the hidden states, one row per slot."""
+        token.  Returns the hidden states, one row per slot (of a request that
+        has left or stopped, no token's)."""
         self.iteration += 1
         gone = np.flatnonzero(self.remaining == self.iteration)
         if len(gone):
             self.cache.free(torch.from_numpy(gone).to(self.left.device, torch.int32))
-        self.cache.extend((self.left > self.iteration).to(torch.int32))
+        self._extend(((self.left > self.iteration) & ~self.stopped).to(torch.int32))
         return self.forward(self.inputs(len(self.tokens)))
 
 
@@ -107,6 +116,9 @@ def main(argv=None):
             e.step()
         end.record()
         used = int(e.cache.pages_used())
+        if bool(e.stopped.any()):
+            raise SystemExit(f"iteration {j}: no room for {int(e.stopped.sum())} of the requests in "
+                             f"{int(inp['kv_capacity'][0])} pages ({kv[j]} blocks projected)")
         if used != kv[j]:
             raise SystemExit(f"iteration {j}: {used} pages in use, {kv[j]} blocks projected")
         if j and (j & (j - 1) == 0 or j == H - 1):
