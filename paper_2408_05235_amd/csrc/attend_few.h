@@ -160,6 +160,13 @@ __device__ __forceinline__ void few_rows(const AttendLaunch& F, int64_t block, F
                     there & (uint32_t)__ballot(first <= last && sees(P.window, P.sinks, first, t));
                 const uint32_t all =
                     (uint32_t)__ballot(sees(P.window, P.sinks, base, t) && sees(P.window, P.sinks, last, t));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int32_t u = 16 * (e / 4) + 4 * g + e % 4;
+                    if (!(any >> u & 1))
+#pragma unroll
+                        for (int y = 0; y < kPer / 2; ++y) w[e][y] = 0;
+                }
                 if (any & ~all) {
                     // values that some rows see and others do not: one that is
                     // not finite would reach the others as 0 x value
@@ -167,13 +174,6 @@ __device__ __forceinline__ void few_rows(const AttendLaunch& F, int64_t block, F
                     for (int e = 0; e < 8; ++e)
 #pragma unroll
                         for (int y = 0; y < kPer / 2; ++y) special |= not_finite2<F16>(w[e][y]);
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int32_t u = 16 * (e / 4) + 4 * g + e % 4;
-                    if (!(any >> u & 1))
-#pragma unroll
-                        for (int y = 0; y < kPer / 2; ++y) w[e][y] = 0;
                 }
             }
             // the softmax's step: lanes n, n + 16, n + 32 and n + 48 hold row n
