@@ -522,7 +522,8 @@ tl_status tl_kv_append(const tl_kv_append_args* args, void* stream);
  * -inf.  What lies in pages beyond the visible tokens, infinities and NaN
  * included, is not used.  Rows that belong to no sequence are left alone.
  *
- * Scores, the softmax's maximum and sum and the output's sums are fp32.  The
+ * Scores, the softmax's maximum and sum and the output's sums are fp32 (sum w v
+ * before its division by sum w, with a largest weight of at most 1).  The
  * weights are rounded to the cache's type for the product with the values (in f16
  * scaled up, so that small ones do not vanish), the output once at the end.
  * workspace: device memory of the caller, 16-byte aligned, for the parts of

@@ -54,7 +54,8 @@ __global__ __launch_bounds__(kFewThreads) void join_kernel(AttendLaunch F, int64
         const int64_t rows = (int64_t)s.n * P.group;
         if ((c.q_offset && rows > kFewRows) || row >= rows) return;
         const int64_t token = row / P.group;
-        join_row<F16, LANES, WAVES>(F, F.few, slot, (s.first + token) * P.n_heads + kvh * P.group + (row - token * P.group));
+        join_row<F16, LANES, WAVES>(F, F.few, slot,
+                                    (s.first + token) * P.n_heads + kvh * P.group + (row - token * P.group), 1.0f);
         return;
     }
     const int64_t to = slot - few_slots, i = to / P.n_heads;
@@ -62,7 +63,7 @@ __global__ __launch_bounds__(kFewThreads) void join_kernel(AttendLaunch F, int64
     if (i >= c.n_tokens || !find_seq(c, i, &b)) return;
     const SeqRows s = seq_rows(c, b);
     if (i < s.first || i - s.first >= s.n || (int64_t)s.n * P.group <= kFewRows) return;
-    join_row<F16, LANES, WAVES>(F, F.tiles, to, to);
+    join_row<F16, LANES, WAVES>(F, F.tiles, to, to, kUnliftTiles<F16>);
 }
 
 template <bool F16, int DP, int WAVES>

@@ -88,12 +88,23 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // rounding).  f16 has no normal numbers below 2^-14: with a largest weight of 1
 // those of less than 2^-25 would vanish, of which a long sequence can have many.  So
 // weights are relative to 2^-LIFT times the largest and at most 2^15 (tile_rows
-// lets them grow by 2^8): those of 2^-29 (few_rows) and 2^-21 (tile_rows) of the
-// largest are still normal.  bf16 has the exponents of 32 bits.
+// lets them grow by 2^kGrowTiles before it scales its sums down): those of 2^-29
+// (few_rows) and 2^-21 (tile_rows) of the largest are still normal.  bf16 has the
+// exponents of 32 bits, and values up to their end: weights are at most 1, so that
+// sums hold as much as sum w |v| does.  (-4 is a constant of the instruction: 32768
+// tokens through a window of 4096 take 560 us so, and 564 with 2^8 and -8.)
+// tile_rows' sums keep the lift, which cancels in the output (kUnliftTiles for
+// what does not).
 template <bool F16>
 constexpr float kLiftFew = F16 ? 15.0f : 0.0f;
 template <bool F16>
-constexpr float kLiftTiles = F16 ? 7.0f : 0.0f;
+constexpr float kGrowTiles = F16 ? 8.0f : 4.0f;
+template <bool F16>
+constexpr float kLiftTiles = F16 ? 7.0f : -kGrowTiles<F16>;
+template <bool F16>
+constexpr float kLiftedTiles = F16 ? 128.0f : 1.0f / 16.0f;         // 2^kLiftTiles
+template <bool F16>
+constexpr float kUnliftTiles = 1.0f / kLiftedTiles<F16>;
 
 // 2^(scaled difference of two scores): the difference first, which is exact for
 // near scores however large they are.
@@ -241,9 +252,11 @@ __device__ RowSums row_alone(const AttendParams& P, int64_t b, int64_t token, in
 // statistics, a part a lane; then LANES lanes with 4 elements each take every
 // (WAVES x 64 / LANES)th part.  Nothing waits for the part before: a part without
 // weight is read all the same and left out by its factor of 0.  With WAVES > 1 the
-// whole workgroup works on one slot.
+// whole workgroup works on one slot.  `unlift`: what brings the parts' sums of
+// weights to a largest weight of 1.
 template <bool F16, int LANES, int WAVES>
-__device__ __forceinline__ void join_row(const AttendLaunch& F, const Parts& parts, int64_t slot, int64_t to) {
+__device__ __forceinline__ void join_row(const AttendLaunch& F, const Parts& parts, int64_t slot, int64_t to,
+                                         float unlift) {
     const AttendParams& P = F.a;
     constexpr int kGroups = kWave / LANES;
     __shared__ f32x4 sums_of[WAVES > 1 ? WAVES - 1 : 1][LANES];
@@ -294,7 +307,7 @@ __device__ __forceinline__ void join_row(const AttendLaunch& F, const Parts& par
     if (all == 0.0f) o = f32x4{0, 0, 0, 0};
     if (group == 0 && d < D)
         *(uint2*)(P.out + to * D + d) = make_uint2(pack2<F16>(o[0] * f, o[1] * f), pack2<F16>(o[2] * f, o[3] * f));
-    if (lane == 0 && P.lse) P.lse[to] = log_sum(top, all, F.score_scale);
+    if (lane == 0 && P.lse) P.lse[to] = log_sum(top, all * unlift, F.score_scale);
 }
 
 }  // namespace tl

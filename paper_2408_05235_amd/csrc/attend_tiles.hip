@@ -433,8 +433,9 @@ __device__ __forceinline__ void tile_rows(const AttendLaunch& F, int64_t block, 
                 float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
                 top = fmaxf(top, other_half(top));
                 // The sums are only scaled down when the maximum has grown by
-                // more than 2^8 for some row: weights up to 2^8 lose nothing.
-                if (__any((top - m) * F.score_scale > 8.0f || (m == kNone && top > kNone))) {
+                // more than 2^kGrowTiles for some row: weights that much larger lose
+                // nothing.
+                if (__any((top - m) * F.score_scale > kGrowTiles<F16> || (m == kNone && top > kNone))) {
                     const float m2 = fmaxf(m, top), keep = weight(m, m2, F.score_scale);
                     l *= keep;
                     m = m2;
@@ -473,14 +474,6 @@ __device__ __forceinline__ void tile_rows(const AttendLaunch& F, int64_t block, 
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         if (!second) phase_end();
         l += __shfl_xor(l, 32);
-        if constexpr (F16) {
-            constexpr float kBack = 1.0f / 128.0f;          // 2^-lift
-            l *= kBack;
-#pragma unroll
-            for (int j = 0; j < kBlocks; ++j)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) acc[j][i] *= kBack;
-        }
     }
 
     const int64_t to = (s.first + token) * P.n_heads + head;
@@ -496,12 +489,12 @@ __device__ __forceinline__ void tile_rows(const AttendLaunch& F, int64_t block, 
             if (lane < 32 && d < D) {
                 const float f = y.l == 0.0f ? 0.0f : 1.0f / y.l;
                 for (int e = 0; e < 8; ++e) {
-                    if (split) F.tiles.sums[part_slot * D + d + e] = y.acc[e];
+                    if (split) F.tiles.sums[part_slot * D + d + e] = y.acc[e] * kLiftedTiles<F16>;
                     else P.out[out * D + d + e] = from_float<F16>(y.l == 0.0f ? 0.0f : y.acc[e] * f);
                 }
             }
             if (lane == 0) {
-                if (split) *(float2*)(F.tiles.stats + part_slot * 2) = make_float2(y.m, y.l);
+                if (split) *(float2*)(F.tiles.stats + part_slot * 2) = make_float2(y.m, y.l * kLiftedTiles<F16>);
                 else if (P.lse) P.lse[out] = log_sum(y.m, y.l, F.score_scale);
             }
         }
@@ -526,7 +519,7 @@ __device__ __forceinline__ void tile_rows(const AttendLaunch& F, int64_t block, 
         }
     if (g == 0) {
         if (split) *(float2*)(F.tiles.stats + slot * 2) = make_float2(m, l);
-        else if (P.lse) P.lse[to] = log_sum(m, l, F.score_scale);
+        else if (P.lse) P.lse[to] = log_sum(m, l * kUnliftTiles<F16>, F.score_scale);
     }
 }
 
