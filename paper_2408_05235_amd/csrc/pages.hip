@@ -25,10 +25,10 @@ constexpr int kAppendTokens = 16;       // most tokens of a workgroup
 // One workgroup moves `tokens` consecutive rows, 16 bytes per lane.  Bound by
 // memory: 65415 tokens of 8 heads of 128 (536 MB) take 111 us, 4.8 TB/s; 64
 // tokens 3 us, a launch and four round trips.
-__global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendParams P, int tokens) {
+__global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendParams P, int tokens, int64_t block) {
     const CacheView& c = P.c;
     __shared__ int64_t dst[kAppendTokens];
-    const int64_t first = (int64_t)blockIdx.x * tokens;
+    const int64_t first = (blockIdx.x + block) * tokens;
     if (P.appended && first == 0 && threadIdx.x == 0) *P.appended = 1;
     if ((int)threadIdx.x < tokens) {
         const int64_t i = first + threadIdx.x;
@@ -533,9 +533,9 @@ hipError_t launch_append(const AppendParams& p, hipStream_t stream) {
     // 8.0 us so, 8.5 with 16); many: 16, which saves workgroups (65415 112 us, 152)
     const int tokens = p.c.n_tokens < 4096 ? 1 : kAppendTokens;
     const int64_t blocks = (p.c.n_tokens + tokens - 1) / tokens;
-    if (!grid_fits(blocks, kAppendThreads)) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL(append_kernel, dim3((unsigned)blocks), dim3(kAppendThreads), 0, stream, p, tokens);
-    return hipGetLastError();
+    return launch_all(blocks, kAppendThreads, [&](dim3 grid, int64_t first) {
+        hipLaunchKernelGGL(append_kernel, grid, dim3(kAppendThreads), 0, stream, p, tokens, first);
+    });
 }
 
 uint64_t pages_work_words(const PagesParams& p) {
@@ -555,13 +555,13 @@ hipError_t launch_pages_fork(const PagesParams& p, int64_t n_forks, const int32_
                        copy_dst, status, work);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    return launch_parts(n_forks, 256, [&](dim3 grid, int64_t first) {
+    return launch_all(n_forks, 256, [&](dim3 grid, int64_t first) {
         hipLaunchKernelGGL(fork_rows_kernel, grid, dim3(256), 0, stream, p, parent, child, copy_dst, work, first);
     });
 }
 
 hipError_t launch_pages_free(const PagesParams& p, int64_t n_free, const int32_t* slots, hipStream_t stream) {
-    return launch_parts(n_free, 256, [&](dim3 grid, int64_t first) {
+    return launch_all(n_free, 256, [&](dim3 grid, int64_t first) {
         hipLaunchKernelGGL(free_kernel, grid, dim3(256), 0, stream, p, slots, first);
     });
 }

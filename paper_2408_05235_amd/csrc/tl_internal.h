@@ -241,16 +241,22 @@ hipError_t launch_lattice_column(const ForestDev& f, const LatticeDev& L, const 
 constexpr int kMaxParts = 4;
 // Wavefronts of a launch.
 constexpr int64_t kMaxLaunchWaves = 0xffffffffll / 64;
+// launch_all does the same without that limit, for calls whose own limits on
+// rows keep the parts few (2^31 - 1 workgroups of 256 threads: 128).
 template <class Launch>
-hipError_t launch_parts(int64_t blocks, int threads, Launch&& launch) {
+hipError_t launch_all(int64_t blocks, int threads, Launch&& launch) {
     const int64_t most = 0xffffffffll / threads;
-    if (blocks > kMaxParts * most) return hipErrorInvalidConfiguration;
     for (int64_t first = 0; first < blocks; first += most) {
         launch(dim3((unsigned)(blocks - first < most ? blocks - first : most)), first);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
+}
+template <class Launch>
+hipError_t launch_parts(int64_t blocks, int threads, Launch&& launch) {
+    if (blocks > kMaxParts * (0xffffffffll / threads)) return hipErrorInvalidConfiguration;
+    return launch_all(blocks, threads, launch);
 }
 inline bool grid_fits(int64_t blocks, int threads) { return blocks >= 0 && blocks <= 0xffffffffll / threads; }
 
