@@ -30,9 +30,10 @@ constexpr int kFewWaves = 4, kFewThreads = kFewWaves * kWave;
 // 97 and 108 us for 4 sequences of 20011 to 36864 tokens.  (Two of a workgroup of
 // eight: wide_few.)
 template <bool F16, int DP, bool EXACT, int WAVES>
-__global__ __launch_bounds__(WAVES * kWave, DP > 128 ? 1 : WAVES > 4 ? 2 : 3) void few_rows_kernel(AttendLaunch F) {
+__global__ __launch_bounds__(WAVES * kWave, DP > 128 ? 1 : WAVES > 4 ? 2 : 3) void few_rows_kernel(AttendLaunch F,
+                                                                                                  int64_t first) {
     __shared__ FewLds<WAVES, DP> lds;
-    few_rows<F16, DP, EXACT, WAVES, true>(F, blockIdx.x, lds);
+    few_rows<F16, DP, EXACT, WAVES, true>(F, blockIdx.x + first, lds);
 }
 
 // Four wavefronts per slot where there are many parts, else one: first the
@@ -42,10 +43,11 @@ __global__ __launch_bounds__(WAVES * kWave, DP > 128 ? 1 : WAVES > 4 ? 2 : 3) vo
 // each one is better (384 rows of 2: 76.9 and 78.3 us; 1024 of 9, with tile_rows: 19.2 and
 // 20.6).
 template <bool F16, int LANES, int WAVES>
-__global__ __launch_bounds__(kFewThreads) void join_kernel(AttendLaunch F, int64_t few_slots) {
+__global__ __launch_bounds__(kFewThreads) void join_kernel(AttendLaunch F, int64_t few_slots, int64_t first) {
     const AttendParams& P = F.a;
     const CacheView& c = P.c;
-    const int64_t slot = WAVES > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * kFewWaves + threadIdx.x / kWave;
+    const int64_t block = blockIdx.x + first;
+    const int64_t slot = WAVES > 1 ? block : block * kFewWaves + threadIdx.x / kWave;
     if (slot < few_slots) {
         const int64_t x = slot / F.slot_rows, row = slot % F.slot_rows;
         const int32_t kvh = (int32_t)(x % c.n_kv_heads);
@@ -68,11 +70,12 @@ __global__ __launch_bounds__(kFewThreads) void join_kernel(AttendLaunch F, int64
 
 template <bool F16, int DP, int WAVES>
 hipError_t launch_waves(const AttendLaunch& f, int64_t blocks, hipStream_t stream) {
-    if (!grid_fits(blocks * f.few.count, WAVES * kWave)) return hipErrorInvalidConfiguration;
-    const dim3 grid((unsigned)(blocks * f.few.count)), block(WAVES * kWave);
-    if (f.a.c.head_dim == DP) hipLaunchKernelGGL((few_rows_kernel<F16, DP, true, WAVES>), grid, block, 0, stream, f);
-    else hipLaunchKernelGGL((few_rows_kernel<F16, DP, false, WAVES>), grid, block, 0, stream, f);
-    return hipGetLastError();
+    return launch_all(blocks * f.few.count, WAVES * kWave, [&](dim3 grid, int64_t first) {
+        const dim3 block(WAVES * kWave);
+        if (f.a.c.head_dim == DP)
+            hipLaunchKernelGGL((few_rows_kernel<F16, DP, true, WAVES>), grid, block, 0, stream, f, first);
+        else hipLaunchKernelGGL((few_rows_kernel<F16, DP, false, WAVES>), grid, block, 0, stream, f, first);
+    });
 }
 
 template <bool F16, int DP>
@@ -85,16 +88,14 @@ hipError_t launch_few(const AttendLaunch& f, int64_t blocks, hipStream_t stream)
 template <bool F16, int DP>
 hipError_t launch_join(const AttendLaunch& f, int64_t few_slots, int64_t tile_slots, hipStream_t stream) {
     const int64_t slots = few_slots + tile_slots;
-    if (std::max(f.few.count, f.tiles.count) > 16) {
-        if (!grid_fits(slots, kFewThreads)) return hipErrorInvalidConfiguration;
-        hipLaunchKernelGGL((join_kernel<F16, DP / 4, kFewWaves>), dim3((unsigned)slots), dim3(kFewThreads), 0, stream, f,
-                           few_slots);
-        return hipGetLastError();
-    }
-    const int64_t blocks = (slots + kFewWaves - 1) / kFewWaves;
-    if (!grid_fits(blocks, kFewThreads)) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((join_kernel<F16, DP / 4, 1>), dim3((unsigned)blocks), dim3(kFewThreads), 0, stream, f, few_slots);
-    return hipGetLastError();
+    if (std::max(f.few.count, f.tiles.count) > 16)
+        return launch_all(slots, kFewThreads, [&](dim3 grid, int64_t first) {
+            hipLaunchKernelGGL((join_kernel<F16, DP / 4, kFewWaves>), grid, dim3(kFewThreads), 0, stream, f, few_slots,
+                               first);
+        });
+    return launch_all((slots + kFewWaves - 1) / kFewWaves, kFewThreads, [&](dim3 grid, int64_t first) {
+        hipLaunchKernelGGL((join_kernel<F16, DP / 4, 1>), grid, dim3(kFewThreads), 0, stream, f, few_slots, first);
+    });
 }
 
 // Row tiles of a sequence and head for few_rows, its workgroups per part, and
@@ -275,6 +276,8 @@ uint64_t attend_workspace_bytes(const AttendParams& p) {
 }
 
 hipError_t launch_attend(const AttendParams& p, hipStream_t stream) {
+    // (sequences without rows count here, which no check before has bounded)
+    if (needs_few(p) && few_blocks(p) > INT32_MAX) return hipErrorInvalidConfiguration;
     AttendLaunch f{};
     f.a = p;
     f.score_scale = p.scale * kLog2e;

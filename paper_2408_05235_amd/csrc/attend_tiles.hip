@@ -527,24 +527,25 @@ __device__ __forceinline__ void tile_rows(const AttendLaunch& F, int64_t block, 
 // and reading on the others.  Two chunks of 512 tokens and 62 single tokens over
 // 9001 to 16384 cached ones: 0.71 ms, 1.00 in two launches.
 template <bool F16, int DP, bool EXACT>
-__global__ __launch_bounds__(tile_waves(DP) * kWave, DP > 128 ? 1 : 2) void mixed_kernel(AttendLaunch F) {
+__global__ __launch_bounds__(tile_waves(DP) * kWave, DP > 128 ? 1 : 2) void mixed_kernel(AttendLaunch F, int64_t first) {
     __shared__ union {
         TileLds<DP> tile;
         FewLds<tile_waves(DP), DP> few;
     } lds;
     const int64_t tiles = F.tile_count * F.a.c.n_kv_heads * F.tiles.count;
-    if (blockIdx.x < tiles) tile_rows<F16, DP, EXACT>(F, blockIdx.x, lds.tile);
-    else few_rows<F16, DP, EXACT, tile_waves(DP), false>(F, blockIdx.x - tiles, lds.few);
+    const int64_t block = blockIdx.x + first;
+    if (block < tiles) tile_rows<F16, DP, EXACT>(F, block, lds.tile);
+    else few_rows<F16, DP, EXACT, tile_waves(DP), false>(F, block - tiles, lds.few);
 }
 
 template <bool F16, int DP>
 hipError_t launch_dim(const AttendLaunch& f, int64_t few_blocks, hipStream_t stream) {
     const int64_t blocks = f.tile_count * f.a.c.n_kv_heads * f.tiles.count + few_blocks * f.few.count;
-    if (!grid_fits(blocks, tile_waves(DP) * kWave)) return hipErrorInvalidConfiguration;
-    const dim3 grid((unsigned)blocks), block(tile_waves(DP) * kWave);
-    if (f.a.c.head_dim == DP) hipLaunchKernelGGL((mixed_kernel<F16, DP, true>), grid, block, 0, stream, f);
-    else hipLaunchKernelGGL((mixed_kernel<F16, DP, false>), grid, block, 0, stream, f);
-    return hipGetLastError();
+    return launch_all(blocks, tile_waves(DP) * kWave, [&](dim3 grid, int64_t first) {
+        const dim3 block(tile_waves(DP) * kWave);
+        if (f.a.c.head_dim == DP) hipLaunchKernelGGL((mixed_kernel<F16, DP, true>), grid, block, 0, stream, f, first);
+        else hipLaunchKernelGGL((mixed_kernel<F16, DP, false>), grid, block, 0, stream, f, first);
+    });
 }
 
 template <bool F16>
