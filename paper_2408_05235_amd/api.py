@@ -416,6 +416,12 @@ def _kv_view(key_pages, value_pages, page_table, length):
                        length.data_ptr())
 
 
+def _no_gradients(who):
+    """Where gradients would be asked for: the paged cache is for serving."""
+    if torch.is_grad_enabled():
+        raise ValueError(f"{who} has no gradients: call it under torch.no_grad(), or with detached tensors")
+
+
 def _granted(t, n):
     return None if t is None else _need(t, torch.int32, "granted", (n + 1,)).data_ptr()
 
@@ -428,7 +434,9 @@ def tl_kv_append(key, value, key_pages, value_pages, page_table, length, q_offse
     [B + 1] int64, or None for one token per sequence.  ``granted`` [B + 1] int32
     is what tl_pages_extend gave the sequences: with it the rows of one that
     got less than it has rows (none, where it was refused) are not written; without,
-    they are its last ``length`` tokens', whatever those are."""
+    they are taken for the last of its ``length`` tokens.  No gradients."""
+    if key.requires_grad or value.requires_grad or key_pages.requires_grad or value_pages.requires_grad:
+        _no_gradients("tl_kv_append")
     v = _kv_view(key_pages, value_pages, page_table, length)
     dtype, (_, heads, _, dim), T = key_pages.dtype, key_pages.shape, key.shape[0]
     ks, vs = _rows3(key, dtype, "key", heads, dim), _rows3(value, dtype, "value", heads, dim, T)
@@ -450,7 +458,10 @@ def tl_attend(query, key_pages, value_pages, page_table, length, q_offset=None, 
     use are allocated when None).  Rows of a sequence that ``granted`` ([B + 1]
     int32, tl_pages_extend's) says was refused see nothing.  Returns out [T, n_heads,
     head_dim], and the log-sums [T, n_heads] fp32 too with ``want_lse``.  For serving:
-    no gradients."""
+    no gradients (refused where a tensor asks for one)."""
+    if (query.requires_grad or key_pages.requires_grad or value_pages.requires_grad
+            or out is not None and out.requires_grad):
+        _no_gradients("tl_attend")
     v = _kv_view(key_pages, value_pages, page_table, length)
     dtype, shape, device = key_pages.dtype, query.shape, query.device
     qs = _rows3(query, dtype, "query", None, key_pages.shape[3])
