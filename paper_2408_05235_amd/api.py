@@ -32,14 +32,25 @@ def _stream():
     return _raw_stream(_raw_device())
 
 
-def _need(t, dtype, name, shape=None):
-    if (t is not None and t.is_cuda and t.dtype == dtype and t.is_contiguous()
-            and (shape is None or t.shape == shape)):
+def _stream_on(device):
+    """The stream for work on tensors of ``device`` (an index), which has to be
+    the current one."""
+    now = torch.cuda.current_device() if _raw_device is None else _raw_device()
+    if now != device:
+        raise ValueError(f"the tensors are on cuda:{device}, the current device is cuda:{now}")
+    return _stream() if _raw_stream is None else _raw_stream(now)
+
+
+def _need(t, dtype, name, shape=None, device=None):
+    if (t is not None and (t.is_cuda if device is None else t.get_device() == device) and t.dtype == dtype
+            and t.is_contiguous() and (shape is None or t.shape == shape)):
         return t
     if t is None:
         raise ValueError(f"{name} is required")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
+    if device is not None and t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, other tensors are on cuda:{device}")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     if not t.is_contiguous():
@@ -373,15 +384,17 @@ def _strides(t):
     return tuple([0 if n <= 1 else s for n, s in zip(t.shape, t.stride())])
 
 
-def _rows3(t, dtype, name, heads=None, dim=None, tokens=None):
+def _rows3(t, dtype, name, device, heads=None, dim=None, tokens=None):
     """The strides of packed rows [tokens, heads, dim], whatever they are for
     tokens and heads (a view into a layer's fused product, say)."""
     shape, strides = t.shape, t.stride()
-    if (t.is_cuda and t.dtype == dtype and len(shape) == 3 and strides[2] == 1 and (heads is None or shape[1] == heads)
-            and shape[2] == dim and (tokens is None or shape[0] == tokens)):
+    if (t.get_device() == device and t.dtype == dtype and len(shape) == 3 and strides[2] == 1
+            and (heads is None or shape[1] == heads) and shape[2] == dim and (tokens is None or shape[0] == tokens)):
         return strides if shape[0] > 1 and shape[1] > 1 else _strides(t)
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, the pages are on cuda:{device}")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     if len(shape) != 3 or (shape[2] > 1 and strides[2] != 1):
@@ -392,13 +405,15 @@ def _rows3(t, dtype, name, heads=None, dim=None, tokens=None):
     return _strides(t)
 
 
-def _kv_view(key_pages, value_pages, page_table, length):
+def _kv_view(key_pages, value_pages, page_table, length, device):
     shape, strides, dtype = key_pages.shape, key_pages.stride(), key_pages.dtype
     kind = _KV_DTYPES.get(dtype)
     if kind is None:
         raise ValueError(f"key_pages must be bfloat16 or float16, got {dtype}")
-    if not key_pages.is_cuda or not value_pages.is_cuda:
+    if device < 0 or not value_pages.is_cuda:
         raise ValueError("pages must be device tensors")
+    if value_pages.get_device() != device:
+        raise ValueError(f"key_pages are on cuda:{device}, value_pages on {value_pages.device}")
     if len(shape) != 4 or shape != value_pages.shape or dtype != value_pages.dtype:
         raise ValueError("key_pages and value_pages must be [n_pages, n_kv_heads, page_tokens, head_dim] alike")
     n_pages, heads, tokens, dim = shape
@@ -409,8 +424,8 @@ def _kv_view(key_pages, value_pages, page_table, length):
     if page_table.dim() != 2:
         raise ValueError("page_table must be [n_seqs, table_width]")
     n_seqs, width = page_table.shape
-    _need(page_table, torch.int32, "page_table")
-    _need(length, torch.int32, "length", (n_seqs,))
+    _need(page_table, torch.int32, "page_table", None, device)
+    _need(length, torch.int32, "length", (n_seqs,), device)
     return _lib.KvView(_VIEW_SIZE, kind, heads, dim, tokens, width, n_pages, n_seqs, strides[0], strides[1],
                        strides[2], key_pages.data_ptr(), value_pages.data_ptr(), page_table.data_ptr(),
                        length.data_ptr())
@@ -422,8 +437,8 @@ def _no_gradients(who):
         raise ValueError(f"{who} has no gradients: call it under torch.no_grad(), or with detached tensors")
 
 
-def _granted(t, n):
-    return None if t is None else _need(t, torch.int32, "granted", (n + 1,)).data_ptr()
+def _granted(t, n, device):
+    return None if t is None else _need(t, torch.int32, "granted", (n + 1,), device).data_ptr()
 
 
 def tl_kv_append(key, value, key_pages, value_pages, page_table, length, q_offset=None, granted=None):
@@ -437,14 +452,15 @@ def tl_kv_append(key, value, key_pages, value_pages, page_table, length, q_offse
     they are taken for the last of its ``length`` tokens.  No gradients."""
     if key.requires_grad or value.requires_grad or key_pages.requires_grad or value_pages.requires_grad:
         _no_gradients("tl_kv_append")
-    v = _kv_view(key_pages, value_pages, page_table, length)
+    device = key_pages.get_device()
+    v = _kv_view(key_pages, value_pages, page_table, length, device)
     dtype, (_, heads, _, dim), T = key_pages.dtype, key_pages.shape, key.shape[0]
-    ks, vs = _rows3(key, dtype, "key", heads, dim), _rows3(value, dtype, "value", heads, dim, T)
+    ks, vs = _rows3(key, dtype, "key", device, heads, dim), _rows3(value, dtype, "value", device, heads, dim, T)
     if q_offset is not None:
-        _need(q_offset, torch.int64, "q_offset", (page_table.shape[0] + 1,))
+        _need(q_offset, torch.int64, "q_offset", (page_table.shape[0] + 1,), device)
     a = _lib.KvAppendArgs(_APPEND_SIZE, 0, v, T, _p(q_offset), key.data_ptr(), value.data_ptr(), ks[0], ks[1], vs[0],
-                          vs[1], None if granted is None else _granted(granted, page_table.shape[0]))
-    check(lib().tl_kv_append(ctypes.byref(a), _stream()))
+                          vs[1], _granted(granted, page_table.shape[0], device))
+    check(lib().tl_kv_append(ctypes.byref(a), _stream_on(device)))
 
 
 def tl_attend(query, key_pages, value_pages, page_table, length, q_offset=None, window=0, sinks=0, scale=None,
@@ -462,43 +478,44 @@ def tl_attend(query, key_pages, value_pages, page_table, length, q_offset=None, 
     if (query.requires_grad or key_pages.requires_grad or value_pages.requires_grad
             or out is not None and out.requires_grad):
         _no_gradients("tl_attend")
-    v = _kv_view(key_pages, value_pages, page_table, length)
+    index = key_pages.get_device()
+    v = _kv_view(key_pages, value_pages, page_table, length, index)
     dtype, shape, device = key_pages.dtype, query.shape, query.device
-    qs = _rows3(query, dtype, "query", None, key_pages.shape[3])
+    qs = _rows3(query, dtype, "query", index, None, key_pages.shape[3])
     T, heads, dim = shape
     if q_offset is not None:
-        _need(q_offset, torch.int64, "q_offset", (page_table.shape[0] + 1,))
+        _need(q_offset, torch.int64, "q_offset", (page_table.shape[0] + 1,), index)
     if out is None:
         out = torch.empty(shape, dtype=dtype, device=device)
     else:
-        _need(out, dtype, "out", shape)
+        _need(out, dtype, "out", shape, index)
     lse = torch.empty((T, heads), dtype=torch.float32, device=device) if want_lse else None
     a = _lib.AttendArgs(_ATTEND_SIZE, heads, v, T, _p(q_offset), query.data_ptr(), qs[0], qs[1],
                         dim ** -0.5 if scale is None else float(scale), int(window), int(sinks), int(max_length),
-                        out.data_ptr(), _p(lse), None, 0,
-                        _granted(granted, page_table.shape[0]))
+                        out.data_ptr(), _p(lse), None, 0, _granted(granted, page_table.shape[0], index))
     L, ref = lib(), ctypes.byref(a)
     if workspace is None:
         n = L.tl_attend_workspace_bytes(ref)
         if n:
             workspace = torch.empty(n, dtype=torch.uint8, device=device)
-    elif workspace.dtype != torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous uint8 device tensor")
+    else:
+        _need(workspace, torch.uint8, "workspace", None, index)
     if workspace is not None:
         a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
-    check(L.tl_attend(ref, _stream()))
+    check(L.tl_attend(ref, _stream_on(index)))
     return (out, lse) if want_lse else out
 
 
 def _pages(ref, page_table, length, page_tokens, granted=None):
     _need(ref, torch.int32, "ref")
-    _need(page_table, torch.int32, "page_table")
+    device = ref.get_device()
+    _need(page_table, torch.int32, "page_table", None, device)
     if ref.dim() != 1 or page_table.dim() != 2:
         raise ValueError("ref must be [n_pages] and page_table [n_slots, table_width]")
     n_slots, width = page_table.shape
-    _need(length, torch.int32, "length", (n_slots,))
+    _need(length, torch.int32, "length", (n_slots,), device)
     return _lib.Pages(_PAGES_SIZE, int(page_tokens), ref.shape[0], n_slots, width, 0, ref.data_ptr(),
-                      page_table.data_ptr(), length.data_ptr(), _granted(granted, n_slots))
+                      page_table.data_ptr(), length.data_ptr(), _granted(granted, n_slots, device))
 
 
 def _pages_work(g, ref, work):
@@ -506,7 +523,7 @@ def _pages_work(g, ref, work):
     words = lib().tl_pages_work_words(ctypes.byref(g))
     if work is None:
         return torch.empty(words, dtype=torch.int32, device=ref.device)
-    if _need(work, torch.int32, "work").numel() < words:
+    if _need(work, torch.int32, "work", None, ref.get_device()).numel() < words:
         raise ValueError("work is too small (tl_pages_work_words)")
     return work
 
@@ -518,11 +535,12 @@ def tl_pages_extend(ref, page_table, length, add, page_tokens, status=None, work
     each slot got since the last append, for tl_kv_append and tl_attend."""
     g = _pages(ref, page_table, length, page_tokens, granted)
     work = _pages_work(g, ref, work)
-    _need(add, torch.int32, "add", (g.n_slots,))
+    device = ref.get_device()
+    _need(add, torch.int32, "add", (g.n_slots,), device)
     if status is None:
         status = torch.empty(g.n_slots, dtype=torch.int32, device=ref.device)
-    _need(status, torch.int32, "status", (g.n_slots,))
-    check(lib().tl_pages_extend(ctypes.byref(g), _p(add), _p(status), _p(work), _stream()))
+    _need(status, torch.int32, "status", (g.n_slots,), device)
+    check(lib().tl_pages_extend(ctypes.byref(g), _p(add), _p(status), _p(work), _stream_on(device)))
     return status
 
 
@@ -532,20 +550,21 @@ def tl_pages_fork(ref, page_table, length, parent, child, page_tokens, work=None
     copy_dst, status) int32 [F]; the pages still have to be copied (tl_pages_copy)."""
     g = _pages(ref, page_table, length, page_tokens, granted)
     work = _pages_work(g, ref, work)
-    F = parent.numel()
-    _need(parent, torch.int32, "parent", (F,))
-    _need(child, torch.int32, "child", (F,))
+    F, device = parent.numel(), ref.get_device()
+    _need(parent, torch.int32, "parent", (F,), device)
+    _need(child, torch.int32, "child", (F,), device)
     src, dst, status = torch.empty((3, F), dtype=torch.int32, device=ref.device).unbind(0)
     check(lib().tl_pages_fork(ctypes.byref(g), F, _p(parent), _p(child), _p(src), _p(dst), _p(status), _p(work),
-                              _stream()))
+                              _stream_on(device)))
     return src, dst, status
 
 
 def tl_pages_free(ref, page_table, length, slots, page_tokens):
     """The sequences in ``slots`` (int32) leave, in place (tl_pages_free)."""
     g = _pages(ref, page_table, length, page_tokens)
-    _need(slots, torch.int32, "slots")
-    check(lib().tl_pages_free(ctypes.byref(g), slots.numel(), _p(slots), _stream()))
+    device = ref.get_device()
+    _need(slots, torch.int32, "slots", None, device)
+    check(lib().tl_pages_free(ctypes.byref(g), slots.numel(), _p(slots), _stream_on(device)))
 
 
 def tl_pages_compact(ref, page_table, length, page_tokens, out=None, work=None):
@@ -554,7 +573,7 @@ def tl_pages_compact(ref, page_table, length, page_tokens, out=None, work=None):
     hold the arguments themselves, or allocated) and the moves (copy_src,
     copy_dst, n_copies [1], all int32), which tl_pages_copy has to make."""
     g = _pages(ref, page_table, length, page_tokens)
-    o, half = out or {}, ref.shape[0] // 2
+    o, half, device = out or {}, ref.shape[0] // 2, ref.get_device()
     # what is not given comes in as few allocations as can be
     sizes = [half, half, 1, lib().tl_pages_work_words(ctypes.byref(g)) if work is None else 0]
     moves = list(torch.empty(sum(sizes), dtype=torch.int32, device=ref.device).split(sizes))
@@ -564,13 +583,13 @@ def tl_pages_compact(ref, page_table, length, page_tokens, out=None, work=None):
         t = o.get(name)
         if t is None:
             return torch.empty(shape, dtype=torch.int32, device=ref.device) if default is None else default
-        return _need(t, torch.int32, name, shape)
+        return _need(t, torch.int32, name, shape, device)
 
     r = dict(ref=buf("ref", ref.shape), page_table=buf("page_table", page_table.shape),
              copy_src=buf("copy_src", (half,), moves[0]), copy_dst=buf("copy_dst", (half,), moves[1]),
              n_copies=buf("n_copies", (1,), moves[2]))
     check(lib().tl_pages_compact(ctypes.byref(g), _p(r["ref"]), _p(r["page_table"]), _p(r["copy_src"]),
-                                 _p(r["copy_dst"]), _p(r["n_copies"]), _p(work), _stream()))
+                                 _p(r["copy_dst"]), _p(r["n_copies"]), _p(work), _stream_on(device)))
     return r
 
 
@@ -581,15 +600,16 @@ def tl_pages_copy(pages, copy_src, copy_dst, n_copies=None):
     device) when given (tl_pages_copy)."""
     if not pages.is_cuda or not pages.is_contiguous() or pages.dim() < 4:
         raise ValueError("pages must be a contiguous device tensor [..., n_pages, n_kv_heads, page_tokens, head_dim]")
-    n = copy_src.numel()
-    _need(copy_src, torch.int32, "copy_src", (n,))
-    _need(copy_dst, torch.int32, "copy_dst", (n,))
-    _opt(n_copies, torch.int32, "n_copies", (1,))
+    n, device = copy_src.numel(), pages.get_device()
+    _need(copy_src, torch.int32, "copy_src", (n,), device)
+    _need(copy_dst, torch.int32, "copy_dst", (n,), device)
+    if n_copies is not None:
+        _need(n_copies, torch.int32, "n_copies", (1,), device)
     n_pages = pages.shape[-4]
     page = pages.shape[-3] * pages.shape[-2] * pages.shape[-1] * pages.element_size()
     planes = pages.numel() * pages.element_size() // (page * n_pages) if page * n_pages else 0
     check(lib().tl_pages_copy(_p(pages), n_pages, page, page, planes, page * n_pages, _p(copy_src), _p(copy_dst), n,
-                              _p(n_copies), _stream()))
+                              _p(n_copies), _stream_on(device)))
 
 
 class KVCache:
