@@ -424,11 +424,22 @@ def _kv_view(key_pages, value_pages, page_table, length, device):
     if page_table.dim() != 2:
         raise ValueError("page_table must be [n_seqs, table_width]")
     n_seqs, width = page_table.shape
-    _need(page_table, torch.int32, "page_table", None, device)
-    _need(length, torch.int32, "length", (n_seqs,), device)
+    if page_table.get_device() != device or page_table.dtype != torch.int32 or not page_table.is_contiguous():
+        _need(page_table, torch.int32, "page_table", None, device)
+    if (length.get_device() != device or length.dtype != torch.int32 or not length.is_contiguous()
+            or length.shape != (n_seqs,)):
+        _need(length, torch.int32, "length", (n_seqs,), device)
     return _lib.KvView(_VIEW_SIZE, kind, heads, dim, tokens, width, n_pages, n_seqs, strides[0], strides[1],
                        strides[2], key_pages.data_ptr(), value_pages.data_ptr(), page_table.data_ptr(),
                        length.data_ptr())
+
+
+def _int32(x, name):
+    """``x`` as a 32-bit argument, which ctypes would cut to its low bits."""
+    x = int(x)
+    if not -(1 << 31) <= x < 1 << 31:
+        raise ValueError(f"{name} {x} does not fit 32 bits")
+    return x
 
 
 def _no_gradients(who):
@@ -438,7 +449,7 @@ def _no_gradients(who):
 
 
 def _granted(t, n, device):
-    return None if t is None else _need(t, torch.int32, "granted", (n + 1,), device).data_ptr()
+    return _need(t, torch.int32, "granted", (n + 1,), device).data_ptr()
 
 
 def tl_kv_append(key, value, key_pages, value_pages, page_table, length, q_offset=None, granted=None):
@@ -459,7 +470,7 @@ def tl_kv_append(key, value, key_pages, value_pages, page_table, length, q_offse
     if q_offset is not None:
         _need(q_offset, torch.int64, "q_offset", (page_table.shape[0] + 1,), device)
     a = _lib.KvAppendArgs(_APPEND_SIZE, 0, v, T, _p(q_offset), key.data_ptr(), value.data_ptr(), ks[0], ks[1], vs[0],
-                          vs[1], _granted(granted, page_table.shape[0], device))
+                          vs[1], None if granted is None else _granted(granted, page_table.shape[0], device))
     check(lib().tl_kv_append(ctypes.byref(a), _stream_on(device)))
 
 
@@ -478,6 +489,10 @@ def tl_attend(query, key_pages, value_pages, page_table, length, q_offset=None, 
     if (query.requires_grad or key_pages.requires_grad or value_pages.requires_grad
             or out is not None and out.requires_grad):
         _no_gradients("tl_attend")
+    window, sinks, max_length = int(window), int(sinks), int(max_length)
+    if (window | sinks | max_length) >> 31:
+        for name, x in (("window", window), ("sinks", sinks), ("max_length", max_length)):
+            _int32(x, name)
     index = key_pages.get_device()
     v = _kv_view(key_pages, value_pages, page_table, length, index)
     dtype, shape, device = key_pages.dtype, query.shape, query.device
@@ -491,8 +506,9 @@ def tl_attend(query, key_pages, value_pages, page_table, length, q_offset=None, 
         _need(out, dtype, "out", shape, index)
     lse = torch.empty((T, heads), dtype=torch.float32, device=device) if want_lse else None
     a = _lib.AttendArgs(_ATTEND_SIZE, heads, v, T, _p(q_offset), query.data_ptr(), qs[0], qs[1],
-                        dim ** -0.5 if scale is None else float(scale), int(window), int(sinks), int(max_length),
-                        out.data_ptr(), _p(lse), None, 0, _granted(granted, page_table.shape[0], index))
+                        dim ** -0.5 if scale is None else float(scale), window, sinks, max_length,
+                        out.data_ptr(), _p(lse), None, 0,
+                        None if granted is None else _granted(granted, page_table.shape[0], index))
     L, ref = lib(), ctypes.byref(a)
     if workspace is None:
         n = L.tl_attend_workspace_bytes(ref)
@@ -507,6 +523,9 @@ def tl_attend(query, key_pages, value_pages, page_table, length, q_offset=None, 
 
 
 def _pages(ref, page_table, length, page_tokens, granted=None):
+    page_tokens = int(page_tokens)
+    if page_tokens >> 31:
+        _int32(page_tokens, "page_tokens")
     _need(ref, torch.int32, "ref")
     device = ref.get_device()
     _need(page_table, torch.int32, "page_table", None, device)
@@ -514,8 +533,9 @@ def _pages(ref, page_table, length, page_tokens, granted=None):
         raise ValueError("ref must be [n_pages] and page_table [n_slots, table_width]")
     n_slots, width = page_table.shape
     _need(length, torch.int32, "length", (n_slots,), device)
-    return _lib.Pages(_PAGES_SIZE, int(page_tokens), ref.shape[0], n_slots, width, 0, ref.data_ptr(),
-                      page_table.data_ptr(), length.data_ptr(), _granted(granted, n_slots, device))
+    return _lib.Pages(_PAGES_SIZE, page_tokens, ref.shape[0], n_slots, width, 0, ref.data_ptr(),
+                      page_table.data_ptr(), length.data_ptr(),
+                      None if granted is None else _granted(granted, n_slots, device))
 
 
 def _pages_work(g, ref, work):

@@ -95,3 +95,16 @@ def test_tensors_of_two_devices(monkeypatch, call, names):
             call(fakes("cuda:1", None))
         with pytest.raises(AssertionError, match="was called"):        # all of them right
             call(fakes("cuda:0", None))
+
+
+@pytest.mark.parametrize("value", [2 ** 31, 2 ** 32 + 5, -2 ** 32, 10 ** 30])
+def test_numbers_beyond_32_bits(value):
+    """They were cut to their low bits: a window of 2^32 + 5 tokens was one of 5."""
+    for name in ("window", "sinks", "max_length"):
+        with pytest.raises(ValueError, match=name):
+            attend(cpu(), **{name: value})
+    i = torch.zeros(3, dtype=torch.int32)
+    for call in (lambda: api.tl_pages_extend(i, i[None], i, i, value), lambda: api.tl_pages_fork(i, i[None], i, i, i, value),
+                 lambda: api.tl_pages_free(i, i[None], i, i, value), lambda: api.tl_pages_compact(i, i[None], i, value)):
+        with pytest.raises(ValueError, match="page_tokens"):
+            call()
