@@ -4,8 +4,11 @@
 //
 // Rows of a sequence and a KV head are its new tokens times the query heads
 // that share the head.  Sequences of up to 16 rows (one new token, or a few) are
-// bound by reading their keys and values once (few_rows), those with more by the
-// matrix products (tile_rows).
+// bound by reading their keys and values once (few_rows), long prompts by the
+// matrix products (tile_rows, which takes all sequences of more than 16 rows that
+// offsets are given for).  Without offsets, one new token each, every sequence is
+// few_rows': for more than 16 heads on a KV head in as many workgroups of 16 rows as it
+// takes, each of which reads the keys and values.
 #include <hip/hip_runtime.h>
 
 #include <float.h>
@@ -25,7 +28,8 @@ namespace {
 constexpr int kFewWaves = 4, kFewThreads = kFewWaves * kWave;
 
 // Bound by reading: 256 sequences of up to 4352 tokens, 20 heads with their
-// own keys, take 0.90 ms, 6.3 TB/s (a copy of 2 GiB reaches 4.95).  Three
+// own keys, take 0.90 ms, 6.3 TB/s (reading 4 GiB with such loads and nothing
+// else reaches 7.1, a copy of 2 GiB 4.95).  Three
 // wavefronts a SIMD (12 steps of 16 KB on their way in a CU): 0.93 ms with two, and
 // 97 and 108 us for 4 sequences of 20011 to 36864 tokens.  (Two of a workgroup of
 // eight: wide_few.)
@@ -99,7 +103,11 @@ hipError_t launch_join(const AttendLaunch& f, int64_t few_slots, int64_t tile_sl
 }
 
 // Row tiles of a sequence and head for few_rows, its workgroups per part, and
-// slots of a sequence and head, and of all.
+// slots of a sequence and head, and of all.  (More than one row tile against
+// tile_rows, which the same call with offsets gets, us: 64 sequences of 16 to 1280
+// tokens with 32, 64 and 71 heads on one 21, 30, 37 and 28, 31, 34; 256 of 500 27, 50, 62
+// and 39, 40, 41; 8 of 20000 34, 51, 79 and 42, 42, 43.  So few_rows is the better one
+// up to 32 heads; beyond 48 it reads too often.)
 int32_t few_row_tiles(const AttendParams& p) { return p.c.q_offset ? 1 : (p.group + kFewRows - 1) / kFewRows; }
 int64_t few_blocks(const AttendParams& p) { return p.c.n_seqs * p.c.n_kv_heads * few_row_tiles(p); }
 int32_t few_slot_rows(const AttendParams& p) { return p.c.q_offset ? kFewRows : p.group; }
@@ -125,7 +133,8 @@ constexpr SplitRule kSplitFew = {768, kFewWaves * kFewTile, 8192};
 constexpr SplitRule kSplitMixed = {512, 8 * kFewTile, 8192};
 // tile_rows: a workgroup a CU; of half the CUs in a batch of more sequences
 // than row tiles, whose other sequences have few rows and read meanwhile (two
-// chunks of 512 tokens with 62 single tokens: 712 us so, 869 us on all CUs).
+// chunks of 512 tokens with 62 single tokens: 712 us so, 869 us on all CUs; the only
+// batch that was timed both ways).
 constexpr SplitRule kSplitTiles = {256, 256, INT64_MAX}, kSplitHalf = {128, 256, INT64_MAX};
 constexpr int64_t kMostParts = 256;
 constexpr int64_t kApartBytes = 192 << 20;
@@ -200,13 +209,17 @@ TileNumbers number_tiles(const AttendParams& p) {
     return {rows / tile + p.c.n_seqs, tile, true};
 }
 
+// The lengths are those that the host knows of: the table's width where the
+// caller gives no bound, and a short prompt in a wide table is split for tokens that it
+// has not (of 64, 500 and 1000 tokens, 32 heads on 8: 15, 25 and 38 us in a table of
+// their own size or with the bound, 24, 31 and 43 in one for 36864).
 // (Workgroups without those that a ragged batch adds: too many parts cost
 // less than too few.)  Rows are many here, and so are the parts' sums, which are
 // written and read in 32 bits: as many parts as make their time, 26 ns a token,
 // and that of the join least.  A prompt of 1000 tokens, 32 heads on 8: 37 us in
 // one part, 55 in three; 8 of up to 1916, 4 heads on one: 63 us in one, 75 in
 // three; 512 new tokens behind 16384: 155 us in four, 439 in one; 64: 41 us in 32, 423
-// in one.
+// in one.  (All of heads of 128; others were not timed apart.)
 int64_t tile_parts(const AttendParams& p) {
     if (!needs_tiles(p)) return 1;
     const int64_t tiles = std::max<int64_t>(1, p.c.n_tokens * p.group / tile_rows_of(p.c.head_dim));

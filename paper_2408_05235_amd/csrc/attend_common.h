@@ -85,7 +85,10 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // Weights are rounded to the 16-bit type for the product with the values: the
 // matrix units take no more, and the output has no more (each is off by up to
 // 2^-9 of itself in bf16 and 2^-12 in f16; their sum is taken in 32 bits, before the
-// rounding).  f16 has no normal numbers below 2^-14: with a largest weight of 1
+// rounding).  Against 64 bits the output of one token is off by 1.9e-3 of itself so
+// and by 1.65e-3 (its own rounding) with weights of 32 bits; a second product, with
+// what the rounding leaves, would cost few_rows 0.2 to 0.8% alone and 1.4% beside
+// tile_rows, and tile_rows half as many matrix instructions again.  f16 has no normal numbers below 2^-14: with a largest weight of 1
 // those of less than 2^-25 would vanish, of which a long sequence can have many.  So
 // weights are relative to 2^-LIFT times the largest and at most 2^15 (tile_rows
 // lets them grow by 2^kGrowTiles before it scales its sums down): those of 2^-29
@@ -166,8 +169,11 @@ struct AttendLaunch {
 
 // Sequences of up to so many rows (new tokens x query heads of a KV head) are
 // few_rows', the others tile_rows'.  64 sequences of 16 to 1280 tokens with 16 rows
-// take 62 us so and 113 in tile_rows, 128 with 8 rows of 16 to 4352 250 and 339; at 32
-// rows few_rows would read everything twice.
+// take 62 us so and 113 in tile_rows, 128 with 8 rows of 16 to 4352 250 and 339.  A
+// wavefront of few_rows holds 16 rows and more would read everything again; in
+// tile_rows 17 to 64 rows leave most of a workgroup's 256 empty: those 64 sequences
+// with 20, 32 and 64 rows take 94, 83 and 70 us, 256 of 500 tokens 174, 168 and 190
+// (112 with 16 rows; reading once takes 74).
 constexpr int kFewRows = 16;
 
 // A workgroup's wavefronts, and the rows that they have in tile_rows: two

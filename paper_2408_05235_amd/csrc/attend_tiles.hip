@@ -3,7 +3,8 @@
 //
 // Rows of a sequence and a KV head are its new tokens times the query heads that
 // share the head, token by token; so the heads of a group share every key and value
-// that is read, and 128 rows are few tokens wide.
+// that is read, and a tile of 256 rows (128 for heads of more than 128 elements) is
+// few tokens wide.
 #include <hip/hip_runtime.h>
 
 #include <float.h>
@@ -120,13 +121,16 @@ __device__ __forceinline__ int value_exchange(int token) {
 // registers hold one wavefront, which takes the phases in turn.)  Copies of later
 // steps are issued between the matrix instructions, one at a time.
 //
-// 32768 tokens through a window of 4096, 8 heads on one KV head: 0.57 ms, 909
-// TFLOP/s; 8 ragged prompts of up to 4096 tokens, 32 heads on 8: 0.55 ms, 795
-// (a 16384^3 product of the library: 1363).  What bounds it is the power budget:
-// the clock falls to 1.7 to 1.9 GHz, and a step takes 4040 cycles of which the matrix
-// units are busy 2048.  A wavefront gets 32 bytes a cycle from LDS, just what its
-// matrix instructions use with 32 rows; 64 rows a wavefront would halve that, but
-// the compiler does not keep their scores in registers.
+// 32768 tokens through a window of 4096, 8 heads on one KV head: 0.56 ms, 925
+// TFLOP/s; 8 ragged prompts of up to 4096 tokens, 32 heads on 8: 0.54 ms, 813
+// (a 16384^3 product of the library: 1363).  A step takes 4040 cycles, of which the
+// matrix units are busy 2048; over the launch, its first and last steps included, they
+// are busy 42% and 37% of the cycles, at 1.97 GHz (few_rows alone runs at 2.31).
+// What holds a step up most is the operands' reads from LDS: without those of the
+// keys it takes a fifth less, and without the exponentials, the copies or the values'
+// reads 6 to 14%.  A wavefront gets 32 bytes a cycle from LDS, just what its matrix
+// instructions use with 32 rows; 64 rows a wavefront would halve that, but the compiler
+// does not keep their scores in registers.
 template <int DP>
 struct TileLds {
     // Steps in LDS: step v copies the keys of step v + kRing - 1 and the values

@@ -3,8 +3,9 @@
 //
 // All of it is memory traffic and latency: no call computes more than
 // prefix sums of counts.  Free pages are listed by ballots in ascending order, so
-// that the tables do not depend on timing; the only atomics add to page
-// counts, whose sums do not depend on the order.
+// that the tables do not depend on timing; atomics add to page counts, take the least
+// of the forks that claim a child and exchange a freed slot's length for 0, all of
+// which come out the same in any order.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
