@@ -137,6 +137,12 @@ constexpr SplitRule kSplitMixed = {512, 8 * kFewTile, 8192};
 // batch that was timed both ways).
 constexpr SplitRule kSplitTiles = {256, 256, INT64_MAX}, kSplitHalf = {128, 256, INT64_MAX};
 constexpr int64_t kMostParts = 256;
+// Parts of `most` tokens, which even out a batch that has a long sequence, as
+// long as their sums take no more than this: the host knows the table's width and not
+// the lengths.  4096 sequences of 16 to 1000 tokens, 32 heads on 8, in a table for a
+// million take 5.6 ms so, with all 128 parts 20 ms and 34 GB, with 256 MiB 2.1 ms; with one
+// of 500000 tokens among them (and offsets) 4.9, 23 and 11.7.
+constexpr int64_t kEvenBytes = 1ll << 30;
 constexpr int64_t kApartBytes = 192 << 20;
 
 // Tokens that a sequence's rows see at most, from what the host knows.
@@ -168,7 +174,7 @@ bool apart(const AttendParams& p) {
            most_tokens(p) * p.c.n_seqs * p.c.n_kv_heads * p.c.head_dim * 4 >= kApartBytes;
 }
 
-int64_t wanted_parts(const AttendParams& p, const SplitRule& rule, int64_t blocks) {
+int64_t wanted_parts(const AttendParams& p, const SplitRule& rule, int64_t blocks, int64_t slots) {
     const int64_t tokens = most_tokens(p);
     // A join costs 4 to 5 us with its launch.  It does not pay for two parts'
     // tokens (8 heads of 250: 10.0 us in one, 14.1 in two), nor for short sequences
@@ -181,7 +187,9 @@ int64_t wanted_parts(const AttendParams& p, const SplitRule& rule, int64_t block
     // 157 parts 15.4, 16.3 and 17.2 us; 2 of 36864 in 64, 128 and 256 22.9, 20.6 and 24.9;
     // 1 of 131072 53.0, 36.3 and 32.8.
     while (fill > 1 && 5 * fill * fill > 2 * tokens) --fill;
-    const int64_t n = std::max(fill, tokens / rule.most + (tokens % rule.most != 0));
+    const int64_t even = std::min(tokens / rule.most + (tokens % rule.most != 0),
+                                  kEvenBytes / (slots * p.c.head_dim * (int64_t)sizeof(float)));
+    const int64_t n = std::max(fill, even);
     return std::max<int64_t>(1, std::min(n, kMostParts));
 }
 const SplitRule& few_rule(const AttendParams& p) {
@@ -190,7 +198,7 @@ const SplitRule& few_rule(const AttendParams& p) {
 // (a lone sequence with many rows leaves none to few_rows)
 int64_t few_parts(const AttendParams& p) {
     if (!needs_few(p) || wide_few(p) || (needs_tiles(p) && p.c.n_seqs == 1)) return 1;
-    return wanted_parts(p, few_rule(p), few_blocks(p));
+    return wanted_parts(p, few_rule(p), few_blocks(p), few_slots(p));
 }
 // How row tiles are numbered.  A sequence of r rows has ceil(r / ROWS), which
 // is at most floor(r / ROWS) + 1, and none if r <= kFewRows, so at most
@@ -223,7 +231,8 @@ TileNumbers number_tiles(const AttendParams& p) {
 int64_t tile_parts(const AttendParams& p) {
     if (!needs_tiles(p)) return 1;
     const int64_t tiles = std::max<int64_t>(1, p.c.n_tokens * p.group / tile_rows_of(p.c.head_dim));
-    const int64_t most = wanted_parts(p, p.c.n_seqs > tiles && !apart(p) ? kSplitHalf : kSplitTiles, tiles * p.c.n_kv_heads);
+    const int64_t most = wanted_parts(p, p.c.n_seqs > tiles && !apart(p) ? kSplitHalf : kSplitTiles,
+                                      tiles * p.c.n_kv_heads, tile_slots(p));
     const int64_t sums = tile_slots(p) * p.c.head_dim * 2 * (int64_t)sizeof(float);     // bytes, of a part
     // (ns: a round of a workgroup a CU takes 8 us to begin and end; the sums at
     // 4.5 TB/s; a number without a tile holds a CU for 1.5 us)

@@ -27,10 +27,9 @@ def exact_rows(q, k, v, most):
 
 
 def test_many_sequences_of_one_token(gpu):
-    """More workgroups than a launch takes, and more rows to join than a launch
-    takes."""
+    """More workgroups than a launch takes, of two parts each."""
     from paper_2408_05235_amd import api
-    n, heads, dim, most = 2 ** 22 + 5, 16, 8, 3
+    n, heads, dim, most = 2 ** 24 + 5, 1, 8, 3
     k, v = page_of(1, 65536, dim)
     q = torch.randn(heads, dim, device="cuda").bfloat16()
     length = few_lengths(n, most)
