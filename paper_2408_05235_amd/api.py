@@ -426,7 +426,7 @@ def _kv_view(key_pages, value_pages, page_table, length, device):
     n_seqs, width = page_table.shape
     if page_table.get_device() != device or page_table.dtype != torch.int32 or not page_table.is_contiguous():
         _need(page_table, torch.int32, "page_table", None, device)
-    if (length.get_device() != device or length.dtype != torch.int32 or not length.is_contiguous()
+    if (length is None or length.get_device() != device or length.dtype != torch.int32 or not length.is_contiguous()
             or length.shape != (n_seqs,)):
         _need(length, torch.int32, "length", (n_seqs,), device)
     return _lib.KvView(_VIEW_SIZE, kind, heads, dim, tokens, width, n_pages, n_seqs, strides[0], strides[1],
@@ -528,11 +528,15 @@ def _pages(ref, page_table, length, page_tokens, granted=None):
         _int32(page_tokens, "page_tokens")
     _need(ref, torch.int32, "ref")
     device = ref.get_device()
-    _need(page_table, torch.int32, "page_table", None, device)
+    if (page_table is None or page_table.get_device() != device or page_table.dtype != torch.int32
+            or not page_table.is_contiguous()):
+        _need(page_table, torch.int32, "page_table", None, device)
     if ref.dim() != 1 or page_table.dim() != 2:
         raise ValueError("ref must be [n_pages] and page_table [n_slots, table_width]")
     n_slots, width = page_table.shape
-    _need(length, torch.int32, "length", (n_slots,), device)
+    if (length is None or length.get_device() != device or length.dtype != torch.int32 or length.shape != (n_slots,)
+            or not length.is_contiguous()):
+        _need(length, torch.int32, "length", (n_slots,), device)
     return _lib.Pages(_PAGES_SIZE, page_tokens, ref.shape[0], n_slots, width, 0, ref.data_ptr(),
                       page_table.data_ptr(), length.data_ptr(),
                       None if granted is None else _granted(granted, n_slots, device))
