@@ -215,7 +215,7 @@ def prepare(case, seed):
     table[torch.from_numpy(at).cuda()] = place.to(torch.int32)
     s.update(table=table.view(B, width), length=dev(old + new))
     s["offset"] = dev(np.concatenate([[0], np.cumsum(new)]), torch.int64) if case["nhi"] else None
-    T = int(new.sum())
+    T = s["tokens"] = int(new.sum())
     if case["kind"] != "select":
         shape = (pool, Hkv, N, D) if case["order"] == "head" else (pool, N, Hkv, D)
         pages = [randn(*shape) for _ in range(1 + (case["kind"] == "attend"))]
@@ -270,7 +270,7 @@ def _run_own(s):
     if c["kind"] == "sample":
         return list(api.tl_sample(s["x"], s["u"], s["temperature"], s["top_k"], s["top_p"], s["min_p"], want_logprob=True))
     if c["kind"] == "bounds":
-        api.tl_page_bounds(s["k"], s["bounds"], s["scale"], s["table"], s["length"], s["offset"])
+        api.tl_page_bounds(s["k"], s["bounds"], s["scale"], s["table"], s["length"], s["tokens"], s["offset"])
         return [s["bounds"], s["scale"]]
     if c["kind"] == "select":
         return [api.tl_select_pages(s["q"], s["bounds"], s["scale"], s["table"], s["length"], c["N"], c["K"], s["offset"],
