@@ -38,7 +38,7 @@ __device__ __forceinline__ int64_t tile_seq(const AttendLaunch& F, int64_t tile)
     while (hi - lo > 1) {
         const int64_t step = (hi - lo + kWave - 1) / kWave, at = lo + lane_id() * step;
         const bool below = at < hi && first_tile(F, at) <= tile;
-        const int k = max(__popcll(__ballot(below)) - 1, 0);
+        const int k = max((int)__popcll(__ballot(below)) - 1, 0);
         lo += k * step;
         hi = min(lo + step, hi);
     }
