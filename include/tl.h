@@ -18,8 +18,9 @@
  * search as the paper states it, querying the model only at probed
  * frequencies) and tl_admit (the admission control of Sec. 4.3.2 for one new
  * query per scenario).  Below them stands the machine that they plan: the paged
- * cache whose blocks tl_project counts (tl_pages_*, tl_kv_append) and the
- * attention over it (tl_attend).
+ * cache whose blocks tl_project counts (tl_pages_*, tl_kv_append), the
+ * attention over it (tl_attend; over selected pages tl_page_bounds, tl_select_pages,
+ * tl_attend_pages), and what an iteration does around it (tl_norm, tl_sample).
  *
  * Conventions shared by every entry point
  *   - Pointers are DEVICE pointers (memory of the device that is current on
@@ -557,6 +558,92 @@ tl_status tl_attend(const tl_attend_args* args, void* stream);
 uint64_t tl_attend_workspace_bytes(const tl_attend_args* args);   /* 0 for arguments that tl_attend refuses */
 
 /* ------------------------------------------------------------------------
+ * Attention over a few of the pages, which a cheap score selects for each new
+ * token and KV head: tl_page_bounds after tl_kv_append, then tl_select_pages, then
+ * tl_attend_pages.
+ *
+ * The summary of page p and KV head g, of its tokens that are in the cache (those
+ * of a sequence's last page end at its length):
+ *   s  = (the largest absolute key value) x fl(1 / 127)            scale[p * scale_stride + g]
+ *   lo = floor(min_t k_td / s), hi = ceil(max_t k_td / s), within [-127, 127]
+ *                                        bounds[p][g][0][d] and bounds[p][g][1][d]
+ * in fp32, each operation rounded once.  Without a key that is not 0 all of it is 0;
+ * with one that is not finite s is +inf and the bounds are 0.
+ *
+ * Of a token at position p the pages 0 .. p / N that the table has are candidates.
+ * With z = (a head's largest absolute query value) x fl(1 / 127) and i_d = rint(q_d
+ * / z) (0 where z is 0 or a value is not finite, and z too), page j scores
+ *   score_j = max over the KV head's query heads of fl(z x sum_d max(i_d lo_d, i_d hi_d))
+ * times s_j; +inf where s_j is not finite.  The sums are exact.  The first
+ * `first` and the last `last` of the pages 0 .. p / N are taken always, then those
+ * that score best, of equal ones the lower page (a score that is NaN is the least),
+ * until there are n_select.
+ * ---------------------------------------------------------------------- */
+#define TL_MAX_SELECTED 4096        /* n_select */
+#define TL_MAX_GROUP 128            /* query heads per KV head of tl_select_pages */
+
+/* The summaries of the pages that the new tokens (rows as in tl_kv_append, whose
+ * call comes first) lie in, from all of the pages' keys.  Other pages' are left as
+ * they are. */
+typedef struct tl_page_bounds_args {
+    uint32_t struct_size;          /* sizeof(tl_page_bounds_args) */
+    uint32_t reserved;
+    tl_kv_view cache;              /* value_pages is not used */
+    int64_t n_tokens;              /* T >= 0 */
+    const int64_t* q_offset;       /* [B+1]; NULL = one token each */
+    int8_t* bounds;                /* [n_pages][n_kv_heads][2][D], 16-byte aligned */
+    float* scale;                  /* [n_pages][n_kv_heads] */
+    int64_t scale_stride;          /* elements between pages, >= 0 */
+    const int32_t* granted;        /* [n_seqs + 1], nullable, as in tl_kv_append */
+} tl_page_bounds_args;
+
+tl_status tl_page_bounds(const tl_page_bounds_args* args, void* stream);
+
+/* selected[i][g]: the n_select best pages (indices into the sequence's table row)
+ * of new token i and KV head g, ascending, -1 behind them where there are fewer.  Rows
+ * that belong to no sequence are left alone.  workspace: device memory of the caller,
+ * 16-byte aligned, for the scores, 4 x n_kv_heads x table_width bytes a token: of one
+ * token at least; with less than tl_select_pages_workspace_bytes(args) the tokens go
+ * in several launches.  A workspace serves one call at a time. */
+typedef struct tl_select_pages_args {
+    uint32_t struct_size;          /* sizeof(tl_select_pages_args) */
+    int32_t n_heads;               /* a multiple of cache.n_kv_heads, at most TL_MAX_GROUP times */
+    tl_kv_view cache;              /* the pages and their strides are not used */
+    int64_t n_tokens;              /* T >= 0 */
+    const int64_t* q_offset;       /* [B+1]; NULL = one token each */
+    const void* query;             /* [T][n_heads][D], strides in elements (multiples of 8) */
+    int64_t query_token_stride, query_head_stride;
+    const int8_t* bounds;          /* as in tl_page_bounds */
+    const float* scale;
+    int64_t scale_stride;
+    int32_t n_select;              /* 1 .. TL_MAX_SELECTED */
+    int32_t first, last;           /* >= 0, together at most n_select */
+    int32_t reserved;
+    int32_t* selected;             /* [T][n_kv_heads][n_select] */
+    void* workspace;
+    uint64_t workspace_bytes;
+    const int32_t* granted;        /* [n_seqs + 1], nullable, as in tl_attend */
+} tl_select_pages_args;
+
+tl_status tl_select_pages(const tl_select_pages_args* args, void* stream);
+uint64_t tl_select_pages_workspace_bytes(const tl_select_pages_args* args);   /* 0 for arguments that it refuses */
+
+/* tl_attend, where token i's heads of KV head g see, of the tokens up to its
+ * position, those of the pages selected[i][g] alone.  A list is a set: its order
+ * and repetitions do not matter, entries outside the table (and without a page) are
+ * nothing.  window and sinks must be 0.  What attend.workspace is for and how the
+ * values are rounded is as in tl_attend. */
+typedef struct tl_attend_pages_args {
+    uint32_t struct_size;          /* sizeof(tl_attend_pages_args) */
+    int32_t n_select;              /* 1 .. TL_MAX_SELECTED */
+    tl_attend_args attend;
+    const int32_t* selected;       /* [T][n_kv_heads][n_select] */
+} tl_attend_pages_args;
+
+tl_status tl_attend_pages(const tl_attend_pages_args* args, void* stream);
+uint64_t tl_attend_pages_workspace_bytes(const tl_attend_pages_args* args);   /* 0 for arguments that it refuses */
+
+/* ------------------------------------------------------------------------
  * The pool's pages.  ref[p] (int32 [n_pages]) counts the table entries that
  * hold page p; 0 = free.  Sequence slots are rows of page_table [n_slots]
  * [table_width]; the first ceil(length / N) entries of a row are its pages.
@@ -629,6 +716,77 @@ tl_status tl_pages_compact(const tl_pages* pages, int32_t* ref_out, int32_t* tab
 tl_status tl_pages_copy(void* pages, int64_t n_pages, int64_t page_bytes, int64_t page_stride, int32_t n_planes,
                         int64_t plane_stride, const int32_t* copy_src, const int32_t* copy_dst, int64_t n_pairs,
                         const int32_t* n_live, void* stream);
+
+/* ------------------------------------------------------------------------
+ * What an iteration does around its attention: the norm before a product, and
+ * the next tokens.
+ * ---------------------------------------------------------------------- */
+#define TL_F32 3
+#define TL_NORM_SAME (-1)
+#define TL_MAX_COLUMNS (1 << 22)
+
+/* With h = x (+ residual) per row of W columns, in fp32:
+ *   sum = h, rounded to dtype
+ *   y   = h / sqrt(mean h^2 + eps) x weight
+ * out is y rounded to dtype (group TL_NORM_SAME), or in 8 bits (e4m3: 4 exponent
+ * bits, 3 of mantissa, no infinities), out = e4m3(y / s), nearest even:
+ *   group 0   a scale a row,          s = max |y| / 448, at least 2^-100
+ *   group n   a scale for n columns,  a power of two in [16, 512]; the last may have fewer
+ * A row with a NaN or an infinity has NaN in its outputs (infinities 0 x inf; the
+ * scales of what holds a NaN are NaN).
+ * Rows may begin at any element.  out (group TL_NORM_SAME) and sum may be x or residual
+ * themselves where those are contiguous; otherwise no output overlaps an input. */
+typedef struct tl_norm_args {
+    uint32_t struct_size;          /* sizeof(tl_norm_args) */
+    int32_t dtype;                 /* TL_BF16, TL_F16 or TL_F32: of x, residual, weight, sum */
+    int64_t n_rows;                /* >= 0 */
+    int32_t n_cols;                /* W, 1 .. TL_MAX_COLUMNS */
+    int32_t group;
+    float eps;                     /* >= 0 */
+    uint32_t reserved;
+    const void* x;                 /* [n_rows][W], rows x_stride elements apart (>= 0) */
+    const void* residual;          /* nullable */
+    const void* weight;            /* [W] */
+    int64_t x_stride, residual_stride;
+    void* out;                     /* [n_rows][W], contiguous */
+    float* scale;                  /* [n_rows] or [n_rows][ceil(W / group)]; 8 bits only */
+    void* sum;                     /* [n_rows][W], contiguous; nullable, and only with residual */
+} tl_norm_args;
+
+tl_status tl_norm(const tl_norm_args* args, void* stream);
+
+/* One token a row from its logits x (a NaN counts as -inf) and a number u.  With m
+ * the largest, e_i = (x_i - m) / temperature in 64 bits (0 where x_i = m) and the
+ * order of the logits, of equal ones the lower index first, the weights are the whole
+ * numbers w_i = rint(2^40 exp(e_i)) and of the tokens
+ *   top_k > 0    the first top_k are kept; of these, with W the sum of their weights,
+ *   top_p < 1    the fewest first ones whose weights reach ceil(top_p x W), one at least;
+ *   min_p > 0    of these those of w >= ceil(min(min_p, 1) x 2^40).
+ * With W the sum of what is kept, r = min(floor(u x W), W - 1) (0 for u <= 0):
+ *   token   = the first, in index order, whose running sum of weights exceeds r
+ *   logprob = e - log(W / 2^40)
+ * so for given numbers the tokens do not depend on the launch, up to the exponential's
+ * last bit.  A temperature that is not above 0 takes the first of the order,
+ * with logprob 0.  A row whose logits are all -inf (or NaN) gives -1 and -inf.  A NaN
+ * among the settings is none. */
+typedef struct tl_sample_args {
+    uint32_t struct_size;          /* sizeof(tl_sample_args) */
+    int32_t dtype;                 /* TL_BF16, TL_F16 or TL_F32: of logits */
+    int64_t n_rows;                /* >= 0 */
+    int32_t n_cols;                /* tokens, 1 .. TL_MAX_COLUMNS */
+    uint32_t reserved;
+    const void* logits;            /* [n_rows][n_cols], rows stride elements apart (>= 0) */
+    int64_t stride;
+    const float* u;                /* [n_rows], in [0, 1) */
+    const float* temperature;      /* [n_rows]; NULL = 1 */
+    const int32_t* top_k;          /* [n_rows]; NULL, or <= 0: all */
+    const float* top_p;            /* [n_rows]; NULL, or >= 1: all */
+    const float* min_p;            /* [n_rows]; NULL, or <= 0: all */
+    int32_t* token;                /* [n_rows] */
+    float* logprob;                /* [n_rows], nullable */
+} tl_sample_args;
+
+tl_status tl_sample(const tl_sample_args* args, void* stream);
 
 #ifdef __cplusplus
 }

@@ -19,7 +19,8 @@ FLAG_BAD_REQUEST, FLAG_LOST, FLAG_OVERCOMMIT, FLAG_OVERFLOW, FLAG_UNSORTED = 1, 
 FLAG_BAD_CANDIDATE = 32
 STATUS_OK, STATUS_INFEASIBLE, STATUS_LOST, STATUS_INVALID = 0, 1, 2, 3
 ADMIT_OK, ADMIT_LOST, ADMIT_QUEUE_CAPACITY, ADMIT_QUEUE_TBT, ADMIT_QUEUE_E2E, ADMIT_INVALID = 0, 1, 2, 3, 4, 5
-BF16, F16 = 1, 2
+BF16, F16, F32 = 1, 2, 3
+NORM_SAME = -1
 PAGES_OK, PAGES_NONE_FREE, PAGES_TABLE_FULL, PAGES_BAD = 0, 1, 2, 3
 MAX_HEAD_DIM = 256
 MAX_HORIZON, MAX_BLOCK_TOKENS, MAX_FREQS, MAX_FEATURES, MAX_DEPTH = 8192, 65536, 4096, 4, 14
@@ -29,7 +30,9 @@ EXPORTED = ("tl_abi_version", "tl_last_error", "tl_forest_create", "tl_forest_de
             "tl_select_freq_binary", "tl_adjust_lengths", "tl_lattice_create", "tl_lattice_destroy",
             "tl_lattice_bytes", "tl_lattice_predict_grid", "tl_forest_predict_grid_noalloc",
             "tl_kv_append", "tl_attend", "tl_attend_workspace_bytes", "tl_pages_work_words", "tl_pages_extend",
-            "tl_pages_fork", "tl_pages_free", "tl_pages_compact", "tl_pages_copy")
+            "tl_pages_fork", "tl_pages_free", "tl_pages_compact", "tl_pages_copy",
+            "tl_page_bounds", "tl_select_pages", "tl_select_pages_workspace_bytes", "tl_attend_pages",
+            "tl_attend_pages_workspace_bytes", "tl_norm", "tl_sample")
 
 
 class ProjectArgs(ctypes.Structure):
@@ -73,6 +76,42 @@ class AttendArgs(ctypes.Structure):
         ("query_token_stride", i64), ("query_head_stride", i64), ("scale", f32), ("window", i32), ("sinks", i32),
         ("max_length", i32), ("out", P), ("lse", P), ("workspace", P), ("workspace_bytes", ctypes.c_uint64),
         ("granted", P),
+    ]
+
+
+class PageBoundsArgs(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", u32), ("reserved", u32), ("cache", KvView), ("n_tokens", i64), ("q_offset", P), ("bounds", P),
+        ("scale", P), ("scale_stride", i64), ("granted", P),
+    ]
+
+
+class SelectPagesArgs(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", u32), ("n_heads", i32), ("cache", KvView), ("n_tokens", i64), ("q_offset", P), ("query", P),
+        ("query_token_stride", i64), ("query_head_stride", i64), ("bounds", P), ("scale", P), ("scale_stride", i64),
+        ("n_select", i32), ("first", i32), ("last", i32), ("reserved", i32), ("selected", P), ("workspace", P),
+        ("workspace_bytes", ctypes.c_uint64), ("granted", P),
+    ]
+
+
+class AttendPagesArgs(ctypes.Structure):
+    _fields_ = [("struct_size", u32), ("n_select", i32), ("attend", AttendArgs), ("selected", P)]
+
+
+class NormArgs(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", u32), ("dtype", i32), ("n_rows", i64), ("n_cols", i32), ("group", i32), ("eps", f32),
+        ("reserved", u32), ("x", P), ("residual", P), ("weight", P), ("x_stride", i64), ("residual_stride", i64),
+        ("out", P), ("scale", P), ("sum", P),
+    ]
+
+
+class SampleArgs(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", u32), ("dtype", i32), ("n_rows", i64), ("n_cols", i32), ("reserved", u32), ("logits", P),
+        ("stride", i64), ("u", P), ("temperature", P), ("top_k", P), ("top_p", P), ("min_p", P), ("token", P),
+        ("logprob", P),
     ]
 
 
@@ -153,6 +192,14 @@ def lib():
     L.tl_pages_compact.restype = ctypes.c_int
     L.tl_pages_copy.argtypes = [P, i64, i64, i64, i32, i64, P, P, i64, P, P]
     L.tl_pages_copy.restype = ctypes.c_int
+    for name, args in (("tl_page_bounds", PageBoundsArgs), ("tl_select_pages", SelectPagesArgs),
+                       ("tl_attend_pages", AttendPagesArgs), ("tl_norm", NormArgs), ("tl_sample", SampleArgs)):
+        getattr(L, name).argtypes = [ctypes.POINTER(args), P]
+        getattr(L, name).restype = ctypes.c_int
+    L.tl_select_pages_workspace_bytes.argtypes = [ctypes.POINTER(SelectPagesArgs)]
+    L.tl_select_pages_workspace_bytes.restype = ctypes.c_uint64
+    L.tl_attend_pages_workspace_bytes.argtypes = [ctypes.POINTER(AttendPagesArgs)]
+    L.tl_attend_pages_workspace_bytes.restype = ctypes.c_uint64
     _lib = L
     return L
 

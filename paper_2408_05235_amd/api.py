@@ -377,6 +377,10 @@ def tl_adjust_lengths(req_offset, generated, pred_len, scale_num, scale_den, max
 _KV_DTYPES = {torch.bfloat16: _lib.BF16, torch.float16: _lib.F16}
 _VIEW_SIZE, _APPEND_SIZE = ctypes.sizeof(_lib.KvView), ctypes.sizeof(_lib.KvAppendArgs)
 _ATTEND_SIZE, _PAGES_SIZE = ctypes.sizeof(_lib.AttendArgs), ctypes.sizeof(_lib.Pages)
+_BOUNDS_SIZE, _SELECT_SIZE = ctypes.sizeof(_lib.PageBoundsArgs), ctypes.sizeof(_lib.SelectPagesArgs)
+_ATTEND_PAGES_SIZE, _NORM_SIZE = ctypes.sizeof(_lib.AttendPagesArgs), ctypes.sizeof(_lib.NormArgs)
+_SAMPLE_SIZE = ctypes.sizeof(_lib.SampleArgs)
+_DTYPES = {torch.bfloat16: _lib.BF16, torch.float16: _lib.F16, torch.float32: _lib.F32}
 
 
 def _strides(t):
@@ -520,6 +524,231 @@ def tl_attend(query, key_pages, value_pages, page_table, length, q_offset=None, 
         a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
     check(L.tl_attend(ref, _stream_on(index)))
     return (out, lse) if want_lse else out
+
+
+def _summaries(bounds, scale, n_pages, heads, dim, device):
+    """The checked summaries' stride between the scales of pages."""
+    if (bounds is None or bounds.get_device() != device or bounds.dtype != torch.int8
+            or bounds.shape != (n_pages, heads, 2, dim) or not bounds.is_contiguous()):
+        _need(bounds, torch.int8, "bounds", (n_pages, heads, 2, dim), device)
+    if (scale is None or scale.get_device() != device or scale.dtype != torch.float32
+            or scale.shape != (n_pages, heads) or heads > 1 and scale.stride(1) != 1):
+        if scale is None or scale.shape != (n_pages, heads) or scale.stride(1) != 1:
+            _need(scale, torch.float32, "scale", (n_pages, heads), device)
+        _need(scale[:1], torch.float32, "scale", None, device)      # its device and type
+    return scale.stride(0) if n_pages > 1 else heads
+
+
+def tl_page_bounds(key_pages, bounds, scale, page_table, length, n_tokens, q_offset=None, granted=None):
+    """The summaries of the pages that the ``n_tokens`` new tokens lie in, in
+    place (tl_page_bounds), after tl_kv_append has written their keys: ``bounds``
+    [n_pages, n_kv_heads, 2, head_dim] int8 and ``scale`` [n_pages, n_kv_heads]
+    fp32 (its rows any distance apart).  The cache, ``q_offset`` and ``granted`` as in
+    tl_kv_append.  No gradients."""
+    if key_pages.requires_grad or scale.requires_grad:
+        _no_gradients("tl_page_bounds")
+    n_tokens, device = int(n_tokens), key_pages.get_device()
+    v = _kv_view(key_pages, key_pages, page_table, length, device)
+    n_pages, heads, _, dim = key_pages.shape
+    stride = _summaries(bounds, scale, n_pages, heads, dim, device)
+    if q_offset is not None:
+        _need(q_offset, torch.int64, "q_offset", (page_table.shape[0] + 1,), device)
+    if n_tokens >> 31:
+        _int32(n_tokens, "n_tokens")
+    a = _lib.PageBoundsArgs(_BOUNDS_SIZE, 0, v, n_tokens, _p(q_offset), bounds.data_ptr(), scale.data_ptr(), stride,
+                            None if granted is None else _granted(granted, page_table.shape[0], device))
+    check(lib().tl_page_bounds(ctypes.byref(a), _stream_on(device)))
+
+
+def tl_select_pages(query, bounds, scale, page_table, length, page_tokens, n_select, q_offset=None, first=1, last=1,
+                    out=None, workspace=None, granted=None):
+    """The ``n_select`` pages that score best for each new token and KV head by
+    their summaries (tl_page_bounds'), of them the ``first`` and the ``last`` ones always
+    (tl_select_pages).  ``query`` [T, n_heads, head_dim]; table, length, ``q_offset``
+    and ``granted`` as in tl_attend.  ``workspace`` is an uint8 tensor (allocated when
+    None).  Returns [T, n_kv_heads, n_select] int32, places in the table's rows,
+    ascending, -1 behind them where a token has fewer.  No gradients: the choice has
+    none (refused where a tensor asks for one)."""
+    if query.requires_grad or scale.requires_grad:
+        _no_gradients("tl_select_pages")
+    page_tokens, n_select, first, last = int(page_tokens), int(n_select), int(first), int(last)
+    if (page_tokens | n_select | first | last) >> 31:
+        for name, x in (("page_tokens", page_tokens), ("n_select", n_select), ("first", first), ("last", last)):
+            _int32(x, name)
+    index = query.get_device()
+    kind = _KV_DTYPES.get(query.dtype)
+    if kind is None:
+        raise ValueError(f"query must be bfloat16 or float16, got {query.dtype}")
+    if index < 0:
+        raise ValueError("query must be a device tensor")
+    if bounds is None or bounds.dim() != 4:
+        raise ValueError("bounds must be [n_pages, n_kv_heads, 2, head_dim]")
+    n_pages, kv_heads, _, dim = bounds.shape
+    qs = _rows3(query, query.dtype, "query", index, None, dim)
+    T, heads, _ = query.shape
+    stride = _summaries(bounds, scale, n_pages, kv_heads, dim, index)
+    if page_table is None or page_table.dim() != 2:
+        raise ValueError("page_table must be [n_seqs, table_width]")
+    n_seqs, width = page_table.shape
+    if page_table.get_device() != index or page_table.dtype != torch.int32 or not page_table.is_contiguous():
+        _need(page_table, torch.int32, "page_table", None, index)
+    if (length is None or length.get_device() != index or length.dtype != torch.int32 or not length.is_contiguous()
+            or length.shape != (n_seqs,)):
+        _need(length, torch.int32, "length", (n_seqs,), index)
+    if q_offset is not None:
+        _need(q_offset, torch.int64, "q_offset", (n_seqs + 1,), index)
+    if out is None:
+        out = torch.empty((T, kv_heads, n_select), dtype=torch.int32, device=query.device)
+    else:
+        _need(out, torch.int32, "out", (T, kv_heads, n_select), index)
+    v = _lib.KvView(_VIEW_SIZE, kind, kv_heads, dim, page_tokens, width, n_pages, n_seqs, 0, 0, 0, None, None,
+                    page_table.data_ptr(), length.data_ptr())
+    a = _lib.SelectPagesArgs(_SELECT_SIZE, heads, v, T, _p(q_offset), query.data_ptr(), qs[0], qs[1], bounds.data_ptr(),
+                             scale.data_ptr(), stride, n_select, first, last, 0, out.data_ptr(), None, 0,
+                             None if granted is None else _granted(granted, n_seqs, index))
+    L, ref = lib(), ctypes.byref(a)
+    if workspace is None:
+        n = L.tl_select_pages_workspace_bytes(ref)
+        if n:
+            workspace = torch.empty(n, dtype=torch.uint8, device=query.device)
+    else:
+        _need(workspace, torch.uint8, "workspace", None, index)
+    if workspace is not None:
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    check(L.tl_select_pages(ref, _stream_on(index)))
+    return out
+
+
+def tl_attend_pages(query, key_pages, value_pages, page_table, length, selected, q_offset=None, scale=None, out=None,
+                    want_lse=False, workspace=None, granted=None):
+    """Attention of the new tokens' queries over the pages that ``selected``
+    [T, n_kv_heads, n_select] int32 (tl_select_pages') names for each of them and KV
+    head (tl_attend_pages).  The rest is as in tl_attend.  For serving: no gradients
+    (refused where a tensor asks for one)."""
+    if (query.requires_grad or key_pages.requires_grad or value_pages.requires_grad
+            or out is not None and out.requires_grad):
+        _no_gradients("tl_attend_pages")
+    index = key_pages.get_device()
+    v = _kv_view(key_pages, value_pages, page_table, length, index)
+    dtype, shape, device = key_pages.dtype, query.shape, query.device
+    qs = _rows3(query, dtype, "query", index, None, key_pages.shape[3])
+    T, heads, dim = shape
+    if (selected is None or selected.get_device() != index or selected.dtype != torch.int32 or selected.dim() != 3
+            or selected.shape[:2] != (T, key_pages.shape[1]) or not selected.is_contiguous()):
+        _need(selected, torch.int32, "selected", None, index)
+        raise ValueError(f"selected must be [{T}, {key_pages.shape[1]}, n_select], got {tuple(selected.shape)}")
+    if q_offset is not None:
+        _need(q_offset, torch.int64, "q_offset", (page_table.shape[0] + 1,), index)
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=device)
+    else:
+        _need(out, dtype, "out", shape, index)
+    lse = torch.empty((T, heads), dtype=torch.float32, device=device) if want_lse else None
+    a = _lib.AttendArgs(_ATTEND_SIZE, heads, v, T, _p(q_offset), query.data_ptr(), qs[0], qs[1],
+                        dim ** -0.5 if scale is None else float(scale), 0, 0, 0, out.data_ptr(), _p(lse), None, 0,
+                        None if granted is None else _granted(granted, page_table.shape[0], index))
+    a = _lib.AttendPagesArgs(_ATTEND_PAGES_SIZE, selected.shape[2], a, selected.data_ptr())
+    L, ref = lib(), ctypes.byref(a)
+    if workspace is None:
+        n = L.tl_attend_pages_workspace_bytes(ref)
+        if n:
+            workspace = torch.empty(n, dtype=torch.uint8, device=device)
+    else:
+        _need(workspace, torch.uint8, "workspace", None, index)
+    if workspace is not None:
+        a.attend.workspace, a.attend.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    check(L.tl_attend_pages(ref, _stream_on(index)))
+    return (out, lse) if want_lse else out
+
+
+def _rows2(t, name, dtype=None, shape=None, device=None):
+    """The stride between the rows of ``t`` [rows, columns]."""
+    if t is None or not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if device is not None and t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, other tensors are on cuda:{device}")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 2 or shape is not None and t.shape != shape:
+        raise ValueError(f"{name} must be " + ("[rows, columns]" if shape is None else f"{tuple(shape)}")
+                         + f", got {tuple(t.shape)}")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return t.stride(0) if rows > 1 else cols
+
+
+def tl_norm(x, weight, eps=1e-6, residual=None, group=None, out=None, sum_out=None):
+    """The norm before a product: h / sqrt(mean h^2 + eps) * weight per row of
+    h = x (+ residual), x [rows, columns] (tl_norm).  Returns y in x's type; with
+    ``group`` (q, scale), y in 8 bits (float8_e4m3fn) with a scale a row (0) or for
+    ``group`` columns (a power of two from 16 to 512).  With ``residual`` the sum h comes
+    last.  ``out`` and ``sum_out`` (contiguous; ``sum_out=residual`` adds in place)
+    take y or q, and h.  No gradients (refused where a tensor asks for one)."""
+    if (x.requires_grad or weight.requires_grad or residual is not None and residual.requires_grad):
+        _no_gradients("tl_norm")
+    dtype, shape, device = x.dtype, x.shape, x.get_device()
+    kind = _DTYPES.get(dtype)
+    if kind is None:
+        raise ValueError(f"x must be bfloat16, float16 or float32, got {dtype}")
+    xs = _rows2(x, "x")
+    rows, cols = shape
+    _need(weight, dtype, "weight", (cols,), device)
+    rs = 0 if residual is None else _rows2(residual, "residual", dtype, shape, device)
+    if group is None:
+        number, kept, scale = _lib.NORM_SAME, dtype, None
+    else:
+        number, kept = int(group), torch.float8_e4m3fn
+        if number < 0 or number >> 31:
+            raise ValueError(f"group {number} is neither 0 nor a power of two from 16 to 512")
+        scale = torch.empty((rows, -(-cols // number)) if number else (rows,), dtype=torch.float32, device=x.device)
+    if out is None:
+        out = torch.empty(shape, dtype=kept, device=x.device)
+    else:
+        _need(out, kept, "out", shape, device)
+    if sum_out is not None:
+        if residual is None:
+            raise ValueError("sum_out needs residual")
+        _need(sum_out, dtype, "sum_out", shape, device)
+    elif residual is not None:
+        sum_out = torch.empty(shape, dtype=dtype, device=x.device)
+    a = _lib.NormArgs(_NORM_SIZE, kind, rows, cols, number, eps, 0, x.data_ptr(), _p(residual), weight.data_ptr(), xs,
+                      rs, out.data_ptr(), _p(scale), _p(sum_out))
+    check(lib().tl_norm(ctypes.byref(a), _stream_on(device)))
+    if group is None:
+        return out if residual is None else (out, sum_out)
+    return (out, scale) if residual is None else (out, scale, sum_out)
+
+
+def tl_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, want_logprob=False, out=None):
+    """The next tokens of rows of logits [rows, tokens], drawn with the numbers
+    ``u`` [rows] fp32 in [0, 1) (tl_sample).  ``temperature``, ``top_p``, ``min_p`` fp32
+    and ``top_k`` int32 are [rows], or None: 1 and no filter.  Returns token [rows]
+    int32, and its log-probability among the kept ones [rows] fp32 too with
+    ``want_logprob``.  No gradients (refused where the logits ask for them)."""
+    if logits.requires_grad:
+        _no_gradients("tl_sample")
+    device, kind = logits.get_device(), _DTYPES.get(logits.dtype)
+    if kind is None:
+        raise ValueError(f"logits must be bfloat16, float16 or float32, got {logits.dtype}")
+    stride = _rows2(logits, "logits")
+    rows, cols = logits.shape
+    row = (rows,)
+    _need(u, torch.float32, "u", row, device)
+    for name, t in (("temperature", temperature), ("top_p", top_p), ("min_p", min_p)):
+        if t is not None:
+            _need(t, torch.float32, name, row, device)
+    if top_k is not None:
+        _need(top_k, torch.int32, "top_k", row, device)
+    if out is None:
+        out = torch.empty(row, dtype=torch.int32, device=logits.device)
+    else:
+        _need(out, torch.int32, "out", row, device)
+    logprob = torch.empty(row, dtype=torch.float32, device=logits.device) if want_logprob else None
+    a = _lib.SampleArgs(_SAMPLE_SIZE, kind, rows, cols, 0, logits.data_ptr(), stride, u.data_ptr(), _p(temperature),
+                        _p(top_k), _p(top_p), _p(min_p), out.data_ptr(), _p(logprob))
+    check(lib().tl_sample(ctypes.byref(a), _stream_on(device)))
+    return (out, logprob) if want_logprob else out
 
 
 def _pages(ref, page_table, length, page_tokens, granted=None):
@@ -716,6 +945,11 @@ admit = tl_admit
 adjust_lengths = tl_adjust_lengths
 kv_append = tl_kv_append
 attend = tl_attend
+page_bounds = tl_page_bounds
+select_pages = tl_select_pages
+attend_pages = tl_attend_pages
+norm = tl_norm
+sample = tl_sample
 
 
 def upload(inp, device="cuda"):

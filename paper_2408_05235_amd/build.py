@@ -16,9 +16,10 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_DIR = os.path.join(PKG, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "libtl.so")
 SOURCES = ["api.cpp", "host_forest.cpp", "project.hip", "forest.hip", "column.hip", "small.hip", "lattice.hip", "select.hip",
-           "cache_api.cpp", "pages.hip", "attend.hip", "attend_tiles.hip"]
+           "cache_api.cpp", "pages.hip", "attend.hip", "attend_tiles.hip", "summary.hip", "attend_pages.hip",
+           "step_api.cpp", "norm.hip", "sample.hip"]
 HEADERS = ["device_util.h", "tl_internal.h", "forest_walk.h", "record_format.h", "host_forest.h", "queue_tries.h",
-           "scratch.h", "status.h", "cache.h", "cache_rows.h", "attend_common.h", "attend_few.h"]
+           "scratch.h", "status.h", "cache.h", "cache_rows.h", "attend_common.h", "attend_few.h", "step.h"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

@@ -47,6 +47,36 @@ struct AttendParams {
     uint64_t workspace_bytes;
 };
 
+struct BoundsParams {
+    CacheView c;                    // (without values)
+    bool f16;
+    int8_t* bounds;
+    float* scale;
+    int64_t scale_stride;
+    int64_t slots;                  // places of touched pages, gaps included
+};
+
+struct SelectPagesParams {
+    CacheView c;                    // (without keys and values)
+    bool f16;
+    int32_t group;                  // query heads per KV head
+    const uint16_t* query;
+    int64_t query_token_stride, query_head_stride;
+    const int8_t* bounds;
+    const float* scale;
+    int64_t scale_stride;
+    int32_t n_select, first, last;
+    int32_t* selected;
+    void* workspace;
+    uint64_t workspace_bytes;
+};
+
+struct AttendPagesParams {
+    AttendParams a;
+    const int32_t* selected;
+    int32_t n_select;
+};
+
 struct PagesParams {
     int32_t page_tokens, table_width;
     int64_t n_pages, n_slots;
@@ -70,6 +100,14 @@ hipError_t launch_append(const AppendParams& p, hipStream_t stream);
 hipError_t launch_attend(const AttendParams& p, hipStream_t stream);
 // Workspace bytes that launch_attend splits its work with.
 uint64_t attend_workspace_bytes(const AttendParams& p);
+
+hipError_t launch_page_bounds(const BoundsParams& p, hipStream_t stream);
+hipError_t launch_select_pages(const SelectPagesParams& p, hipStream_t stream);
+// Workspace bytes that a call needs at least, and can use.
+uint64_t select_workspace_least(const SelectPagesParams& p);
+uint64_t select_workspace_bytes(const SelectPagesParams& p);
+hipError_t launch_attend_pages(const AttendPagesParams& p, hipStream_t stream);
+uint64_t attend_pages_workspace_bytes(const AttendPagesParams& p);
 
 // int32 words of `work` of the page calls.
 uint64_t pages_work_words(const PagesParams& p);

@@ -26,8 +26,9 @@ constexpr size_t kPagesSize = offsetof(tl_pages, granted);
 
 // Checks of a cache view and the packed rows that go with it, and their
 // translation; `who` prefixes messages.
+enum { kNoPages, kKeys, kKeysAndValues };       // what a call uses of a cache's pages
 tl_status view_params(const tl_kv_view* v, int64_t n_tokens, const int64_t* q_offset, const char* who,
-                      tl::CacheView* c) {
+                      tl::CacheView* c, int uses = kKeysAndValues) {
     if (v->struct_size < sizeof(tl_kv_view))
         return fail(TL_EINVAL, "%s: cache.struct_size %u < %zu", who, v->struct_size, sizeof(tl_kv_view));
     if (v->dtype != TL_BF16 && v->dtype != TL_F16)
@@ -54,7 +55,8 @@ tl_status view_params(const tl_kv_view* v, int64_t n_tokens, const int64_t* q_of
     if (n_tokens > 0 && v->n_seqs > 0) {
         if (!v->length || (v->table_width > 0 && !v->page_table))
             return fail(TL_EINVAL, "%s: NULL required pointer", who);
-        if (v->n_pages > 0 && (!v->key_pages || !v->value_pages)) return fail(TL_EINVAL, "%s: NULL pages", who);
+        if (v->n_pages > 0 && ((uses >= kKeys && !v->key_pages) || (uses >= kKeysAndValues && !v->value_pages)))
+            return fail(TL_EINVAL, "%s: NULL pages", who);
     }
     if (!aligned16(v->key_pages) || !aligned16(v->value_pages))
         return fail(TL_EINVAL, "%s: pages must be 16-byte aligned", who);
@@ -75,6 +77,74 @@ tl_status view_params(const tl_kv_view* v, int64_t n_tokens, const int64_t* q_of
     c->length = v->length;
     c->n_tokens = n_tokens;
     c->q_offset = q_offset;
+    return TL_OK;
+}
+
+// Query heads, their strides and their number of rows.
+tl_status query_params(const tl_kv_view* v, int64_t n_tokens, int32_t n_heads, const void* query, int64_t token_stride,
+                       int64_t head_stride, const char* who) {
+    if (n_heads < 1 || n_heads % v->n_kv_heads != 0)
+        return fail(TL_EINVAL, "%s: n_heads %d is not a positive multiple of n_kv_heads %d", who, n_heads, v->n_kv_heads);
+    if (token_stride < 0 || head_stride < 0 || token_stride % 8 != 0 || head_stride % 8 != 0)
+        return fail(TL_EINVAL, "%s: query strides must be non-negative multiples of 8 elements", who);
+    if (n_tokens > 0 && !query) return fail(TL_EINVAL, "%s: NULL required pointer", who);
+    if (!aligned16(query)) return fail(TL_EINVAL, "%s: query must be 16-byte aligned", who);
+    if ((int64_t)n_heads * n_tokens > kMaxCount)
+        return fail(TL_EUNSUPPORTED, "%s: n_tokens x n_heads beyond 2^31-1", who);
+    return TL_OK;
+}
+
+tl_status selected_params(int32_t n_select, const char* who) {
+    if (n_select < 1) return fail(TL_EINVAL, "%s: n_select %d < 1", who, n_select);
+    if (n_select > TL_MAX_SELECTED)
+        return fail(TL_EUNSUPPORTED, "%s: n_select %d beyond %d", who, n_select, TL_MAX_SELECTED);
+    return TL_OK;
+}
+
+// How the summaries lie.
+tl_status summary_params(const tl_kv_view* v, int64_t n_tokens, const void* bounds, const void* scale,
+                         int64_t scale_stride, const char* who) {
+    if (v->n_pages > 0 && n_tokens > 0 && v->n_seqs > 0 && (!bounds || !scale))
+        return fail(TL_EINVAL, "%s: NULL required pointer", who);
+    if (!aligned16(bounds)) return fail(TL_EINVAL, "%s: bounds must be 16-byte aligned", who);
+    if (scale_stride < 0) return fail(TL_EINVAL, "%s: scale_stride %lld < 0", who, (long long)scale_stride);
+    return TL_OK;
+}
+
+tl_status select_params(const tl_select_pages_args* a, const char* who, tl::SelectPagesParams* p) {
+    if (a->struct_size < sizeof(tl_select_pages_args))
+        return fail(TL_EINVAL, "%s: struct_size %u < %zu", who, a->struct_size, sizeof(tl_select_pages_args));
+    *p = tl::SelectPagesParams{};
+    tl_status st = view_params(&a->cache, a->n_tokens, a->q_offset, who, &p->c, kNoPages);
+    if (st == TL_OK)
+        st = query_params(&a->cache, a->n_tokens, a->n_heads, a->query, a->query_token_stride, a->query_head_stride, who);
+    if (st == TL_OK) st = selected_params(a->n_select, who);
+    if (st == TL_OK) st = summary_params(&a->cache, a->n_tokens, a->bounds, a->scale, a->scale_stride, who);
+    if (st != TL_OK) return st;
+    if (a->first < 0 || a->last < 0 || (int64_t)a->first + a->last > a->n_select)
+        return fail(TL_EINVAL, "%s: first %d and last %d are not at least 0 and together at most n_select %d", who,
+                    a->first, a->last, a->n_select);
+    p->group = a->n_heads / a->cache.n_kv_heads;
+    if (p->group > TL_MAX_GROUP)
+        return fail(TL_EUNSUPPORTED, "%s: %d query heads per KV head, beyond %d", who, p->group, TL_MAX_GROUP);
+    if (a->n_tokens > 0 && !a->selected) return fail(TL_EINVAL, "%s: NULL required pointer", who);
+    if (!aligned16(a->workspace)) return fail(TL_EINVAL, "%s: workspace must be 16-byte aligned", who);
+    p->f16 = a->cache.dtype == TL_F16;
+    p->query = (const uint16_t*)a->query;
+    p->query_token_stride = a->query_token_stride;
+    p->query_head_stride = a->query_head_stride;
+    p->bounds = a->bounds;
+    p->scale = a->scale;
+    p->scale_stride = a->scale_stride;
+    p->n_select = a->n_select;
+    p->first = a->first;
+    p->last = a->last;
+    p->selected = a->selected;
+    p->workspace = a->workspace;
+    p->workspace_bytes = a->workspace ? a->workspace_bytes : 0;
+    p->c.granted = a->granted;
+    p->c.refused_only = true;
+    if (p->c.n_pages == 0) p->c.table_width = 0;    // nothing is in the cache
     return TL_OK;
 }
 
@@ -116,6 +186,20 @@ tl_status attend_params(const tl_attend_args* a, const char* who, tl::AttendPara
     p->c.granted = a->struct_size >= sizeof(tl_attend_args) ? a->granted : nullptr;
     p->c.refused_only = true;
     if (p->c.n_pages == 0) p->c.table_width = 0;    // nothing is in the cache
+    return TL_OK;
+}
+
+tl_status attend_pages_params(const tl_attend_pages_args* a, const char* who, tl::AttendPagesParams* p) {
+    if (a->struct_size < sizeof(tl_attend_pages_args))
+        return fail(TL_EINVAL, "%s: struct_size %u < %zu", who, a->struct_size, sizeof(tl_attend_pages_args));
+    tl_status st = attend_params(&a->attend, who, &p->a);
+    if (st == TL_OK) st = selected_params(a->n_select, who);
+    if (st != TL_OK) return st;
+    if (a->attend.window != 0 || a->attend.sinks != 0)
+        return fail(TL_EINVAL, "%s: window and sinks must be 0 (the lists say what is seen)", who);
+    if (a->attend.n_tokens > 0 && !a->selected) return fail(TL_EINVAL, "%s: NULL required pointer", who);
+    p->selected = a->selected;
+    p->n_select = a->n_select;
     return TL_OK;
 }
 
@@ -194,6 +278,58 @@ uint64_t tl_attend_workspace_bytes(const tl_attend_args* a) {
     tl::AttendParams p;
     if (!a || attend_params(a, "tl_attend_workspace_bytes", &p) != TL_OK) return 0;
     return tl::attend_workspace_bytes(p);
+}
+
+tl_status tl_page_bounds(const tl_page_bounds_args* a, void* stream) {
+    const char* const who = "tl_page_bounds";
+    if (!a) return fail(TL_EINVAL, "%s: args is NULL", who);
+    if (a->struct_size < sizeof(tl_page_bounds_args))
+        return fail(TL_EINVAL, "%s: struct_size %u < %zu", who, a->struct_size, sizeof(tl_page_bounds_args));
+    tl::BoundsParams p{};
+    tl_status st = view_params(&a->cache, a->n_tokens, a->q_offset, who, &p.c, kKeys);
+    if (st == TL_OK) st = summary_params(&a->cache, a->n_tokens, a->bounds, a->scale, a->scale_stride, who);
+    if (st != TL_OK) return st;
+    p.f16 = a->cache.dtype == TL_F16;
+    p.bounds = a->bounds;
+    p.scale = a->scale;
+    p.scale_stride = a->scale_stride;
+    p.c.granted = a->granted;
+    if (a->n_tokens == 0 || p.c.n_seqs == 0 || p.c.n_pages == 0 || p.c.table_width == 0) return ok();
+    return from_hip(tl::launch_page_bounds(p, (hipStream_t)stream), "tl_page_bounds: launch");
+}
+
+tl_status tl_select_pages(const tl_select_pages_args* a, void* stream) {
+    const char* const who = "tl_select_pages";
+    if (!a) return fail(TL_EINVAL, "%s: args is NULL", who);
+    tl::SelectPagesParams p;
+    const tl_status st = select_params(a, who, &p);
+    if (st != TL_OK) return st;
+    if (a->n_tokens == 0 || p.c.n_seqs == 0) return ok();
+    if (p.workspace_bytes < tl::select_workspace_least(p))
+        return fail(TL_EINVAL, "%s: workspace of %llu bytes, needs at least %llu", who,
+                    (unsigned long long)p.workspace_bytes, (unsigned long long)tl::select_workspace_least(p));
+    return from_hip(tl::launch_select_pages(p, (hipStream_t)stream), "tl_select_pages: launch");
+}
+
+uint64_t tl_select_pages_workspace_bytes(const tl_select_pages_args* a) {
+    tl::SelectPagesParams p;
+    if (!a || select_params(a, "tl_select_pages_workspace_bytes", &p) != TL_OK) return 0;
+    return tl::select_workspace_bytes(p);
+}
+
+tl_status tl_attend_pages(const tl_attend_pages_args* a, void* stream) {
+    if (!a) return fail(TL_EINVAL, "tl_attend_pages: args is NULL");
+    tl::AttendPagesParams p;
+    const tl_status st = attend_pages_params(a, "tl_attend_pages", &p);
+    if (st != TL_OK) return st;
+    if (p.a.c.n_tokens == 0 || p.a.c.n_seqs == 0) return ok();
+    return from_hip(tl::launch_attend_pages(p, (hipStream_t)stream), "tl_attend_pages: launch");
+}
+
+uint64_t tl_attend_pages_workspace_bytes(const tl_attend_pages_args* a) {
+    tl::AttendPagesParams p;
+    if (!a || attend_pages_params(a, "tl_attend_pages_workspace_bytes", &p) != TL_OK) return 0;
+    return tl::attend_pages_workspace_bytes(p);
 }
 
 uint64_t tl_pages_work_words(const tl_pages* g) {

@@ -1,0 +1,163 @@
+"""The norm before a product (tl_norm) against 64 bits."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+EPS = 1e-5
+
+
+def inputs(seed, rows, cols, dtype, residual, spread=1.0):
+    g = torch.Generator().manual_seed(seed)
+    dt = DTYPES[dtype]
+    r = lambda *s: (torch.randn(*s, generator=g) * spread)
+    x, w = r(rows, cols), 1 + 0.2 * torch.randn(cols, generator=g)
+    x[:, ::7] *= 9
+    return (x.to(dt).cuda(), w.to(dt).cuda(), r(rows, cols).to(dt).cuda() if residual else None)
+
+
+def exact(x, w, res, eps=EPS):
+    h = x.double() + (0 if res is None else res.double())
+    return h, h / torch.sqrt((h * h).mean(1, keepdim=True) + eps) * w.double()
+
+
+def check(got, x, w, res, group, eps=EPS):
+    """Half a step of the output's type (a step is finfo.eps of the value at
+    most); before it fp32: the sum of squares in chains of at most 8 + W / 8192 + 32
+    + 22 additions, whose error the root halves, x + r, the root, the quotient and
+    two products, each 2^-24.  In e4m3 half a step is 2^-4 of the value, or 2^-10 of
+    a scale where that is more (below 2^-6 the steps are 2^-9), and the quotient by
+    the scale adds two roundings."""
+    dt, W = x.dtype, x.shape[1]
+    got = list(got) if isinstance(got, tuple) else [got]
+    h, y = exact(x, w, res, eps)
+    rough = 2.0 ** -24 * (64 + W / 8192 + 8)
+    tiny = 2.0 ** -25 if dt == torch.float16 else 1e-40      # half a step of the least numbers
+    close = lambda a, b, t: bool(((a.double() - b).abs() <= t).all())
+    rough_y = y.abs() * rough
+    if res is not None:
+        s = got.pop()
+        assert s.dtype == dt and close(s, h, h.abs() * (torch.finfo(dt).eps / 2 + 2.0 ** -23) + tiny)
+    if group is None:
+        assert got[0].dtype == dt
+        assert close(got[0], y, y.abs() * torch.finfo(dt).eps / 2 + rough_y + tiny)
+        return
+    q, scale = got
+    assert q.dtype == torch.float8_e4m3fn and scale.dtype == torch.float32
+    per = group or W
+    n = -(-W // per)
+    most = torch.nn.functional.pad(y.abs(), (0, n * per - W)).view(-1, n, per).amax(2)
+    want = (most / 448).clamp(min=2.0 ** -100)
+    got_scale = scale.view(-1, n).double()
+    assert bool(((got_scale - want).abs() <= want * (rough + 2.0 ** -22)).all())
+    s = got_scale.repeat_interleave(per, 1)[:, :W]
+    back = q.double() * s
+    assert close(back, y, y.abs() * (2.0 ** -4 + 2.0 ** -20) + s * 2.0 ** -10 + rough_y)
+
+
+SIZES = [(1, 1), (3, 7), (2, 8), (5, 63), (64, 512), (4, 520), (3, 1000), (9, 1024), (2, 1030), (7, 2048), (3, 4096),
+         (2, 5000), (5, 8192), (2, 8200), (3, 16384), (1, 20001), (2, 32768), (2, 32770), (1, 100003)]
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("rows,cols", SIZES)
+def test_sizes(gpu, rows, cols, dtype):
+    from paper_2408_05235_amd import api
+    for residual in (False, True):
+        x, w, res = inputs(rows * cols, rows, cols, dtype, residual)
+        for group in (None, 0, 16, 64, 512):
+            print(f"norm {rows} x {cols} {dtype} residual {residual} group {group}", flush=True)
+            check(api.tl_norm(x, w, EPS, res, group), x, w, res, group)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("cols", [33, 640, 40000])
+def test_rows_anywhere_and_in_place(gpu, cols, dtype):
+    from paper_2408_05235_amd import api
+    x, w, res = inputs(5, 6, cols + 3, dtype, True)
+    xs, rs, ws = x[::2, 1:cols + 1], res[::2, 3:], w[2:cols + 2]
+    for group in (None, 0, 32):
+        check(api.tl_norm(xs, ws.contiguous(), EPS, rs, group), xs, ws, rs, group)
+    # one row for all
+    check(api.tl_norm(x[:1].expand(4, -1), w, EPS, res[:4], 0), x[:1].expand(4, -1), w, res[:4], 0)
+    # out and the sum in the inputs' place
+    want = api.tl_norm(x, w, EPS, res)
+    for group in (None, 0, 128):
+        a, b = x.clone(), res.clone()
+        want = api.tl_norm(x, w, EPS, res, group)
+        got = api.tl_norm(a, w, EPS, b, group, out=a if group is None else None, sum_out=b)
+        assert got[-1].data_ptr() == b.data_ptr()
+        for p, q in zip(got, want):
+            assert torch.equal(p.view(torch.uint8), q.view(torch.uint8))
+    want = api.tl_norm(x, w, EPS)
+    a = x.clone()
+    assert torch.equal(api.tl_norm(a, w, EPS, out=a), want)
+
+
+@pytest.mark.parametrize("cols", [100, 40000])
+def test_zeros_infinities_and_nan(gpu, cols):
+    from paper_2408_05235_amd import api
+    for dtype in DTYPES:
+        x, w, _ = inputs(1, 6, cols, dtype, False)
+        x[0] = 0
+        x[1, 17] = math.nan
+        x[2, 99] = math.inf
+        x[3] = 0
+        x[3, 5] = 1e-4
+        for group in (None, 0, 64):
+            got = api.tl_norm(x, w, EPS, None, group)
+            y = got if group is None else got[0].float()
+            assert bool((y[0] == 0).all())
+            assert bool(torch.isnan(y[1]).all())
+            assert bool(torch.isnan(y[2, 99]))
+            if group is None:
+                assert bool((y[2, :99] == 0).all())
+            if group == 0:
+                assert got[1][0] == 2.0 ** -100 and bool(torch.isnan(got[1][1:3]).all())
+            if group == 64:     # the group that holds the infinity, and no other
+                n = torch.isnan(got[1][2])
+                assert bool(n[1]) and int(n.sum()) == 1 and bool((y[2, :64] == 0).all())
+                assert bool((got[1][0] == 2.0 ** -100).all())
+        keep = [4, 5] + [3]
+        for group in (None, 0, 64):
+            got = api.tl_norm(x[keep], w, EPS, None, group)
+            check(got, x[keep], w, None, group)
+    # a zero row without eps: 0 x inf, as the formula has it
+    x = torch.zeros(1, 8, device="cuda")
+    assert bool(torch.isnan(api.tl_norm(x, torch.ones(8, device="cuda"), 0.0)).all())
+
+
+def test_many_rows_and_none(gpu):
+    from paper_2408_05235_amd import api
+    x, w, _ = inputs(2, 70001, 24, "bf16", False)
+    check(api.tl_norm(x, w, EPS, None, 16), x, w, None, 16)
+    q, s = api.tl_norm(x[:0], w, EPS, None, 16)
+    assert q.shape == (0, 24) and s.shape == (0, 2)
+
+
+def test_streams_and_replays(gpu):
+    """On another stream, and in a graph that is replayed with eager work
+    between its replays."""
+    from paper_2408_05235_amd import api
+    x, w, res = inputs(3, 64, 4096, "bf16", True)
+    want = [t.view(torch.uint8).clone() for t in api.tl_norm(x, w, EPS, res, 128)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = api.tl_norm(x, w, EPS, res, 128)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a.view(torch.uint8), b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = api.tl_norm(x, w, EPS, res, 128)
+    for seed in (4, 5, 6):
+        a, _, b = inputs(seed, 64, 4096, "bf16", True)
+        x.copy_(a)
+        res.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = api.tl_norm(x, w, EPS, res, 128)
+        assert all(torch.equal(p.view(torch.uint8), q.view(torch.uint8)) for p, q in zip(out, eager))
