@@ -870,18 +870,24 @@ class KVCache:
     pages of ``page_tokens`` tokens, the page table, the lengths and the pages'
     counts, all on the device.  One iteration of an engine extends the slots
     by their new tokens, then appends and attends in every layer; finished
-    sequences are freed.  Where the pool has no room for a slot, nothing of what
+    sequences are freed.  With ``summaries`` append keeps those of the pages up
+    to date too, which select looks for the pages in that attend_pages then reads.  Where the pool has no room for a slot, nothing of what
     the others do depends on it, and its cached tokens stay as they are.  Nothing here
     waits for the device."""
 
     def __init__(self, n_layers, n_pages, n_kv_heads, page_tokens, head_dim, n_slots, max_tokens,
-                 dtype=torch.bfloat16, device="cuda"):
+                 dtype=torch.bfloat16, device="cuda", summaries=False):
         if dtype not in _KV_DTYPES:
             raise ValueError(f"dtype must be bfloat16 or float16, got {dtype}")
         self.page_tokens, self.max_tokens = int(page_tokens), int(max_tokens)
         width = -(-self.max_tokens // self.page_tokens)
         i32 = dict(dtype=torch.int32, device=device)
         self.pages = torch.empty((n_layers, 2, n_pages, n_kv_heads, page_tokens, head_dim), dtype=dtype, device=device)
+        self.bounds = self.scales = None
+        if summaries:
+            self.bounds = torch.zeros((n_layers, n_pages, n_kv_heads, 2, head_dim), dtype=torch.int8, device=device)
+            # (whole 16 bytes a page, which tl_pages_copy moves)
+            self.scales = torch.zeros((n_layers, n_pages, 1, 1, -(-n_kv_heads // 4) * 4), device=device)
         self.ref = torch.zeros(n_pages, **i32)
         self.page_table = torch.full((n_slots, width), -1, **i32)
         self.length = torch.zeros(n_slots, **i32)
@@ -906,6 +912,26 @@ class KVCache:
         and without ``q_offset`` those that asked for none) are left as they are."""
         k, v = self.pages[layer]
         tl_kv_append(key, value, k, v, self.page_table, self.length, q_offset, self.granted)
+        if self.bounds is not None:
+            bounds, scale = self._summaries(layer)
+            tl_page_bounds(k, bounds, scale, self.page_table, self.length, key.shape[0], q_offset, self.granted)
+
+    def _summaries(self, layer):
+        if self.bounds is None:
+            raise ValueError("the cache was made without summaries")
+        return self.bounds[layer], self.scales[layer, :, 0, 0, :self.bounds.shape[2]]
+
+    def select(self, layer, query, n_select, q_offset=None, **kw):
+        """The pages of one layer that score best for the new tokens (after
+        append; tl_select_pages)."""
+        bounds, scale = self._summaries(layer)
+        return tl_select_pages(query, bounds, scale, self.page_table, self.length, self.page_tokens, n_select, q_offset,
+                               granted=self.granted, **kw)
+
+    def attend_pages(self, layer, query, selected, q_offset=None, **kw):
+        """The new tokens' attention over the selected pages of one layer."""
+        k, v = self.pages[layer]
+        return tl_attend_pages(query, k, v, self.page_table, self.length, selected, q_offset, granted=self.granted, **kw)
 
     def attend(self, layer, query, q_offset=None, **kw):
         """The new tokens' attention over one layer (after append); zeros for
@@ -915,7 +941,8 @@ class KVCache:
 
     def fork(self, parent, child):
         """Empty slots ``child`` become copies of ``parent``; returns the
-        statuses."""
+        statuses.  (The summary of a copied page is made with the child's first new
+        token, which lies in it.)"""
         src, dst, status = tl_pages_fork(*self._state(), parent, child, self.page_tokens, self.work, self.granted)
         tl_pages_copy(self.pages, src, dst)
         return status
@@ -929,7 +956,9 @@ class KVCache:
         pages moved (int32 [1], on the device)."""
         r = tl_pages_compact(*self._state(), self.page_tokens, dict(ref=self.ref, page_table=self.page_table),
                              self.work)
-        tl_pages_copy(self.pages, r["copy_src"], r["copy_dst"], r["n_copies"])
+        for pages in (self.pages, self.bounds, self.scales):
+            if pages is not None:
+                tl_pages_copy(pages, r["copy_src"], r["copy_dst"], r["n_copies"])
         return r["n_copies"]
 
     def pages_used(self):
