@@ -83,12 +83,18 @@ __device__ __forceinline__ int32_t build_list(const PagesLaunch& L, int64_t b, i
             const int bit = __builtin_ctz(left);
             uint32_t who = 0;
             for (int32_t s = 0; s < many; ++s) who |= (bits[s * words + k] >> bit & 1) << s;
-            const int32_t j = w0 + k * 32 + bit, page = c.table[b * c.table_width + j];
-            if (at < L.list) list[at] = Entry{page >= 0 && page < c.n_pages ? page : -1, j, who};
+            if (at < L.list) list[at] = Entry{-1, w0 + k * 32 + bit, who};
         }
         __syncthreads();
     }
-    return min(n, L.list);
+    n = min(n, L.list);
+    // (the table by all lanes: not one behind the other)
+    for (int32_t k = threadIdx.x; k < n; k += kPagesThreads) {
+        const int32_t page = c.table[b * c.table_width + list[k].index];
+        list[k].page = page >= 0 && page < c.n_pages ? page : -1;
+    }
+    __syncthreads();
+    return n;
 }
 
 // Token u of the list: where it lies (-1: nowhere), its position and who names it.
@@ -198,7 +204,6 @@ __global__ __launch_bounds__(kPagesThreads, DP > 128 ? 1 : 3) void attend_pages_
 #pragma unroll
     for (int j = 0; j < kPer; ++j) acc[j] = f32x4{0, 0, 0, 0};
     float m = kNone, l = 0.0f;
-    bool special = false;
     u32x4 q[kSteps];
 #pragma unroll
     for (int k = 0; k < kSteps; ++k) {
@@ -279,20 +284,13 @@ __global__ __launch_bounds__(kPagesThreads, DP > 128 ? 1 : 3) void attend_pages_
                     for (int i = 0; i < 4; ++i)
                         if (!(sees >> (16 * h + 4 * g + i) & 1)) sc[h][i] = -INFINITY;
                 // values that no row sees are not used, whatever they are
+                if (any != ~0u)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    if (!(any >> (16 * (e / 4) + 4 * g + e % 4) & 1))
+                    for (int e = 0; e < 8; ++e) {
+                        if (!(any >> (16 * (e / 4) + 4 * g + e % 4) & 1))
 #pragma unroll
-                        for (int y = 0; y < kPer / 2; ++y) w[e][y] = 0;
-                }
-                if (any & ~all) {
-                    // values that some rows see and others do not: one that is
-                    // not finite would reach the others as 0 x value
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-#pragma unroll
-                        for (int y = 0; y < kPer / 2; ++y) special |= not_finite2<F16>(w[e][y]);
-                }
+                            for (int y = 0; y < kPer / 2; ++y) w[e][y] = 0;
+                    }
             }
             // the softmax's step: lanes n, n + 16, n + 32 and n + 48 hold row n
             float top = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
@@ -331,8 +329,15 @@ __global__ __launch_bounds__(kPagesThreads, DP > 128 ? 1 : 3) void attend_pages_
         for (int j = 0; j < kPer; ++j) acc[j] *= kBack;
     }
 
-    // Rows whose values hold what is not finite and is not everybody's: one by
-    // one, a wavefront takes every fourth.
+    // Values that some rows see and others do not reach the others as 0 x value,
+    // which is NaN where they are not finite.  Where sums are, the rows are computed one
+    // by one instead, a wavefront takes every fourth.
+    bool special = false;
+    if (L.slots > 1)
+#pragma unroll
+        for (int j = 0; j < kPer; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) special |= !__builtin_isfinite(acc[j][i]);
     RowSums alone[kFewRows / WAVES];
     const bool one_by_one = __syncthreads_or(special);
     if (one_by_one) {

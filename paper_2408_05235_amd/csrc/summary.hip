@@ -53,7 +53,7 @@ __device__ __forceinline__ uint32_t pack_bytes(const float (&x)[8], int from) {
 
 // A wavefront per slot and KV head: `lanes` lanes (a power of two of at least
 // head_dim / 8) take 8 elements each of a token, the others other tokens.
-template <bool F16>
+template <bool F16, int BATCH>
 __global__ __launch_bounds__(kBoundsThreads) void bounds_kernel(BoundsParams P, int lanes, int64_t first) {
     const CacheView& c = P.c;
     const int64_t item = (blockIdx.x + first) * kBoundsWaves + threadIdx.x / kWave;
@@ -79,18 +79,23 @@ __global__ __launch_bounds__(kBoundsThreads) void bounds_kernel(BoundsParams P, 
     for (int i = 0; i < 8; ++i) hi[i] = -INFINITY, lo[i] = INFINITY;
     bool special = false;
     if (in) {
-#pragma unroll 4
-        for (int r = sub; r < count; r += per) {
-            const u32x4 v = *(const u32x4*)(keys + (int64_t)r * c.token_stride);
+        // (the last token again in the place of those behind it, which changes nothing)
+        for (int r0 = sub; r0 < count; r0 += BATCH * per) {
+            u32x4 v[BATCH];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                special |= not_finite2<F16>(v[i]);
-                const float a = to_float<F16>((uint16_t)v[i]), z = to_float<F16>((uint16_t)(v[i] >> 16));
-                hi[2 * i] = fmaxf(hi[2 * i], a);
-                lo[2 * i] = fminf(lo[2 * i], a);
-                hi[2 * i + 1] = fmaxf(hi[2 * i + 1], z);
-                lo[2 * i + 1] = fminf(lo[2 * i + 1], z);
-            }
+            for (int y = 0; y < BATCH; ++y)
+                v[y] = *(const u32x4*)(keys + (int64_t)min(r0 + y * per, count - 1) * c.token_stride);
+#pragma unroll
+            for (int y = 0; y < BATCH; ++y)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    special |= not_finite2<F16>(v[y][i]);
+                    const float a = to_float<F16>((uint16_t)v[y][i]), z = to_float<F16>((uint16_t)(v[y][i] >> 16));
+                    hi[2 * i] = fmaxf(hi[2 * i], a);
+                    lo[2 * i] = fminf(lo[2 * i], a);
+                    hi[2 * i + 1] = fmaxf(hi[2 * i + 1], z);
+                    lo[2 * i + 1] = fminf(lo[2 * i + 1], z);
+                }
         }
     }
     for (int o = lanes; o < kWave; o <<= 1)
@@ -135,14 +140,15 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 
 constexpr int kScoreWaves = 4, kScoreThreads = kScoreWaves * kWave;
 
-// A workgroup scores a range of pages for a tile of rows of one KV head.  A tile
-// is `slots` tokens of `per` rows each (query heads of the KV head; per: the next
-// power of two of them), or a token's heads in `tiles` times 16 rows.  Lane (n =
+// A workgroup scores a range of pages for rows of one KV head, 16 rows (query heads)
+// a tile: `tiles` tiles of `slots` tokens of `per` rows each (the next power of two of
+// the heads that share the KV head), or the more than 16 heads of one token.  Lane (n =
 // lane % 16, g = lane / 16) holds the bytes 64 k + 16 g .. of row n and of page n (K =
 // 64 bytes a matrix instruction), and of the result the rows 4 g .. 4 g + 3 of page n.
 struct ScoreLaunch {
     SelectPagesParams s;
-    int32_t per, slots, tiles;
+    int32_t per, per_bits, slots, tiles;    // per = 1 << per_bits
+    int32_t tokens_of;      // tokens of a workgroup: slots x tiles, or 1
     int32_t span;           // pages of a workgroup
     int32_t spans;          // workgroups of a row tile
     int64_t token0, tokens; // the tokens of this launch
@@ -154,8 +160,14 @@ struct ScoreLaunch {
 template <int STEPS>
 constexpr int kRowBytes = STEPS * 64 + 16;
 
-template <bool F16, int STEPS>
+// Pages that a wavefront has on their way at once: 16 KB of them.
+template <int STEPS>
+constexpr int kPagesOfStep = STEPS > 4 ? 32 : 64;
+
+// V: values that a lane keeps of a tile's column (4 of 1 row each, 2 of 2, else 1).
+template <bool F16, int STEPS, int V>
 __global__ __launch_bounds__(kScoreThreads) void score_kernel(ScoreLaunch F, int64_t first) {
+    constexpr int kSub = kPagesOfStep<STEPS> / 16, kStep = kPagesOfStep<STEPS>;
     extern __shared__ __attribute__((aligned(16))) unsigned char rows_lds[];
     const SelectPagesParams& P = F.s;
     const CacheView& c = P.c;
@@ -166,131 +178,192 @@ __global__ __launch_bounds__(kScoreThreads) void score_kernel(ScoreLaunch F, int
     const int32_t span = (int32_t)(x % F.spans);
     x /= F.spans;
     const int32_t kvh = (int32_t)(x % c.n_kv_heads);
-    const int64_t t0 = x / c.n_kv_heads * F.slots;          // of this launch
+    const int64_t t0 = x / c.n_kv_heads * F.tokens_of;      // of this launch
+    const bool one = P.group > 16;                          // one token's heads
 
-    // the rows in 127ths of their largest value
-    for (int row = wave; row < n_rows; row += kScoreWaves) {
-        const int32_t slot = F.tiles > 1 ? 0 : row / F.per, head = F.tiles > 1 ? row : row % F.per;
-        const bool real = slot < F.slots && t0 + slot < F.tokens && head < P.group;
-        const int d = lane * 8;
-        float q[8] = {};
-        bool special = false;
+    // A run of the tokens from s0 on that are one sequence's: up to s_end, the
+    // first at position pos0, and the pages of this workgroup that the last one sees
+    // (s_end = s0: the token is nobody's).
+    struct Run {
+        int32_t s_end, p_end;
+        int64_t pos0;
+        const int32_t* table_row;
+    };
+    auto run_from = [&](int32_t s0) {
+        const int64_t i0 = F.token0 + t0 + s0;
+        int64_t b;
+        const bool of_one = find_seq(c, i0, &b);
+        const SeqRows s = of_one ? seq_rows(c, b) : SeqRows{};
+        Run r = {s0, 0, 0, nullptr};
+        if (!of_one || i0 < s.first || i0 - s.first >= s.n) return r;
+        const int32_t many = (int32_t)min(min((int64_t)(F.tokens_of - s0), s.first + s.n - i0), F.tokens - t0 - s0);
+        r.s_end = s0 + many;
+        r.pos0 = (int64_t)s.length - s.n + (i0 - s.first);
+        const int64_t last = min(r.pos0 + many - 1, table_tokens(c) - 1);
+        const int32_t pages = last < 0 ? 0 : (int32_t)(div_u32((uint32_t)last, c.div_page) + 1);
+        r.p_end = (int32_t)min((int64_t)pages, (int64_t)(span + 1) * F.span);
+        r.table_row = c.table + b * c.table_width;
+        return r;
+    };
+    const int32_t p_span = (int32_t)min((int64_t)span * F.span, (int64_t)INT32_MAX);
+    Run run = run_from(0);
+    if (F.tokens_of == 1 && run.p_end <= p_span) return;
+
+    // The rows in 127ths of their largest value, kRowsAtOnce a wavefront, 8 elements
+    // a lane.  (Rows behind the last head are that head's again, which changes no
+    // maximum; what is in no token's row is not used.)
+    constexpr int kLanes = STEPS * 4, kRowsAtOnce = kWave / kLanes;
+    const int used = one || F.tokens_of > 1 ? n_rows : F.per, d = lane % kLanes * 8;
+    for (int r0 = wave * kRowsAtOnce; r0 < used; r0 += kScoreWaves * kRowsAtOnce) {
+        const int row = r0 + lane / kLanes;
+        const int32_t slot = one ? 0 : row / 16 * F.slots + ((row & 15) >> F.per_bits);
+        const int32_t head = min(one ? row : row & (F.per - 1), P.group - 1);
+        const bool real = row < used && t0 + slot < F.tokens;
+        float q[8] = {}, most = 0.0f;
         if (real && d < D) {
             const u32x4 v = *(const u32x4*)(P.query + (F.token0 + t0 + slot) * P.query_token_stride +
                                             (int64_t)(kvh * P.group + head) * P.query_head_stride + d);
+            bool special = false;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 special |= not_finite2<F16>(v[i]);
                 q[2 * i] = to_float<F16>((uint16_t)v[i]);
                 q[2 * i + 1] = to_float<F16>((uint16_t)(v[i] >> 16));
             }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(q[i]));
+            if (special) most = INFINITY;
         }
-        float most = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(q[i]));
+        for (int o = 1; o < kLanes; o <<= 1) most = fmaxf(most, __shfl_xor(most, o));
+        const float z = most < INFINITY ? most * kInv127 : 0.0f;
+        // rint(q / z): by the reciprocal, whose product is off by less than 2^-14, and
+        // divided where that could round the other way
+        const float inverse = 1.0f / z;
+        float y[8];
+        bool near = !(z > 1e-30f);
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) most = fmaxf(most, __shfl_xor(most, o));
-        most = __shfl(most, 0);                             // (lanes 32 and up hold no elements)
-        const float z = __any(special) ? 0.0f : most * kInv127;
+        for (int i = 0; i < 8; ++i) {
+            y[i] = q[i] * inverse;
+            near |= fabsf(fabsf(y[i] - rintf(y[i])) - 0.5f) < 0x1p-13f;
+        }
+        if (near)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = z > 0.0f ? q[i] / z : 0.0f;
         float low[8], high[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float r = z > 0.0f ? rintf(q[i] / z) : 0.0f;
-            low[i] = fminf(r, 0.0f);
-            high[i] = fmaxf(r, 0.0f);
+            y[i] = rintf(y[i]);
+            low[i] = fminf(y[i], 0.0f);
+            high[i] = fmaxf(y[i], 0.0f);
         }
-        unsigned char* const to = rows_lds + row * kRowBytes<STEPS>;
-        if (d < D) {
-            *(uint2*)(to + d) = make_uint2(pack_bytes(low, 0), pack_bytes(low, 4));
-            *(uint2*)(to + D + d) = make_uint2(pack_bytes(high, 0), pack_bytes(high, 4));
+        if (row < used) {
+            unsigned char* const to = rows_lds + row * kRowBytes<STEPS>;
+            if (d < D) {
+                *(uint2*)(to + d) = make_uint2(pack_bytes(low, 0), pack_bytes(low, 4));
+                *(uint2*)(to + D + d) = make_uint2(pack_bytes(high, 0), pack_bytes(high, 4));
+            } else {
+                *(uint2*)(to + 2 * d) = make_uint2(0, 0);
+                *(uint2*)(to + 2 * d + 8) = make_uint2(0, 0);
+            }
+            if (d == 0) unit[row] = z;
         }
-        for (int o = 2 * D + lane * 8; o < STEPS * 64; o += kWave * 8) *(uint2*)(to + o) = make_uint2(0, 0);
-        if (lane == 0) unit[row] = z;
     }
     __syncthreads();
 
-    auto fragment = [&](int tile, int k) {
-        return *(const i32x4*)(rows_lds + (tile * 16 + n) * kRowBytes<STEPS> + 64 * k + 16 * g);
-    };
-    i32x4 q[STEPS];
-    float z[4];
-#pragma unroll
-    for (int k = 0; k < STEPS; ++k) q[k] = fragment(0, k);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) z[i] = unit[4 * g + i];
-
-    // The tile's tokens can be of several sequences, whose pages differ: each
-    // sequence in its turn.
-    for (int32_t s0 = 0; s0 < F.slots;) {
-        const int64_t i0 = F.token0 + t0 + s0;
-        if (t0 + s0 >= F.tokens) return;
-        int64_t b;
-        const bool of_one = find_seq(c, i0, &b);
-        const SeqRows s = of_one ? seq_rows(c, b) : SeqRows{};
-        if (!of_one || i0 < s.first || i0 - s.first >= s.n) {
+    // The tokens can be of several sequences, whose pages differ: each sequence
+    // in its turn.
+    for (int32_t s0 = 0; s0 < F.tokens_of && t0 + s0 < F.tokens;) {
+        if (s0 > 0) run = run_from(s0);
+        if (run.s_end == s0) {
             ++s0;
             continue;
         }
-        const int32_t many = (int32_t)min(min((int64_t)(F.slots - s0), s.first + s.n - i0), F.tokens - t0 - s0);
-        const int32_t s_end = s0 + many;
-        const int64_t pos0 = (int64_t)s.length - s.n + (i0 - s.first);
-        // pages that the last of these tokens sees
-        const int64_t last = min(pos0 + many - 1, table_tokens(c) - 1);
-        const int32_t pages = last < 0 ? 0 : (int32_t)(div_u32((uint32_t)last, c.div_page) + 1);
-        const int32_t p_end = (int32_t)min((int64_t)pages, (int64_t)(span + 1) * F.span);
-        const int32_t* const table_row = c.table + b * c.table_width;
-        for (int64_t p0 = (int64_t)span * F.span + wave * 16; p0 < p_end; p0 += kScoreWaves * 16) {
-            const int32_t j = (int32_t)p0 + n;
-            const int32_t page = j < p_end ? table_row[j] : -1;
-            const bool there = page >= 0 && page < c.n_pages;
-            const int64_t at = ((int64_t)(there ? page : 0) * c.n_kv_heads + kvh) * 2 * D;
-            i32x4 a[STEPS];
+        const int32_t s_end = run.s_end, p_end = run.p_end;
+        const int64_t pos0 = run.pos0;
+        const int32_t* const table_row = run.table_row;
+        const int32_t tile0 = one ? 0 : s0 / F.slots, tile1 = one ? F.tiles : (s_end - 1) / F.slots + 1;
+        const int64_t p_first = (int64_t)p_span + wave * kStep;
+        // a step of kStep pages, whose bytes come at once; lane l has page l of it
+        int32_t next = p_first + lane < p_end && lane < kStep ? table_row[p_first + lane] : -1;
+        for (int64_t p0 = p_first; p0 < p_end; p0 += kScoreWaves * kStep) {
+            const bool is_page = next >= 0 && next < c.n_pages;
+            const uint32_t is_there = (uint32_t)is_page;
+            const int32_t mine = is_page ? next : 0;
+            const float scale_of_lane = is_page ? P.scale[(int64_t)mine * P.scale_stride + kvh] : 0.0f;
+            i32x4 a[kSub][STEPS];
+            float scale[kSub];
+            bool there[kSub];
 #pragma unroll
-            for (int k = 0; k < STEPS; ++k) {
-                const int d = 64 * k + 16 * g;
-                a[k] = i32x4{0, 0, 0, 0};
-                if (there && d < 2 * D) a[k] = *(const i32x4*)(P.bounds + at + d);
-            }
-            const float scale = there ? P.scale[(int64_t)page * P.scale_stride + kvh] : 0.0f;
-            float top[4];
+            for (int u = 0; u < kSub; ++u) {
+                const int32_t page = __shfl(mine, u * 16 + n);
+                there[u] = __shfl((int)is_there, u * 16 + n) != 0;
+                const int8_t* const at = P.bounds + ((int64_t)page * c.n_kv_heads + kvh) * 2 * D;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) top[i] = -INFINITY;
-            for (int tile = 0; tile < F.tiles; ++tile) {
-                if (F.tiles > 1) {
-#pragma unroll
-                    for (int k = 0; k < STEPS; ++k) q[k] = fragment(tile, k);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) z[i] = unit[tile * 16 + 4 * g + i];
-                }
-                i32x4 acc = {0, 0, 0, 0};
-#pragma unroll
-                for (int k = 0; k < STEPS; ++k) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[k], a[k], acc, 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int row = 4 * g + i, head = F.tiles > 1 ? tile * 16 + row : row % F.per;
-                    if (head < P.group) top[i] = fmaxf(top[i], z[i] * (float)acc[i]);
+                for (int k = 0; k < STEPS; ++k) {
+                    const int d = 64 * k + 16 * g;
+                    a[u][k] = i32x4{0, 0, 0, 0};
+                    if (there[u] && d < 2 * D) a[u][k] = *(const i32x4*)(at + d);
                 }
             }
-            if (F.per >= 2) {
-                top[0] = fmaxf(top[0], top[1]);
-                top[2] = fmaxf(top[2], top[3]);
-            }
-            if (F.per >= 4) top[0] = fmaxf(top[0], top[2]);
-            if (F.per >= 8) top[0] = fmaxf(top[0], __shfl_xor(top[0], 16));
-            if (F.per >= 16) top[0] = fmaxf(top[0], __shfl_xor(top[0], 32));
-            if (j < p_end) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int32_t slot = (4 * g + i) / F.per;
-                    if ((4 * g + i) % F.per != 0 || slot < s0 || slot >= s_end) continue;
+            for (int u = 0; u < kSub; ++u) scale[u] = __shfl(scale_of_lane, u * 16 + n);
+            const int64_t p_next = p0 + kScoreWaves * kStep + lane;
+            next = p_next < p_end && lane < kStep ? table_row[p_next] : -1;
+
+            float top[kSub][V];
+            for (int tile = tile0; tile < tile1; ++tile) {
+                const unsigned char* const row_at = rows_lds + (tile * 16 + n) * kRowBytes<STEPS> + 16 * g;
+                i32x4 q[STEPS];
+                float z[4];
+#pragma unroll
+                for (int k = 0; k < STEPS; ++k) q[k] = *(const i32x4*)(row_at + 64 * k);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[i] = unit[tile * 16 + 4 * g + i];
+                // the page that each value's token is in (below 0: the lane writes no key)
+                int32_t cur[V];
+                int64_t to[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const int32_t row = 4 * g + v * (4 / V), at = row >> F.per_bits;
+                    const int32_t slot = one ? 0 : tile * F.slots + at;
                     const int64_t pos = pos0 + (slot - s0);
-                    uint32_t key = kNoPage;
-                    if (there && pos >= 0 && (int64_t)j * c.page_tokens <= pos) {
-                        const int32_t cur = (int32_t)div_u32((uint32_t)pos, c.div_page);
-                        if (j < P.first || j > cur - P.last) key = kAlways;
-                        else key = order_of(__builtin_isfinite(scale) ? top[i] * scale : INFINITY);
+                    const bool writes = (row & (F.per - 1)) == 0 && at < F.slots && slot >= s0 && slot < s_end;
+                    cur[v] = !writes ? -2 : pos < 0 ? -1 : (int32_t)div_u32((uint32_t)pos, c.div_page);
+                    to[v] = ((t0 + slot) * c.n_kv_heads + kvh) * c.table_width + p0 + n;
+                }
+#pragma unroll
+                for (int u = 0; u < kSub; ++u) {
+                    i32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+                    for (int k = 0; k < STEPS; ++k)
+                        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[k], a[u][k], acc, 0, 0, 0);
+                    float m[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) m[i] = z[i] * (float)acc[i];
+                    if constexpr (V == 2) {
+                        m[0] = fmaxf(m[0], m[1]);
+                        m[1] = fmaxf(m[2], m[3]);
                     }
-                    F.keys[((t0 + slot) * c.n_kv_heads + kvh) * c.table_width + j] = key;
+                    if constexpr (V == 1) {
+                        m[0] = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+                        if (F.per >= 8) m[0] = fmaxf(m[0], __shfl_xor(m[0], 16));
+                        if (F.per >= 16) m[0] = fmaxf(m[0], __shfl_xor(m[0], 32));
+                    }
+#pragma unroll
+                    for (int v = 0; v < V; ++v) top[u][v] = one && tile > 0 ? fmaxf(top[u][v], m[v]) : m[v];
+                    const int32_t j = (int32_t)p0 + u * 16 + n;
+                    if ((one && tile + 1 < tile1) || j >= p_end) continue;
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        if (cur[v] < -1) continue;
+                        uint32_t key = kNoPage;
+                        if (there[u] && j <= cur[v]) {
+                            if (j < P.first || j > cur[v] - P.last) key = kAlways;
+                            else key = order_of(__builtin_isfinite(scale[u]) ? top[u][v] * scale[u] : INFINITY);
+                        }
+                        F.keys[to[v] + u * 16] = key;
+                    }
                 }
             }
         }
@@ -300,18 +373,39 @@ __global__ __launch_bounds__(kScoreThreads) void score_kernel(ScoreLaunch F, int
 
 // ---------------------------------------------------------------- the choice
 
-constexpr int kPickThreads = 256, kPickWaves = kPickThreads / kWave;
-
 // The K best pages of one token and KV head, in ascending order: the K-th
-// largest key by its digits of 8 bits, from the top, then the pages above it and as
-// many of those equal to it, lowest first, as are left.
-__global__ __launch_bounds__(kPickThreads) void pick_kernel(ScoreLaunch F, int64_t first) {
+// largest key by digits of 8 bits, from the top bit in which the keys differ, then the
+// pages above it and as many of those equal to it, lowest first, as are left.  Bound
+// by latency: WAVES wavefronts keep HELD keys a lane in registers, the others are read
+// again for each digit.
+template <int WAVES, int HELD>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void pick_kernel(ScoreLaunch F, int64_t first) {
+    constexpr int kThreads = WAVES * kWave, kItems = WAVES == 1 ? 4 : 1;
+    struct Lds {
+        int32_t count[256];
+        uint32_t found[3];
+        uint32_t low[WAVES], high[WAVES];
+        int32_t above[WAVES], ties[WAVES];
+    };
+    __shared__ Lds all[kItems];
     const SelectPagesParams& P = F.s;
     const CacheView& c = P.c;
-    const int64_t x = blockIdx.x + first;
+    Lds& lds = all[WAVES == 1 ? threadIdx.x / kWave : 0];
+    const int wave = WAVES == 1 ? 0 : threadIdx.x / kWave, lane = lane_id(), tid = wave * kWave + lane;
+    auto sync = [] {
+        if constexpr (WAVES > 1) {
+            __syncthreads();
+        } else {
+            // (a wavefront's own LDS operations are in order; the compiler keeps them so)
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        }
+    };
+    const int64_t x = (blockIdx.x + first) * kItems + (WAVES == 1 ? threadIdx.x / kWave : 0);
     const int64_t i = F.token0 + x / c.n_kv_heads;
     int64_t b;
-    if (!find_seq(c, i, &b)) return;
+    if (x >= F.tokens * c.n_kv_heads || !find_seq(c, i, &b)) return;
     const SeqRows s = seq_rows(c, b);
     if (i < s.first || i - s.first >= s.n) return;
     const int64_t pos = (int64_t)s.length - s.n + (i - s.first);
@@ -320,95 +414,174 @@ __global__ __launch_bounds__(kPickThreads) void pick_kernel(ScoreLaunch F, int64
     const uint32_t* const keys = F.keys + x * c.table_width;
     int32_t* const out = P.selected + (F.token0 * c.n_kv_heads + x) * P.n_select;
 
-    __shared__ int32_t count[256];
-    __shared__ uint32_t found[2];
-    __shared__ int32_t wave_above[kPickWaves], wave_ties[kPickWaves];
-    const int wave = threadIdx.x / kWave, lane = lane_id();
-    uint32_t prefix = 0, mask = 0;
-    int32_t left = P.n_select;              // rank of the K-th among those that match the prefix
-    if (n <= P.n_select) {
-        // all that are candidates: keys above kNoPage
-        left = 0;
-    } else {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            count[threadIdx.x] = 0;
-            __syncthreads();
-            for (int32_t p = threadIdx.x; p < n; p += kPickThreads) {
-                const uint32_t k = keys[p];
-                if ((k & mask) == prefix) atomicAdd(&count[k >> shift & 255], 1);
+    // a wavefront's keys are consecutive: key p0 + 64 e + lane
+    const int32_t chunk = ((n + WAVES - 1) / WAVES + kWave - 1) / kWave * kWave;
+    const int32_t p0 = min(wave * chunk, n), p1 = min(p0 + chunk, n);
+    uint32_t held[HELD];
+#pragma unroll
+    for (int e = 0; e < HELD; ++e) held[e] = p0 + e * kWave + lane < p1 ? keys[p0 + e * kWave + lane] : kNoPage;
+    auto each = [&](auto f) {
+#pragma unroll
+        for (int e = 0; e < HELD; ++e)
+            if (e * kWave < p1 - p0) f(p0 + e * kWave + lane, held[e]);
+        for (int32_t p = p0 + HELD * kWave; p < p1; p += kWave) f(p + lane, p + lane < p1 ? keys[p + lane] : kNoPage);
+    };
+
+    uint32_t threshold = 0;
+    int32_t left = 0;                       // of the keys equal to the threshold
+    if (n > P.n_select) {
+        // the keys that are not taken anyway lie in [low, high]
+        uint32_t low = kAlways, high = 0;
+        int32_t always = 0, real = 0;
+        each([&](int32_t, uint32_t k) {
+            always += __popcll(__ballot(k == kAlways));
+            real += __popcll(__ballot(k != kNoPage));
+            if (k != kNoPage && k != kAlways) {
+                low = min(low, k);
+                high = max(high, k);
+            }
+        });
+#pragma unroll
+        for (int o = 1; o < kWave; o <<= 1) {
+            low = min(low, (uint32_t)__shfl_xor((int)low, o));
+            high = max(high, (uint32_t)__shfl_xor((int)high, o));
+        }
+        if constexpr (WAVES > 1) {
+            if (lane == 0) {
+                lds.low[wave] = low;
+                lds.high[wave] = high;
+                lds.above[wave] = always;
+                lds.ties[wave] = real;
             }
             __syncthreads();
-            if (wave == 0) {
-                // lane l has the digits 255 - 4 l .. 252 - 4 l
-                int32_t d[4], sum = 0;
+            always = real = 0;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    d[e] = count[255 - 4 * lane - e];
-                    sum += d[e];
-                }
-                const int32_t before = wave_incl_scan(sum) - sum;
-                int32_t at = before;
+            for (int w = 0; w < WAVES; ++w) {
+                low = min(low, lds.low[w]);
+                high = max(high, lds.high[w]);
+                always += lds.above[w];
+                real += lds.ties[w];
+            }
+            __syncthreads();
+        }
+        left = P.n_select - always;
+        if (real <= P.n_select) {
+            left = 0;                       // all candidates
+        } else if (left <= 0) {
+            threshold = kAlways;
+            left = P.n_select;
+        } else {
+            // digits from the highest bit in which low and high differ
+            int bits = low == high ? 0 : 32 - __builtin_clz(low ^ high);
+            uint32_t mask = bits >= 32 ? 0 : ~0u << bits;
+            threshold = high & mask;
+            while (bits > 0) {
+                const int take = min(bits, 8), shift = bits - take;
+                const uint32_t digits = (1u << take) - 1;
+                for (int k = tid; k < 256; k += kThreads) lds.count[k] = 0;
+                sync();
+                each([&](int32_t, uint32_t k) {
+                    if (k != kNoPage && k != kAlways && (k & mask) == threshold) atomicAdd(&lds.count[k >> shift & digits], 1);
+                });
+                sync();
+                if (wave == 0) {
+                    // lane l has the digits 255 - 4 l .. 252 - 4 l
+                    int32_t d[4], sum = 0;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (at < left && at + d[e] >= left) {
-                        found[0] = (uint32_t)(255 - 4 * lane - e);
-                        found[1] = (uint32_t)(left - at);
+                    for (int e = 0; e < 4; ++e) {
+                        d[e] = lds.count[255 - 4 * lane - e];
+                        sum += d[e];
                     }
-                    at += d[e];
+                    int32_t at = wave_incl_scan(sum) - sum;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (at < left && at + d[e] >= left) {
+                            lds.found[0] = (uint32_t)(255 - 4 * lane - e);
+                            lds.found[1] = (uint32_t)(left - at);
+                            lds.found[2] = (uint32_t)d[e];
+                        }
+                        at += d[e];
+                    }
                 }
+                sync();
+                threshold |= lds.found[0] << shift;
+                mask |= digits << shift;
+                left = (int32_t)lds.found[1];
+                const bool done = lds.found[2] == (uint32_t)left;       // all keys of this prefix
+                sync();
+                if (done && shift > 0) {
+                    // every key from here up is taken
+                    left = 0;
+                    threshold = threshold ? threshold - 1 : 0;
+                    break;
+                }
+                bits = shift;
             }
-            __syncthreads();
-            prefix |= found[0] << shift;
-            mask |= 255u << shift;
-            left = (int32_t)found[1];
         }
     }
-    // a key above `prefix`, or one equal to it among the first `left`; no
+    // a key above the threshold, or one equal to it among the first `left`; no
     // candidate (kNoPage) is never taken
-    const int32_t chunk = (n + kPickWaves - 1) / kPickWaves, p0 = wave * chunk, p1 = min(p0 + chunk, n);
     int32_t above = 0, ties = 0;
-    for (int32_t p = p0; p < p1; p += kWave) {
-        const uint32_t k = p + lane < p1 ? keys[p + lane] : kNoPage;
-        above += __popcll(__ballot(k > prefix));
-        ties += __popcll(__ballot(k == prefix && k != kNoPage));
-    }
-    if (lane == 0) {
-        wave_above[wave] = above;
-        wave_ties[wave] = ties;
-    }
-    __syncthreads();
-    int32_t a0 = 0, e0 = 0;
-    for (int w = 0; w < wave; ++w) {
-        a0 += wave_above[w];
-        e0 += wave_ties[w];
+    each([&](int32_t, uint32_t k) {
+        above += __popcll(__ballot(k > threshold));
+        ties += __popcll(__ballot(k == threshold && k != kNoPage));
+    });
+    int32_t a0 = 0, e0 = 0, all_above = above, all_ties = ties;
+    if constexpr (WAVES > 1) {
+        if (lane == 0) {
+            lds.above[wave] = above;
+            lds.ties[wave] = ties;
+        }
+        __syncthreads();
+        all_above = all_ties = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            a0 += w < wave ? lds.above[w] : 0;
+            e0 += w < wave ? lds.ties[w] : 0;
+            all_above += lds.above[w];
+            all_ties += lds.ties[w];
+        }
     }
     const uint64_t below = (1ull << lane) - 1;
-    for (int32_t p = p0; p < p1; p += kWave) {
-        const uint32_t k = p + lane < p1 ? keys[p + lane] : kNoPage;
-        const uint64_t ma = __ballot(k > prefix), me = __ballot(k == prefix && k != kNoPage);
-        const int32_t ra = a0 + __popcll(ma & below), re = e0 + __popcll(me & below);
-        if (k > prefix || (k == prefix && k != kNoPage && re < left)) out[ra + min(re, left)] = p + lane;
+    each([&](int32_t p, uint32_t k) {
+        const bool is_above = k > threshold, is_tie = k == threshold && k != kNoPage;
+        const uint64_t ma = __ballot(is_above), me = __ballot(is_tie);
+        const int32_t ra = a0 + (int32_t)__popcll(ma & below), re = e0 + (int32_t)__popcll(me & below);
+        if (is_above || (is_tie && re < left)) out[ra + min(re, left)] = p;
         a0 += __popcll(ma);
         e0 += __popcll(me);
-    }
-    int32_t all_above = 0, all_ties = 0;
-    for (int w = 0; w < kPickWaves; ++w) {
-        all_above += wave_above[w];
-        all_ties += wave_ties[w];
-    }
-    for (int32_t k = all_above + min(all_ties, left) + (int32_t)threadIdx.x; k < P.n_select; k += kPickThreads) out[k] = -1;
+    });
+    for (int32_t k = all_above + min(all_ties, left) + tid; k < P.n_select; k += kThreads) out[k] = -1;
+}
+
+// One wavefront holds up to 1024 pages (8192 choices of 683: 41.8 us with four
+// of them and digits from the top), four up to 4096.
+template <int WAVES, int HELD>
+hipError_t launch_pick(const ScoreLaunch& f, hipStream_t stream) {
+    const int64_t items = f.tokens * f.s.c.n_kv_heads, blocks = WAVES == 1 ? (items + 3) / 4 : items;
+    const int threads = WAVES == 1 ? 256 : WAVES * kWave;
+    return launch_all(blocks, threads, [&](dim3 grid, int64_t first) {
+        hipLaunchKernelGGL((pick_kernel<WAVES, HELD>), grid, dim3(threads), 0, stream, f, first);
+    });
 }
 
 int64_t key_bytes(const SelectPagesParams& p, int64_t tokens) {
     return tokens * p.c.n_kv_heads * p.c.table_width * (int64_t)sizeof(uint32_t);
 }
 
-template <bool F16, int STEPS>
-hipError_t launch_steps(const ScoreLaunch& f, int64_t blocks, hipStream_t stream) {
+template <bool F16, int STEPS, int V>
+hipError_t launch_values(const ScoreLaunch& f, int64_t blocks, hipStream_t stream) {
     const size_t lds = (size_t)f.tiles * 16 * (kRowBytes<STEPS> + sizeof(float));
     return launch_all(blocks, kScoreThreads, [&](dim3 grid, int64_t first) {
-        hipLaunchKernelGGL((score_kernel<F16, STEPS>), grid, dim3(kScoreThreads), lds, stream, f, first);
+        hipLaunchKernelGGL((score_kernel<F16, STEPS, V>), grid, dim3(kScoreThreads), lds, stream, f, first);
     });
+}
+
+template <bool F16, int STEPS>
+hipError_t launch_steps(const ScoreLaunch& f, int64_t blocks, hipStream_t stream) {
+    if (f.per == 1) return launch_values<F16, STEPS, 4>(f, blocks, stream);
+    if (f.per == 2) return launch_values<F16, STEPS, 2>(f, blocks, stream);
+    return launch_values<F16, STEPS, 1>(f, blocks, stream);
 }
 
 template <bool F16>
@@ -432,11 +605,18 @@ hipError_t launch_page_bounds(const BoundsParams& q, hipStream_t stream) {
     int lanes = 1;
     while (lanes * 8 < p.c.head_dim) lanes *= 2;
     const int64_t blocks = (p.slots * p.c.n_kv_heads + kBoundsWaves - 1) / kBoundsWaves;
+    const bool few = p.c.page_tokens <= 4 * (kWave / lanes);
     return launch_all(blocks, kBoundsThreads, [&](dim3 grid, int64_t first) {
-        if (p.f16) hipLaunchKernelGGL((bounds_kernel<true>), grid, dim3(kBoundsThreads), 0, stream, p, lanes, first);
-        else hipLaunchKernelGGL((bounds_kernel<false>), grid, dim3(kBoundsThreads), 0, stream, p, lanes, first);
+        const dim3 block(kBoundsThreads);
+        if (p.f16 && few) hipLaunchKernelGGL((bounds_kernel<true, 4>), grid, block, 0, stream, p, lanes, first);
+        else if (p.f16) hipLaunchKernelGGL((bounds_kernel<true, 8>), grid, block, 0, stream, p, lanes, first);
+        else if (few) hipLaunchKernelGGL((bounds_kernel<false, 4>), grid, block, 0, stream, p, lanes, first);
+        else hipLaunchKernelGGL((bounds_kernel<false, 8>), grid, block, 0, stream, p, lanes, first);
     });
 }
+
+// Tiles of rows that a workgroup scores the pages that it reads for.
+constexpr int kSharedTiles = 4;
 
 // Scores of up to so many bytes at once; of more tokens in several launches.
 constexpr int64_t kMostKeys = 256ll << 20;
@@ -451,28 +631,29 @@ hipError_t launch_select_pages(const SelectPagesParams& p, hipStream_t stream) {
     ScoreLaunch f{};
     f.s = p;
     f.per = 1;
-    while (f.per < p.group && f.per < 16) f.per *= 2;
-    f.tiles = (p.group + 15) / 16;
+    while (f.per < p.group && f.per < 16) f.per *= 2, ++f.per_bits;
     // tokens of one sequence share what is read; single ones of several do not
-    f.slots = p.c.q_offset && p.c.n_tokens > 2 * p.c.n_seqs ? 16 / f.per : 1;
+    const bool share = p.c.q_offset && p.c.n_tokens > 2 * p.c.n_seqs;
+    f.slots = share ? 16 / f.per : 1;
+    f.tiles = p.group > 16 ? (p.group + 15) / 16 : share ? kSharedTiles : 1;
+    f.tokens_of = p.group > 16 ? 1 : f.slots * f.tiles;
     f.keys = (uint32_t*)p.workspace;
     const int64_t one = key_bytes(p, 1);
     const int64_t slab = one ? std::min<int64_t>(p.c.n_tokens, (int64_t)(p.workspace_bytes / (uint64_t)one)) : p.c.n_tokens;
     for (f.token0 = 0; f.token0 < p.c.n_tokens; f.token0 += slab) {
         f.tokens = std::min(slab, p.c.n_tokens - f.token0);
-        const int64_t row_tiles = (f.tokens + f.slots - 1) / f.slots * p.c.n_kv_heads;
+        const int64_t row_tiles = (f.tokens + f.tokens_of - 1) / f.tokens_of * p.c.n_kv_heads;
         // spans of pages until the chip is full
-        const int64_t steps = ((int64_t)p.c.table_width + 63) / 64;
+        const int32_t round = kScoreWaves * (p.c.head_dim > 128 ? kPagesOfStep<8> : kPagesOfStep<4>);
+        const int64_t steps = ((int64_t)p.c.table_width + round - 1) / round;
         const int64_t want = std::max<int64_t>(1, std::min<int64_t>(steps, (2048 + row_tiles - 1) / std::max<int64_t>(row_tiles, 1)));
-        f.span = (int32_t)((steps + want - 1) / std::max<int64_t>(want, 1) * 64);
+        f.span = (int32_t)((steps + want - 1) / std::max<int64_t>(want, 1) * round);
         f.spans = f.span ? (int32_t)((p.c.table_width + (int64_t)f.span - 1) / f.span) : 0;
         hipError_t e = hipSuccess;
         if (f.spans > 0)
             e = p.f16 ? launch_scores<true>(f, row_tiles * f.spans, stream) : launch_scores<false>(f, row_tiles * f.spans, stream);
         if (e != hipSuccess) return e;
-        e = launch_all(f.tokens * p.c.n_kv_heads, kPickThreads, [&](dim3 grid, int64_t first) {
-            hipLaunchKernelGGL(pick_kernel, grid, dim3(kPickThreads), 0, stream, f, first);
-        });
+        e = p.c.table_width <= 1024 ? launch_pick<1, 16>(f, stream) : launch_pick<4, 16>(f, stream);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
