@@ -55,7 +55,7 @@ __host__ __device__ inline size_t list_bytes(const PagesLaunch& L) {
 __device__ __forceinline__ int32_t build_list(const PagesLaunch& L, int64_t b, int64_t token, int32_t kvh, int32_t many,
                                               int32_t w0, int32_t pages, uint32_t* bits, Entry* list, int32_t* wave_sum) {
     const CacheView& c = L.f.a.c;
-    const int wave = threadIdx.x / kWave;
+    const int wave = wave_number();
     const int32_t words = min(L.words, (pages - w0 + 31) / 32);
     for (int32_t k = threadIdx.x; k < many * words; k += kPagesThreads) bits[k] = 0;
     __syncthreads();
@@ -161,7 +161,7 @@ __global__ __launch_bounds__(kPagesThreads, DP > 128 ? 1 : 3) void attend_pages_
     const AttendParams& P = F.a;
     const CacheView& c = P.c;
     const int D = EXACT ? DP : c.head_dim;
-    const int wave = threadIdx.x / kWave, lane = lane_id(), n = lane & 15, g = lane >> 4;
+    const int wave = wave_number(), lane = lane_id(), n = lane & 15, g = lane >> 4;
 
     int64_t x = blockIdx.x + first;
     const int32_t part = (int32_t)(x % F.few.count);
@@ -437,7 +437,7 @@ __global__ __launch_bounds__(kPagesThreads, DP > 128 ? 1 : 3) void attend_pages_
 template <bool F16, int LANES>
 __global__ __launch_bounds__(kPagesThreads) void join_pages_kernel(AttendLaunch F, int64_t first) {
     const AttendParams& P = F.a;
-    const int64_t to = (blockIdx.x + first) * kPagesWaves + threadIdx.x / kWave, i = to / P.n_heads;
+    const int64_t to = (blockIdx.x + first) * kPagesWaves + wave_number(), i = to / P.n_heads;
     int64_t b;
     if (i >= P.c.n_tokens || !find_seq(P.c, i, &b)) return;
     const SeqRows s = seq_rows(P.c, b);

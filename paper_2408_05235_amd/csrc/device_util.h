@@ -41,6 +41,9 @@ __device__ __forceinline__ uint32_t ceil_div_u32(uint32_t x, DivU32 q) {
 // the write that feeds it, which is how the listings are checked for other uses of M0.
 #define TL_M0_WAIT ".long 0xbf800000"
 
+// The wavefront's number in its workgroup, in a scalar register.
+__device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)); }
+
 __device__ __forceinline__ int lane_id() { return (int)(threadIdx.x & (kWave - 1)); }
 
 // Wavefront scans by DPP (data movement inside the VALU, no LDS round

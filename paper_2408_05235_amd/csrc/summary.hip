@@ -56,7 +56,7 @@ __device__ __forceinline__ uint32_t pack_bytes(const float (&x)[8], int from) {
 template <bool F16, int BATCH>
 __global__ __launch_bounds__(kBoundsThreads) void bounds_kernel(BoundsParams P, int lanes, int64_t first) {
     const CacheView& c = P.c;
-    const int64_t item = (blockIdx.x + first) * kBoundsWaves + threadIdx.x / kWave;
+    const int64_t item = (blockIdx.x + first) * kBoundsWaves + wave_number();
     const int64_t slot = item / c.n_kv_heads;
     const int32_t kvh = (int32_t)(item - slot * c.n_kv_heads);
     if (slot >= P.slots) return;
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(kScoreThreads) void score_kernel(ScoreLaunch F, int
     extern __shared__ __attribute__((aligned(16))) unsigned char rows_lds[];
     const SelectPagesParams& P = F.s;
     const CacheView& c = P.c;
-    const int wave = threadIdx.x / kWave, lane = lane_id(), n = lane & 15, g = lane >> 4;
+    const int wave = wave_number(), lane = lane_id(), n = lane & 15, g = lane >> 4;
     const int D = c.head_dim, n_rows = F.tiles * 16;
     float* const unit = (float*)(rows_lds + n_rows * kRowBytes<STEPS>);
     int64_t x = blockIdx.x + first;
@@ -390,8 +390,9 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void pick_kernel(
     __shared__ Lds all[kItems];
     const SelectPagesParams& P = F.s;
     const CacheView& c = P.c;
-    Lds& lds = all[WAVES == 1 ? threadIdx.x / kWave : 0];
-    const int wave = WAVES == 1 ? 0 : threadIdx.x / kWave, lane = lane_id(), tid = wave * kWave + lane;
+    const int w = wave_number(), lane = lane_id();
+    const int wave = WAVES == 1 ? 0 : w, tid = wave * kWave + lane;
+    Lds& lds = all[WAVES == 1 ? w : 0];
     auto sync = [] {
         if constexpr (WAVES > 1) {
             __syncthreads();
@@ -402,7 +403,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void pick_kernel(
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         }
     };
-    const int64_t x = (blockIdx.x + first) * kItems + (WAVES == 1 ? threadIdx.x / kWave : 0);
+    const int64_t x = (blockIdx.x + first) * kItems + (WAVES == 1 ? w : 0);
     const int64_t i = F.token0 + x / c.n_kv_heads;
     int64_t b;
     if (x >= F.tokens * c.n_kv_heads || !find_seq(c, i, &b)) return;
@@ -616,7 +617,7 @@ hipError_t launch_page_bounds(const BoundsParams& q, hipStream_t stream) {
 }
 
 // Tiles of rows that a workgroup scores the pages that it reads for.
-constexpr int kSharedTiles = 4;
+constexpr int kSharedTiles = 8;
 
 // Scores of up to so many bytes at once; of more tokens in several launches.
 constexpr int64_t kMostKeys = 256ll << 20;
@@ -646,7 +647,7 @@ hipError_t launch_select_pages(const SelectPagesParams& p, hipStream_t stream) {
         // spans of pages until the chip is full
         const int32_t round = kScoreWaves * (p.c.head_dim > 128 ? kPagesOfStep<8> : kPagesOfStep<4>);
         const int64_t steps = ((int64_t)p.c.table_width + round - 1) / round;
-        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(steps, (2048 + row_tiles - 1) / std::max<int64_t>(row_tiles, 1)));
+        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(steps, (4096 + row_tiles - 1) / std::max<int64_t>(row_tiles, 1)));
         f.span = (int32_t)((steps + want - 1) / std::max<int64_t>(want, 1) * round);
         f.spans = f.span ? (int32_t)((p.c.table_width + (int64_t)f.span - 1) / f.span) : 0;
         hipError_t e = hipSuccess;
