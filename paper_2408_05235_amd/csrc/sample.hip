@@ -138,13 +138,16 @@ struct Chunks {
 #pragma unroll 1
         for (; i < end; i += kStep) {
             float y[kPer];
-            if (end - i >= kPer) {
-                P::split(*(const typename P::vec*)(x + i), y);
-            } else {
-#pragma unroll
-                for (int e = 0; e < kPer; ++e) y[e] = i + e < end ? raw<DT>(x[i + e]) : -INFINITY;
-            }
+            piece(x, i, end, y);
             f(i, y);
+        }
+    }
+    __device__ static __forceinline__ void piece(const elem<DT>* x, int32_t i, int32_t end, float (&y)[kPer]) {
+        if (end - i >= kPer) {
+            P::split(*(const typename P::vec*)(x + i), y);
+        } else {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) y[e] = i + e < end ? raw<DT>(x[i + e]) : -INFINITY;
         }
     }
 };
@@ -273,19 +276,20 @@ __global__ __launch_bounds__(WAVES * kWave) void sample_kernel(SampleParams P, i
                 for (int e = 0; e < kPer; ++e)
                     if (b[e] < kBins - 1) atomicAdd(&lds.bins[b[e]], 1u);
             }, largest);
-        // its first place is looked for again in its chunk
+        // its first place, which only the best token needs, is looked for again in its chunk
         const float f = clean(m1);
         int32_t at = 0;
-        if (f > -INFINITY) {
+        if (!draws && f > -INFINITY) {
             at = V;
-            const int32_t end = min(V, (chunk_of + 1) * Row::kSize);
-#pragma unroll 1
-            for (int b = 0; b < Row::kBatch; ++b)
-#pragma unroll 1
-                for (int e = 0; e < kPer; ++e) {
-                    const int32_t i = chunk_of * Row::kSize + b * Row::kStep + tid * kPer + e;
-                    if (i < end && raw<DT>(x[i]) == f) at = min(at, i);
-                }
+            const int32_t from = chunk_of * Row::kSize + tid * kPer;
+#pragma unroll
+            for (int b = Row::kBatch - 1; b >= 0; --b) {
+                float y[kPer];
+                Row::piece(x, from + b * Row::kStep, V, y);
+#pragma unroll
+                for (int e = kPer - 1; e >= 0; --e)
+                    if (y[e] == f) at = from + b * Row::kStep + e;
+            }
         }
         top = (uint64_t)order_of(f) << 32 | (uint32_t)~at;
     }
@@ -714,30 +718,38 @@ __global__ __launch_bounds__(WAVES * kWave) void sample_kernel(SampleParams P, i
 
     // the chunk that it falls into, a stretch of it a thread
     constexpr int kStretch = Row::kSize / kThreads;
-    const int32_t t0 = (int32_t)min((int64_t)hit * Row::kSize + tid * kStretch, (int64_t)V), t1 = min(t0 + kStretch, V);
-    auto weight_at = [&](int32_t i, float f) -> uint64_t {
+    const int32_t t0 = hit * Row::kSize + tid * kStretch;
+    float y[Row::kBatch][kPer];
+#pragma unroll
+    for (int b = 0; b < Row::kBatch; ++b) Row::piece(x, t0 + b * kPer, V, y[b]);
+    uint64_t w[kStretch], sum = 0;
+#pragma unroll
+    for (int e = 0; e < kStretch; ++e) {
+        const float f = clean(y[e / kPer][e % kPer]);
         const uint32_t key = order_of(f);
         const bool is_above = !whole && bin(f) < low;
-        return (is_above ? key >= least_key : kept(key, (uint32_t)i)) ? weight_of(f) : 0;
-    };
-    uint64_t sum = 0;
-#pragma unroll 1
-    for (int32_t i = t0; i < t1; ++i) sum += weight_at(i, logit<DT>(x[i]));
+        w[e] = (is_above ? key >= least_key : kept(key, (uint32_t)(t0 + e))) ? weight_of(f) : 0;
+        sum += w[e];
+        if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+    }
     const uint64_t incl = wave_incl_scan_u64(sum);
     if (lane == kWave - 1) lds.wave[wave] = incl;
     __syncthreads();
     uint64_t before = incl - sum;
     for (int w = 0; w < wave; ++w) before += lds.wave[w];
     if (r < before || r >= before + sum) return;    // (one thread goes on)
-    for (int32_t i = t0; i < t1; ++i) {
-        const float f = logit<DT>(x[i]);
-        before += weight_at(i, f);
-        if (before > r) {
-            P.token[row] = i;
-            if (P.logprob) P.logprob[row] = (float)(exponent(f, m, inverse) - log((double)total / kUnit));
-            return;
+    int32_t token = -1;
+    float f = 0.0f;
+#pragma unroll
+    for (int e = 0; e < kStretch; ++e) {
+        before += w[e];
+        if (token < 0 && before > r) {
+            token = t0 + e;
+            f = clean(y[e / kPer][e % kPer]);
         }
     }
+    P.token[row] = token;
+    if (P.logprob) P.logprob[row] = (float)(exponent(f, m, inverse) - log((double)total / kUnit));
 }
 
 template <int DT, int WAVES, int CAP>
