@@ -663,6 +663,11 @@ def tl_attend_pages(query, key_pages, value_pages, page_table, length, selected,
 
 def _rows2(t, name, dtype=None, shape=None, device=None):
     """The stride between the rows of ``t`` [rows, columns]."""
+    if t is not None and t.is_cuda and (device is None or t.get_device() == device) and t.dim() == 2:
+        rows, cols = size = t.shape
+        step, one = t.stride()
+        if (dtype is None or t.dtype == dtype) and (shape is None or size == shape) and (one == 1 or cols <= 1):
+            return step if rows > 1 else cols
     if t is None or not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     if device is not None and t.get_device() != device:
@@ -672,10 +677,7 @@ def _rows2(t, name, dtype=None, shape=None, device=None):
     if t.dim() != 2 or shape is not None and t.shape != shape:
         raise ValueError(f"{name} must be " + ("[rows, columns]" if shape is None else f"{tuple(shape)}")
                          + f", got {tuple(t.shape)}")
-    rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
-        raise ValueError(f"{name} must have contiguous rows")
-    return t.stride(0) if rows > 1 else cols
+    raise ValueError(f"{name} must have contiguous rows")
 
 
 def tl_norm(x, weight, eps=1e-6, residual=None, group=None, out=None, sum_out=None):
@@ -693,11 +695,10 @@ def tl_norm(x, weight, eps=1e-6, residual=None, group=None, out=None, sum_out=No
         raise ValueError(f"x must be bfloat16, float16 or float32, got {dtype}")
     xs = _rows2(x, "x")
     rows, cols = shape
-    _need(weight, dtype, "weight", (cols,), device)
-    rs = 0 if residual is None else _rows2(residual, "residual", dtype, shape, device)
-    if group is None:
-        number, kept, scale = _lib.NORM_SAME, dtype, None
-    else:
+    if weight.get_device() != device or weight.dtype != dtype or weight.shape != (cols,) or not weight.is_contiguous():
+        _need(weight, dtype, "weight", (cols,), device)
+    number, kept, scale = _lib.NORM_SAME, dtype, None
+    if group is not None:
         number, kept = int(group), torch.float8_e4m3fn
         if number < 0 or number >> 31:
             raise ValueError(f"group {number} is neither 0 nor a power of two from 16 to 512")
@@ -706,14 +707,18 @@ def tl_norm(x, weight, eps=1e-6, residual=None, group=None, out=None, sum_out=No
         out = torch.empty(shape, dtype=kept, device=x.device)
     else:
         _need(out, kept, "out", shape, device)
-    if sum_out is not None:
-        if residual is None:
-            raise ValueError("sum_out needs residual")
-        _need(sum_out, dtype, "sum_out", shape, device)
-    elif residual is not None:
-        sum_out = torch.empty(shape, dtype=dtype, device=x.device)
-    a = _lib.NormArgs(_NORM_SIZE, kind, rows, cols, number, eps, 0, x.data_ptr(), _p(residual), weight.data_ptr(), xs,
-                      rs, out.data_ptr(), _p(scale), _p(sum_out))
+    rs = r = total = None
+    if residual is not None:
+        rs, r = _rows2(residual, "residual", dtype, shape, device), residual.data_ptr()
+        if sum_out is None:
+            sum_out = torch.empty(shape, dtype=dtype, device=x.device)
+        else:
+            _need(sum_out, dtype, "sum_out", shape, device)
+        total = sum_out.data_ptr()
+    elif sum_out is not None:
+        raise ValueError("sum_out needs residual")
+    a = _lib.NormArgs(_NORM_SIZE, kind, rows, cols, number, eps, 0, x.data_ptr(), r, weight.data_ptr(), xs, rs or 0,
+                      out.data_ptr(), None if scale is None else scale.data_ptr(), total)
     check(lib().tl_norm(ctypes.byref(a), _stream_on(device)))
     if group is None:
         return out if residual is None else (out, sum_out)

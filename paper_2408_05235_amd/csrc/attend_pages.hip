@@ -1,8 +1,8 @@
 // Attention of new tokens over the pages that a list names for each of them and
 // KV head (tl_attend_pages).
 //
-// Rows of a workgroup are up to 16: the query heads that share the KV head, of
-// one token or of several neighbouring ones of a sequence, whose lists are mostly
+// Rows of a workgroup are up to 16, or 32: the query heads that share the KV head,
+// of one token or of several neighbouring ones of a sequence, whose lists are mostly
 // alike; it reads every page that one of them names once.  The products are
 // few_rows': a step is 32 tokens a wavefront, K Q^T and V^T P^T, and a lane keeps one
 // row.
@@ -148,15 +148,25 @@ __device__ void row_alone_pages(const AttendParams& P, int64_t token, int32_t he
     }
 }
 
+// The wavefronts' sums of a workgroup.
+template <int DP, int TILES>
+struct PagesLds {
+    float sums[kPagesWaves][TILES * kFewRows][DP + 4];
+    float stats[kPagesWaves][TILES * kFewRows][2];
+};
+
+// TILES: of 16 rows, which share what is read and turned.  Two tiles where sequences
+// have many new tokens: 512 of two sequences, each with 48 of up to 683 pages of 24
+// tokens, 32 heads on 8, 88 us, and 117 with one.
 // Workgroups: part fastest, then the heads' tile, then the KV head, then the
 // tokens' tile (numbered through the batch with gaps: those of sequence b begin at
 // floor(q_offset[b] / slots) + b).
-template <bool F16, int DP, bool EXACT>
-__global__ __launch_bounds__(kPagesThreads, DP > 128 ? 1 : 3) void attend_pages_kernel(PagesLaunch L, int64_t first) {
+template <bool F16, int DP, bool EXACT, int TILES>
+__global__ __launch_bounds__(kPagesThreads, DP > 128 ? 1 : TILES > 1 ? 2 : 3) void attend_pages_kernel(PagesLaunch L, int64_t first) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_bytes[];
     __shared__ int32_t wave_sum[kPagesWaves];
     constexpr int WAVES = kPagesWaves;
-    constexpr int kSteps = DP / 32, kPer = DP / 16;
+    constexpr int kSteps = DP / 32, kPer = DP / 16, kRows = TILES * kFewRows;
     const AttendLaunch& F = L.f;
     const AttendParams& P = F.a;
     const CacheView& c = P.c;
@@ -190,28 +200,38 @@ __global__ __launch_bounds__(kPagesThreads, DP > 128 ? 1 : 3) void attend_pages_
     const int32_t many = (int32_t)min((int64_t)L.slots, s.n - s0);
     const int64_t token0 = s.first + s0;
     const int32_t pos0 = (int32_t)(s.length - s.n + s0);
-    const int32_t here = min(L.slots > 1 ? many * P.group : P.group - row_tile * kFewRows, kFewRows);
-    const bool real = n < here;
-    const int32_t slot = real && L.slots > 1 ? n / P.group : 0;
-    const int32_t head = kvh * P.group + (real ? row_tile * kFewRows + n - slot * P.group : 0);
+    const int32_t here = min(L.slots > 1 ? many * P.group : P.group - row_tile * kRows, kRows);
+    bool real[TILES];
+    int32_t slot[TILES];
+#pragma unroll
+    for (int y = 0; y < TILES; ++y) {
+        real[y] = y * kFewRows + n < here;
+        slot[y] = real[y] && L.slots > 1 ? (y * kFewRows + n) / P.group : 0;
+    }
     const int64_t last = min((int64_t)pos0 + many - 1, table_tokens(c) - 1);
     const int32_t pages = last < 0 ? 0 : (int32_t)(div_u32((uint32_t)last, c.div_page) + 1);
 
     uint32_t* const bits = (uint32_t*)lds_bytes;
     Entry* const list = (Entry*)(lds_bytes + (size_t)L.slots * L.words * sizeof(uint32_t));
 
-    f32x4 acc[kPer];
+    f32x4 acc[TILES][kPer];
+    float m[TILES], l[TILES];
+    u32x4 q[TILES][kSteps];
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) acc[j] = f32x4{0, 0, 0, 0};
-    float m = kNone, l = 0.0f;
-    u32x4 q[kSteps];
+    for (int y = 0; y < TILES; ++y) {
+        m[y] = kNone;
+        l[y] = 0.0f;
 #pragma unroll
-    for (int k = 0; k < kSteps; ++k) {
-        const int d = 32 * k + 8 * g;
-        q[k] = u32x4{0, 0, 0, 0};
-        if (real && (EXACT || d < D))
-            q[k] = *(const u32x4*)(P.query + (token0 + slot) * P.query_token_stride +
-                                   (int64_t)head * P.query_head_stride + d);
+        for (int j = 0; j < kPer; ++j) acc[y][j] = f32x4{0, 0, 0, 0};
+        const int32_t head = kvh * P.group + row_tile * kRows + y * kFewRows + n - slot[y] * P.group;
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            const int d = 32 * k + 8 * g;
+            q[y][k] = u32x4{0, 0, 0, 0};
+            if (real[y] && (EXACT || d < D))
+                q[y][k] = *(const u32x4*)(P.query + (token0 + slot[y]) * P.query_token_stride +
+                                          (int64_t)head * P.query_head_stride + d);
+        }
     }
     const uint16_t* const keys = c.key + (int64_t)kvh * c.head_stride;
     const uint16_t* const values = c.value + (int64_t)kvh * c.head_stride;
@@ -261,124 +281,114 @@ __global__ __launch_bounds__(kPagesThreads, DP > 128 ? 1 : 3) void attend_pages_
                 }
             }
             // the step's tokens that each row sees, by the row's token
-            uint32_t sees = 0, any = 0, all = ~0u;
+            uint32_t sees[TILES] = {}, any = 0, all = ~0u;
             for (int32_t t = 0; t < many; ++t) {
                 const uint32_t y = (uint32_t)__ballot((at.who >> t & 1) && at.t <= pos0 + t);
-                if (t == slot) sees = y;
+#pragma unroll
+                for (int z = 0; z < TILES; ++z) sees[z] = t == slot[z] ? y : sees[z];
                 any |= y;
                 all &= y;
             }
             if (v + WAVES < v_end) at = place_of(c, list, entries, (int64_t)(v + WAVES) * kFewTile + (lane & 31));
 
-            f32x4 sc[2];
+            u32x4 pw[TILES];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                sc[h] = f32x4{0, 0, 0, 0};
+            for (int y = 0; y < TILES; ++y) {
+                f32x4 sc[2];
 #pragma unroll
-                for (int e = 0; e < kSteps; ++e) sc[h] = mfma16<F16>(k[h][e], q[e], sc[h]);
-            }
-            if (all != ~0u) {
+                for (int h = 0; h < 2; ++h) {
+                    sc[h] = f32x4{0, 0, 0, 0};
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                    for (int e = 0; e < kSteps; ++e) sc[h] = mfma16<F16>(k[h][e], q[y][e], sc[h]);
+                }
+                if (all != ~0u)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (!(sees >> (16 * h + 4 * g + i) & 1)) sc[h][i] = -INFINITY;
-                // values that no row sees are not used, whatever they are
-                if (any != ~0u)
+                    for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        if (!(any >> (16 * (e / 4) + 4 * g + e % 4) & 1))
+                        for (int i = 0; i < 4; ++i)
+                            if (!(sees[y] >> (16 * h + 4 * g + i) & 1)) sc[h][i] = -INFINITY;
+                // the softmax's step: lanes n, n + 16, n + 32 and n + 48 hold row n
+                float top = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
+                                  fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                if (__any(top > m[y])) {
+                    const float m2 = fmaxf(m[y], top);
+                    const float keep = weight(m[y], m2, F.score_scale);
+                    m[y] = m2;
+                    l[y] *= keep;
 #pragma unroll
-                            for (int y = 0; y < kPer / 2; ++y) w[e][y] = 0;
-                    }
-            }
-            // the softmax's step: lanes n, n + 16, n + 32 and n + 48 hold row n
-            float top = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
-                              fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float m2 = fmaxf(m, top);
-            const float keep = weight(m, m2, F.score_scale);
-            m = m2;
-            float p[8];
+                    for (int j = 0; j < kPer; ++j) acc[y][j] *= keep;
+                }
+                float p[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) p[e] = weight(sc[e / 4][e % 4], m, F.score_scale, kLiftFew<F16>);
-            const float sum = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-            l = fmaf(l, keep, sum);     // of this lane's tokens
-            const u32x4 pw = {pack2<F16>(p[0], p[1]), pack2<F16>(p[2], p[3]), pack2<F16>(p[4], p[5]),
+                for (int e = 0; e < 8; ++e) p[e] = weight(sc[e / 4][e % 4], m[y], F.score_scale, kLiftFew<F16>);
+                l[y] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));     // of this lane's tokens
+                pw[y] = u32x4{pack2<F16>(p[0], p[1]), pack2<F16>(p[2], p[3]), pack2<F16>(p[4], p[5]),
                               pack2<F16>(p[6], p[7])};
+            }
+            // values that no row sees are not used, whatever they are
+            if (any != ~0u)
 #pragma unroll
-            for (int j = 0; j < kPer; ++j) acc[j] *= keep;
+                for (int e = 0; e < 8; ++e) {
+                    if (!(any >> (16 * (e / 4) + 4 * g + e % 4) & 1))
+#pragma unroll
+                        for (int y = 0; y < kPer / 2; ++y) w[e][y] = 0;
+                }
 #pragma unroll
             for (int j = 0; j < kPer; ++j) {
                 const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;
                 u32x4 a;
 #pragma unroll
                 for (int y = 0; y < 4; ++y) a[y] = __builtin_amdgcn_perm(w[2 * y + 1][j / 2], w[2 * y][j / 2], sel);
-                acc[j] = mfma16<F16>(a, pw, acc[j]);
+#pragma unroll
+                for (int y = 0; y < TILES; ++y) acc[y][j] = mfma16<F16>(a, pw[y], acc[y][j]);
             }
         }
         __syncthreads();                // the list is read
     }
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    if constexpr (F16) {
-        constexpr float kBack = 1.0f / 32768.0f;        // 2^-lift
-        l *= kBack;
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) acc[j] *= kBack;
-    }
-
-    // Values that some rows see and others do not reach the others as 0 x value,
-    // which is NaN where they are not finite.  Where sums are, the rows are computed one
-    // by one instead, a wavefront takes every fourth.
     bool special = false;
-    if (L.slots > 1)
 #pragma unroll
-        for (int j = 0; j < kPer; ++j)
+    for (int y = 0; y < TILES; ++y) {
+        l[y] += __shfl_xor(l[y], 16);
+        l[y] += __shfl_xor(l[y], 32);
+        constexpr float kBack = F16 ? 1.0f / 32768.0f : 1.0f;       // 2^-lift
+        l[y] *= kBack;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) special |= !__builtin_isfinite(acc[j][i]);
-    RowSums alone[kFewRows / WAVES];
+        for (int j = 0; j < kPer; ++j) {
+            acc[y][j] *= kBack;
+            // Values that some rows see and others do not reach the others as 0 x value,
+            // which is NaN where they are not finite.  Where sums are, the rows are
+            // computed one by one instead, a wavefront takes every fourth.
+#pragma unroll
+            for (int i = 0; i < 4; ++i) special |= L.slots > 1 && !__builtin_isfinite(acc[y][j][i]);
+        }
+    }
     const bool one_by_one = __syncthreads_or(special);
+    PagesLds<DP, TILES>& lds = *(PagesLds<DP, TILES>*)lds_bytes;
+    auto& sums = lds.sums;
+    auto& stats = lds.stats;
     if (one_by_one) {
+        // (the list and the sums share their memory: all rows before any sums)
+        RowSums alone[kRows / WAVES];
 #pragma unroll
-        for (int k = 0; k < kFewRows / WAVES; ++k) alone[k] = RowSums{{}, kNone, 0.0f};
+        for (int k = 0; k < kRows / WAVES; ++k) alone[k] = RowSums{{}, kNone, 0.0f};
         for (int64_t w0 = 0; w0 < pages; w0 += (int64_t)L.words * 32) {
             const int32_t entries = build_list(L, b, token0, kvh, many, (int32_t)w0, pages, bits, list, wave_sum);
             int32_t v_first, v_end;
             steps_of(entries, &v_first, &v_end);
 #pragma unroll
-            for (int k = 0; k < kFewRows / WAVES; ++k) {
+            for (int k = 0; k < kRows / WAVES; ++k) {
                 const int r = k * WAVES + wave, sl = L.slots > 1 ? r / P.group : 0;
                 if (r < here)
-                    row_alone_pages<F16>(P, token0 + sl, kvh * P.group + row_tile * kFewRows + r - sl * P.group,
-                                         pos0 + sl, 1u << sl, list, entries, (int64_t)v_first * kFewTile,
-                                         (int64_t)v_end * kFewTile, F.score_scale, alone[k]);
+                    row_alone_pages<F16>(P, token0 + sl, kvh * P.group + row_tile * kRows + r - sl * P.group, pos0 + sl,
+                                         1u << sl, list, entries, (int64_t)v_first * kFewTile, (int64_t)v_end * kFewTile,
+                                         F.score_scale, alone[k]);
             }
             __syncthreads();
         }
-    }
-
-    // join the wavefronts: acc[j][i] is element kPer * (4 g + i) + j of row n
-    FewLds<WAVES, DP>& lds = *(FewLds<WAVES, DP>*)lds_bytes;
-    auto& sums = lds.sums;
-    auto& stats = lds.stats;
-    if (!one_by_one) {
-        if (real) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < kPer; j += 4)
-                    *(f32x4*)&sums[wave][n][kPer * (4 * g + i) + j] =
-                        f32x4{acc[j][i], acc[j + 1][i], acc[j + 2][i], acc[j + 3][i]};
-            if (g == 0) {
-                stats[wave][n][0] = m;
-                stats[wave][n][1] = l;
-            }
-        }
-    } else {
-#pragma unroll
-        for (int k = 0; k < kFewRows / WAVES; ++k) {
+        for (int k = 0; k < kRows / WAVES; ++k) {
             const int r = k * WAVES + wave;
             RowSums y = alone[k];
             // the halves' tokens
@@ -401,6 +411,23 @@ __global__ __launch_bounds__(kPagesThreads, DP > 128 ? 1 : 3) void attend_pages_
                 }
             }
         }
+    } else {
+        // acc[y][j][i] is element kPer * (4 g + i) + j of row 16 y + n
+#pragma unroll
+        for (int y = 0; y < TILES; ++y) {
+            if (!real[y]) continue;
+            const int r = y * kFewRows + n;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < kPer; j += 4)
+                    *(f32x4*)&sums[wave][r][kPer * (4 * g + i) + j] =
+                        f32x4{acc[y][j][i], acc[y][j + 1][i], acc[y][j + 2][i], acc[y][j + 3][i]};
+            if (g == 0) {
+                stats[wave][r][0] = m[y];
+                stats[wave][r][1] = l[y];
+            }
+        }
     }
     __syncthreads();
     for (int e = threadIdx.x; e < here * (DP / 4); e += kPagesThreads) {
@@ -419,7 +446,7 @@ __global__ __launch_bounds__(kPagesThreads, DP > 128 ? 1 : 3) void attend_pages_
             for (int i = 0; i < 4; ++i) o[i] = fmaf(y[i], f, o[i]);
         }
         const int32_t sl = L.slots > 1 ? r / P.group : 0;
-        const int64_t to = (token0 + sl) * P.n_heads + kvh * P.group + row_tile * kFewRows + r - sl * P.group;
+        const int64_t to = (token0 + sl) * P.n_heads + kvh * P.group + row_tile * kRows + r - sl * P.group;
         if (F.few.count > 1) {
             const int64_t at = to * F.few.count + part;
             if (d < D && all != 0.0f) *(f32x4*)(F.few.sums + at * D + d) = o;
@@ -445,26 +472,40 @@ __global__ __launch_bounds__(kPagesThreads) void join_pages_kernel(AttendLaunch 
     join_row<F16, LANES, 1>(F, F.few, to, to, 1.0f);
 }
 
+// Workgroups of two tiles from which on they are taken.
+constexpr int64_t kTwoTiles = 256;
+
 int64_t out_slots(const AttendParams& p) { return p.c.n_tokens * p.n_heads; }
 
-// Tokens of a workgroup: several where sequences have several and their heads
-// leave room.
-int32_t tokens_of(const AttendPagesParams& q) {
+// Rows of a workgroup, and its tokens: several where sequences have several and
+// their heads leave room; twice as many where there are workgroups enough.
+struct RowTiles {
+    int32_t tiles, slots;
+};
+RowTiles tiles_of(const AttendPagesParams& q) {
     const AttendParams& p = q.a;
-    if (!p.c.q_offset || p.c.n_tokens <= 2 * p.c.n_seqs || p.group > kFewRows / 2) return 1;
-    return std::max(1, std::min({kFewRows / p.group, TL_MAX_SELECTED / std::max(q.n_select, 1)}));
+    const bool share = p.c.q_offset && p.c.n_tokens > 2 * p.c.n_seqs;
+    auto slots = [&](int32_t tiles) {
+        return std::max(1, std::min(tiles * kFewRows / p.group, TL_MAX_SELECTED / std::max(q.n_select, 1)));
+    };
+    if (!share || p.group > kFewRows) return {1, 1};
+    if (p.c.head_dim <= 128 && slots(2) > slots(1) && p.c.n_tokens / slots(2) * p.c.n_kv_heads >= kTwoTiles) return {2, slots(2)};
+    return {1, slots(1)};
 }
-int64_t workgroups(const AttendPagesParams& q, int32_t slots) {
+int64_t workgroups(const AttendPagesParams& q, const RowTiles& r) {
     const AttendParams& p = q.a;
-    const int64_t tiles = p.c.q_offset ? p.c.n_tokens / slots + p.c.n_seqs : p.c.n_seqs;
-    return tiles * p.c.n_kv_heads * ((p.group + kFewRows - 1) / kFewRows);
+    const int64_t tiles = p.c.q_offset ? p.c.n_tokens / r.slots + p.c.n_seqs : p.c.n_seqs;
+    return tiles * p.c.n_kv_heads * ((p.group + r.tiles * kFewRows - 1) / (r.tiles * kFewRows));
 }
 
 constexpr int kLeastTokens = kPagesWaves * kFewTile;
 int64_t wanted(const AttendPagesParams& q) {
-    const int64_t blocks = workgroups(q, tokens_of(q)), tokens = (int64_t)q.n_select * q.a.c.page_tokens;
-    if (tokens <= 2 * kLeastTokens) return 1;
-    int64_t n = std::min((768 + blocks - 1) / std::max<int64_t>(blocks, 1), (tokens + kLeastTokens - 1) / kLeastTokens);
+    const RowTiles r = tiles_of(q);
+    const int64_t blocks = workgroups(q, r), tokens = (int64_t)q.n_select * q.a.c.page_tokens;
+    // workgroups that the chip holds: three a CU, of two tiles two
+    const int64_t fill = r.tiles > 1 ? 512 : 768;
+    if (tokens <= 2 * kLeastTokens || (3 * blocks >= 2 * fill && tokens <= 16 * kLeastTokens)) return 1;
+    int64_t n = std::min((fill + blocks - 1) / std::max<int64_t>(blocks, 1), (tokens + kLeastTokens - 1) / kLeastTokens);
     while (n > 1 && 5 * n * n > 2 * tokens) --n;
     return n;
 }
@@ -478,16 +519,23 @@ int64_t parts_bytes(const AttendParams& p, int64_t parts) {
     return parts > 1 ? sums_bytes(p, parts) + aligned(out_slots(p) * parts * 2 * (int64_t)sizeof(float)) : 0;
 }
 
-template <bool F16, int DP>
-hipError_t launch_dim(const PagesLaunch& l, int64_t blocks, hipStream_t stream) {
-    const AttendParams& p = l.f.a;
-    const size_t lds = std::max(sizeof(FewLds<kPagesWaves, DP>), list_bytes(l));
-    hipError_t e = launch_all(blocks * l.f.few.count, kPagesThreads, [&](dim3 grid, int64_t first) {
+template <bool F16, int DP, int TILES>
+hipError_t launch_tiles(const PagesLaunch& l, int64_t blocks, hipStream_t stream) {
+    const size_t lds = std::max(sizeof(PagesLds<DP, TILES>), list_bytes(l));
+    return launch_all(blocks * l.f.few.count, kPagesThreads, [&](dim3 grid, int64_t first) {
         const dim3 block(kPagesThreads);
-        if (p.c.head_dim == DP)
-            hipLaunchKernelGGL((attend_pages_kernel<F16, DP, true>), grid, block, lds, stream, l, first);
-        else hipLaunchKernelGGL((attend_pages_kernel<F16, DP, false>), grid, block, lds, stream, l, first);
+        if (l.f.a.c.head_dim == DP)
+            hipLaunchKernelGGL((attend_pages_kernel<F16, DP, true, TILES>), grid, block, lds, stream, l, first);
+        else hipLaunchKernelGGL((attend_pages_kernel<F16, DP, false, TILES>), grid, block, lds, stream, l, first);
     });
+}
+
+template <bool F16, int DP>
+hipError_t launch_dim(const PagesLaunch& l, int32_t tiles, int64_t blocks, hipStream_t stream) {
+    const AttendParams& p = l.f.a;
+    hipError_t e = hipSuccess;
+    if constexpr (DP <= 128) e = tiles > 1 ? launch_tiles<F16, DP, 2>(l, blocks, stream) : launch_tiles<F16, DP, 1>(l, blocks, stream);
+    else e = launch_tiles<F16, DP, 1>(l, blocks, stream);
     if (e != hipSuccess || l.f.few.count == 1) return e;
     return launch_all((out_slots(p) + kPagesWaves - 1) / kPagesWaves, kPagesThreads, [&](dim3 grid, int64_t first) {
         hipLaunchKernelGGL((join_pages_kernel<F16, DP / 4>), grid, dim3(kPagesThreads), 0, stream, l.f, first);
@@ -495,10 +543,10 @@ hipError_t launch_dim(const PagesLaunch& l, int64_t blocks, hipStream_t stream) 
 }
 
 template <bool F16>
-hipError_t launch_type(const PagesLaunch& l, int64_t blocks, hipStream_t stream) {
-    if (l.f.a.c.head_dim <= 64) return launch_dim<F16, 64>(l, blocks, stream);
-    if (l.f.a.c.head_dim <= 128) return launch_dim<F16, 128>(l, blocks, stream);
-    return launch_dim<F16, 256>(l, blocks, stream);
+hipError_t launch_type(const PagesLaunch& l, int32_t tiles, int64_t blocks, hipStream_t stream) {
+    if (l.f.a.c.head_dim <= 64) return launch_dim<F16, 64>(l, tiles, blocks, stream);
+    if (l.f.a.c.head_dim <= 128) return launch_dim<F16, 128>(l, tiles, blocks, stream);
+    return launch_dim<F16, 256>(l, tiles, blocks, stream);
 }
 
 }  // namespace
@@ -514,8 +562,9 @@ hipError_t launch_attend_pages(const AttendPagesParams& q, hipStream_t stream) {
     l.f.score_scale = q.a.scale * kLog2e;
     l.selected = q.selected;
     l.n_select = q.n_select;
-    l.slots = tokens_of(q);
-    l.row_tiles = (q.a.group + kFewRows - 1) / kFewRows;
+    const RowTiles r = tiles_of(q);
+    l.slots = r.slots;
+    l.row_tiles = (q.a.group + r.tiles * kFewRows - 1) / (r.tiles * kFewRows);
     l.words = (int32_t)std::max<int64_t>(1, std::min<int64_t>(((int64_t)q.a.c.table_width + 31) / 32, kMostWords / l.slots));
     l.list = (int32_t)std::max<int64_t>(1, std::min<int64_t>((int64_t)l.slots * q.n_select, (int64_t)l.words * 32));
     int64_t want = wanted(q);
@@ -525,8 +574,8 @@ hipError_t launch_attend_pages(const AttendPagesParams& q, hipStream_t stream) {
         l.f.few.sums = (float*)q.a.workspace;
         l.f.few.stats = (float*)((unsigned char*)q.a.workspace + sums_bytes(q.a, want));
     }
-    const int64_t blocks = workgroups(q, l.slots);
-    return q.a.f16 ? launch_type<true>(l, blocks, stream) : launch_type<false>(l, blocks, stream);
+    const int64_t blocks = workgroups(q, r);
+    return q.a.f16 ? launch_type<true>(l, r.tiles, blocks, stream) : launch_type<false>(l, r.tiles, blocks, stream);
 }
 
 }  // namespace tl

@@ -46,31 +46,51 @@ __device__ __forceinline__ elem<DT> round_to(float x) {
     else return __builtin_bit_cast(uint16_t, (__bf16)x);
 }
 
-// n (1 .. 8) columns; the others are 0.
+// A piece as it lies in memory, n (1 .. 8) columns; the others are 0.
 template <int DT>
-__device__ __forceinline__ void load_piece(const elem<DT>* p, int n, float (&x)[kPer]) {
+struct Raw {
+    uint32_t v[DT == TL_F32 ? 8 : 4];
+};
+template <int DT>
+__device__ __forceinline__ Raw<DT> load_raw(const elem<DT>* p, int n) {
+    Raw<DT> r;
     if (n == kPer) {
         if constexpr (DT == TL_F32) {
             const piece32 a = *(const piece32*)p, b = *(const piece32*)(p + 4);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                // (values of their own: a bit cast of a vector's element takes the first one)
-                const uint32_t lo = a[i], hi = b[i];
-                x[i] = __builtin_bit_cast(float, lo);
-                x[4 + i] = __builtin_bit_cast(float, hi);
+                r.v[i] = a[i];
+                r.v[4 + i] = b[i];
             }
         } else {
             const piece16 a = *(const piece16*)p;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[2 * i] = to_f32<DT>((uint16_t)a[i]);
-                x[2 * i + 1] = to_f32<DT>((uint16_t)(a[i] >> 16));
-            }
+            for (int i = 0; i < 4; ++i) r.v[i] = a[i];
         }
-        return;
+        return r;
     }
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) x[i] = i < n ? to_f32<DT>(p[i]) : 0.0f;
+    for (int i = 0; i < kPer; ++i) {
+        if constexpr (DT == TL_F32) {
+            r.v[i] = i < n ? __builtin_bit_cast(uint32_t, p[i]) : 0;
+        } else {
+            const uint32_t x = i < n ? p[i] : 0;
+            r.v[i / 2] = i % 2 ? r.v[i / 2] | x << 16 : x;
+        }
+    }
+    return r;
+}
+template <int DT>
+__device__ __forceinline__ void expand(const Raw<DT>& r, float (&x)[kPer]) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        if constexpr (DT == TL_F32) x[i] = __builtin_bit_cast(float, r.v[i]);
+        else x[i] = to_f32<DT>((uint16_t)(r.v[i / 2] >> (16 * (i % 2))));
+    }
+}
+template <int DT>
+__device__ __forceinline__ void load_piece(const elem<DT>* p, int n, float (&x)[kPer]) {
+    expand<DT>(load_raw<DT>(p, n), x);
 }
 
 template <int DT>
@@ -197,12 +217,14 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(Nor
     const elem<DT>* const x = (const elem<DT>*)P.x + row * P.x_stride;
     const elem<DT>* const res = (const elem<DT>*)P.residual + row * P.residual_stride;
     const elem<DT>* const weight = (const elem<DT>*)P.weight;
-    float h[CH][kPer], w[CH][kPer];
+    float h[CH][kPer];
+    Raw<DT> w[CH];                                  // (as it lies: half the registers in 16 bits)
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int col = (c * THREADS + t) * kPer, n = min(W - col, kPer);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) h[c][i] = w[c][i] = 0.0f;
+        for (int i = 0; i < kPer; ++i) h[c][i] = 0.0f;
+        w[c] = Raw<DT>{};
         if (n > 0) {
             load_piece<DT>(x + col, n, h[c]);
             if constexpr (RES) {
@@ -211,7 +233,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(Nor
 #pragma unroll
                 for (int i = 0; i < kPer; ++i) h[c][i] += y[i];
             }
-            load_piece<DT>(weight + col, n, w[c]);
+            w[c] = load_raw<DT>(weight + col, n);
         }
     }
     float squares = 0.0f;
@@ -226,8 +248,10 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(Nor
         const int col = (c * THREADS + t) * kPer, n = min(W - col, kPer);
         if constexpr (RES)
             if (real && n > 0 && P.sum) store_piece<DT>((elem<DT>*)P.sum + row * W + col, n, h[c]);
+        float y[kPer];
+        expand<DT>(w[c], y);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) h[c][i] = h[c][i] * f * w[c][i];
+        for (int i = 0; i < kPer; ++i) h[c][i] = h[c][i] * f * y[i];
         if constexpr (OUT == kSame) {
             if (real && n > 0) store_piece<DT>((elem<DT>*)P.out + row * W + col, n, h[c]);
         } else if constexpr (OUT == kRowScale) {
@@ -340,6 +364,7 @@ hipError_t launch_out(const NormParams& p, hipStream_t stream) {
     if (pieces <= 128) return launch_row<DT, OUT, 1, 128>(p, stream);
     if (pieces <= 256) return launch_row<DT, OUT, 1, 256>(p, stream);
     if (pieces <= 512) return launch_row<DT, OUT, 2, 256>(p, stream);
+    if (pieces <= 768) return launch_row<DT, OUT, 3, 256>(p, stream);
     if (pieces <= 1024) return launch_row<DT, OUT, 4, 256>(p, stream);
     if (pieces <= 2048) return launch_row<DT, OUT, 4, 512>(p, stream);
     if (pieces <= 4096) return launch_row<DT, OUT, 4, 1024>(p, stream);

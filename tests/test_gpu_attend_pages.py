@@ -214,3 +214,31 @@ def test_streams_and_replays(gpu):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, call())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("heads,kv,dim", [(64, 8, 64), (40, 8, 128), (16, 16, 80)])
+def test_two_tiles_of_rows(gpu, heads, kv, dim, dtype):
+    """Chunks of many tokens, which go 32 rows a workgroup."""
+    print(f"attend_pages two tiles, {heads} on {kv} of {dim} {dtype}", flush=True)
+    for kind in ("alike", "any"):
+        c = cache_cases.make(13, dtype, heads, kv, dim, 16, [300, 0, 41], [301, 1, 260])
+        check(c, lists(13, c, 7, kind))
+
+
+def test_infinities_in_two_tiles(gpu):
+    c = cache_cases.make(14, "bf16", 64, 8, 64, 16, [400], [300], poison=False)
+    sel = lists(14, c, 5)
+    sel[:, :, 0] = 3
+    sel[:, :, 1:] = torch.where(sel[:, :, 1:] == 9, 8, sel[:, :, 1:])
+    sel[200, 2, 4] = 9
+    table = c["table"].cpu().long()
+    c["v"][table[0, 9], 2, 7, 11] = -math.inf
+    c["dense"][0][1][9 * 16 + 7, 2, 11] = -math.inf
+    got, _ = run(c, sel)
+    out, _, tol, _ = exact(c, sel)
+    assert bool((got[200, 16:24, 11] == -math.inf).all())
+    rest = torch.ones_like(got, dtype=torch.bool)
+    rest[200, 16:24, 11] = False
+    assert bool(torch.isfinite(got[rest]).all())
+    assert bool(((got.double() - out).abs() <= tol)[rest].all())
