@@ -161,7 +161,7 @@ struct PagesLds {
 // Workgroups: part fastest, then the heads' tile, then the KV head, then the
 // tokens' tile (numbered through the batch with gaps: those of sequence b begin at
 // floor(q_offset[b] / slots) + b).
-template <bool F16, int DP, bool EXACT, int TILES>
+template <bool F16, int DP, bool EXACT, int TILES, bool STREAM>
 __global__ __launch_bounds__(kPagesThreads, DP > 128 ? 1 : TILES > 1 ? 2 : 3) void attend_pages_kernel(PagesLaunch L, int64_t first) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_bytes[];
     __shared__ int32_t wave_sum[kPagesWaves];
@@ -257,7 +257,7 @@ __global__ __launch_bounds__(kPagesThreads, DP > 128 ? 1 : TILES > 1 ? 2 : 3) vo
                 const uint16_t* const p = keys + shuffle64(at0, 16 * h + n) + 8 * g;
 #pragma unroll
                 for (int e = 0; e < kSteps; ++e) {
-                    if (EXACT || 32 * e + 8 * g < D) k[h][e] = *(const u32x4*)(p + 32 * e);
+                    if (EXACT || 32 * e + 8 * g < D) k[h][e] = load_once<STREAM>(p + 32 * e);
                     else k[h][e] = u32x4{0, 0, 0, 0};
                 }
             }
@@ -274,7 +274,7 @@ __global__ __launch_bounds__(kPagesThreads, DP > 128 ? 1 : TILES > 1 ? 2 : 3) vo
                         w[e][1] = z.y;
                     } else {
                         u32x4 z = {0, 0, 0, 0};
-                        if (EXACT || kPer * n + y < D) z = *(const u32x4*)(p + y);
+                        if (EXACT || kPer * n + y < D) z = load_once<STREAM>(p + y);
 #pragma unroll
                         for (int u = 0; u < 4; ++u) w[e][y / 2 + u] = z[u];
                     }
@@ -519,14 +519,14 @@ int64_t parts_bytes(const AttendParams& p, int64_t parts) {
     return parts > 1 ? sums_bytes(p, parts) + aligned(out_slots(p) * parts * 2 * (int64_t)sizeof(float)) : 0;
 }
 
-template <bool F16, int DP, int TILES>
+template <bool F16, int DP, int TILES, bool STREAM>
 hipError_t launch_tiles(const PagesLaunch& l, int64_t blocks, hipStream_t stream) {
     const size_t lds = std::max(sizeof(PagesLds<DP, TILES>), list_bytes(l));
     return launch_all(blocks * l.f.few.count, kPagesThreads, [&](dim3 grid, int64_t first) {
         const dim3 block(kPagesThreads);
         if (l.f.a.c.head_dim == DP)
-            hipLaunchKernelGGL((attend_pages_kernel<F16, DP, true, TILES>), grid, block, lds, stream, l, first);
-        else hipLaunchKernelGGL((attend_pages_kernel<F16, DP, false, TILES>), grid, block, lds, stream, l, first);
+            hipLaunchKernelGGL((attend_pages_kernel<F16, DP, true, TILES, STREAM>), grid, block, lds, stream, l, first);
+        else hipLaunchKernelGGL((attend_pages_kernel<F16, DP, false, TILES, STREAM>), grid, block, lds, stream, l, first);
     });
 }
 
@@ -534,8 +534,9 @@ template <bool F16, int DP>
 hipError_t launch_dim(const PagesLaunch& l, int32_t tiles, int64_t blocks, hipStream_t stream) {
     const AttendParams& p = l.f.a;
     hipError_t e = hipSuccess;
-    if constexpr (DP <= 128) e = tiles > 1 ? launch_tiles<F16, DP, 2>(l, blocks, stream) : launch_tiles<F16, DP, 1>(l, blocks, stream);
-    else e = launch_tiles<F16, DP, 1>(l, blocks, stream);
+    if (l.slots == 1) e = launch_tiles<F16, DP, 1, true>(l, blocks, stream);
+    else if (tiles == 1) e = launch_tiles<F16, DP, 1, false>(l, blocks, stream);
+    else if constexpr (DP <= 128) e = launch_tiles<F16, DP, 2, false>(l, blocks, stream);
     if (e != hipSuccess || l.f.few.count == 1) return e;
     return launch_all((out_slots(p) + kPagesWaves - 1) / kPagesWaves, kPagesThreads, [&](dim3 grid, int64_t first) {
         hipLaunchKernelGGL((join_pages_kernel<F16, DP / 4>), grid, dim3(kPagesThreads), 0, stream, l.f, first);
