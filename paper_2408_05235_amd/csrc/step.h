@@ -20,6 +20,7 @@ struct NormParams {
     void* out;
     float* scale;
     void* sum;                      // nullable
+    bool past;                      // outputs past the caches
 };
 
 struct SampleParams {
