@@ -576,6 +576,8 @@ hipError_t launch_attend_pages(const AttendPagesParams& q, hipStream_t stream) {
         l.f.few.stats = (float*)((unsigned char*)q.a.workspace + sums_bytes(q.a, want));
     }
     const int64_t blocks = workgroups(q, r);
+    // (sequences without rows count here, which no check before has bounded)
+    if (q.a.c.n_seqs > INT32_MAX / q.a.c.n_kv_heads || blocks > INT32_MAX) return hipErrorInvalidConfiguration;
     return q.a.f16 ? launch_type<true>(l, r.tiles, blocks, stream) : launch_type<false>(l, r.tiles, blocks, stream);
 }
 

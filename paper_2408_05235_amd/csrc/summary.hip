@@ -598,6 +598,9 @@ hipError_t launch_scores(const ScoreLaunch& f, int64_t blocks, hipStream_t strea
 
 }  // namespace
 
+// More than this no memory could back (sequences without rows count too).
+constexpr int64_t kMostBlocks = INT32_MAX;
+
 int64_t bounds_slots(const CacheView& c) {
     return c.q_offset ? c.n_tokens / c.page_tokens + 2 * c.n_seqs : c.n_seqs;
 }
@@ -607,6 +610,7 @@ hipError_t launch_page_bounds(const BoundsParams& q, hipStream_t stream) {
     p.slots = bounds_slots(p.c);
     int lanes = 1;
     while (lanes * 8 < p.c.head_dim) lanes *= 2;
+    if (p.slots > kMostBlocks / p.c.n_kv_heads) return hipErrorInvalidConfiguration;
     const int64_t blocks = (p.slots * p.c.n_kv_heads + kBoundsWaves - 1) / kBoundsWaves;
     const bool few = p.c.page_tokens <= 4 * (kWave / lanes);
     return launch_all(blocks, kBoundsThreads, [&](dim3 grid, int64_t first) {
@@ -650,7 +654,7 @@ hipError_t launch_select_pages(const SelectPagesParams& p, hipStream_t stream) {
         const int32_t round = kScoreWaves * (p.c.head_dim > 128 ? kPagesOfStep<8> : kPagesOfStep<4>);
         const int64_t steps = ((int64_t)p.c.table_width + round - 1) / round;
         const int64_t want = std::max<int64_t>(1, std::min<int64_t>(steps, (4096 + row_tiles - 1) / std::max<int64_t>(row_tiles, 1)));
-        f.span = (int32_t)((steps + want - 1) / std::max<int64_t>(want, 1) * round);
+        f.span = (int32_t)std::min<int64_t>((steps + want - 1) / want * round, INT32_MAX);
         f.spans = f.span ? (int32_t)((p.c.table_width + (int64_t)f.span - 1) / f.span) : 0;
         hipError_t e = hipSuccess;
         if (f.spans > 0)

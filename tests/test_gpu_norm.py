@@ -134,6 +134,14 @@ def test_many_rows_and_none(gpu):
     from paper_2408_05235_amd import api
     x, w, _ = inputs(2, 70001, 24, "bf16", False)
     check(api.tl_norm(x, w, EPS, None, 16), x, w, None, 16)
+    # more elements than 32 bits count
+    x, w, _ = inputs(3, 8, 1 << 14, "bf16", False)
+    big = x.repeat(1 << 14, 1)
+    y = api.tl_norm(big, w, EPS)
+    check(y[-8:], x, w, None, None)
+    assert torch.equal(y[:8], y[-8:])
+    del big, y
+    x, w, _ = inputs(2, 70001, 24, "bf16", False)
     q, s = api.tl_norm(x[:0], w, EPS, None, 16)
     assert q.shape == (0, 24) and s.shape == (0, 2)
 

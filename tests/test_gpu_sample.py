@@ -157,6 +157,30 @@ def test_edges(gpu, V):
     assert np.array_equal(t.cpu().numpy()[keep], token[keep])
 
 
+@pytest.mark.parametrize("spread", [0.02, 0.3, 1.5, 6.0])
+def test_thresholds_among_many(gpu, spread):
+    """Flat rows and steep ones, with a top-p near 1, and a logit far above the first
+    ones of its row: thresholds where many tokens lie, or where the bins end."""
+    V = 131072
+    x, T, k, p, q, g = draw(21, 12, V, "f32", False, spread)
+    p[:] = [0.5, 0.9, 0.99, 0.999, 0.9999, 0.3, 0.97, 0.95, 0.6, 0.99, 0.999, 0.2]
+    k[8:10] = 40000, 100000
+    q[10] = 1e-4
+    T[:] = np.linspace(0.25, 1.6, 12)
+    x[5, 100000] = 40.0
+    x[6, 70000:70009] = 25.0
+    check(x, T, k, p, q, g)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_most_columns(gpu, dtype):
+    V = 1 << 22
+    x, T, k, p, q, g = draw(5, 2, V, dtype, False, 0.5)
+    p[0], k[1] = 0.9, 1000000
+    T[:] = 0.7
+    check(x, T, k, p, q, g)
+
+
 def test_defaults_strides_and_rows(gpu):
     from paper_2408_05235_amd import api
     x, T, k, p, q, g = draw(8, 700, 501, "bf16", False)
@@ -164,8 +188,10 @@ def test_defaults_strides_and_rows(gpu):
     u, token, _ = expect(x, T, k, p, q, g)
     wide = torch.zeros(1400, 510, dtype=torch.bfloat16)
     wide[::2, 4:505] = x
-    got = api.tl_sample(wide.cuda()[::2, 4:505], torch.from_numpy(u).cuda())
-    assert np.array_equal(got.cpu().numpy(), token)
+    for at in (4, 3):           # rows that begin at any element
+        wide[::2, at:at + 501] = x
+        got = api.tl_sample(wide.cuda()[::2, at:at + 501], torch.from_numpy(u).cuda())
+        assert np.array_equal(got.cpu().numpy(), token)
     assert api.tl_sample(x[:0].cuda(), torch.zeros(0, device="cuda")).shape == (0,)
     # one row, many numbers: as often as it weighs
     row = x[:1].expand(4000, -1).cuda()
