@@ -51,6 +51,14 @@ __device__ __forceinline__ uint32_t pack_bytes(const float (&x)[8], int from) {
     return w;
 }
 
+typedef __attribute__((ext_vector_type(2))) short s16x2;
+
+// The other bits of negative values turned round; its own inverse.
+__device__ __forceinline__ s16x2 turned(s16x2 x) { return x ^ ((x >> 15) & s16x2{0x7fff, 0x7fff}); }
+__device__ __forceinline__ s16x2 shuffled(s16x2 x, int o) {
+    return __builtin_bit_cast(s16x2, __shfl_xor(__builtin_bit_cast(int, x), o));
+}
+
 // A wavefront per slot and KV head: `lanes` lanes (a power of two of at least
 // head_dim / 8) take 8 elements each of a token, the others other tokens.
 template <bool F16, int BATCH>
@@ -74,10 +82,12 @@ __global__ __launch_bounds__(kBoundsThreads) void bounds_kernel(BoundsParams P, 
     const int piece = lane_id() & (lanes - 1), sub = lane_id() / lanes, per = kWave / lanes;
     const bool in = piece * 8 < c.head_dim;
     const uint16_t* const keys = c.key + (int64_t)page * c.page_stride + (int64_t)kvh * c.head_stride + piece * 8;
-    float hi[8], lo[8];
+    // Two elements a word, as 16-bit whole numbers that order as the floats do (a
+    // negative one's other bits turned round), whose packed maxima and minima take half
+    // the instructions of the floats'.  Infinities and NaN are beyond all others.
+    s16x2 hi[4], lo[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) hi[i] = -INFINITY, lo[i] = INFINITY;
-    bool special = false;
+    for (int i = 0; i < 4; ++i) hi[i] = s16x2{-32768, -32768}, lo[i] = s16x2{32767, 32767};
     if (in) {
         // (the last token again in the place of those behind it, which changes nothing)
         for (int r0 = sub; r0 < count; r0 += BATCH * per) {
@@ -89,40 +99,59 @@ __global__ __launch_bounds__(kBoundsThreads) void bounds_kernel(BoundsParams P, 
             for (int y = 0; y < BATCH; ++y)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    special |= not_finite2<F16>(v[y][i]);
-                    const float a = to_float<F16>((uint16_t)v[y][i]), z = to_float<F16>((uint16_t)(v[y][i] >> 16));
-                    hi[2 * i] = fmaxf(hi[2 * i], a);
-                    lo[2 * i] = fminf(lo[2 * i], a);
-                    hi[2 * i + 1] = fmaxf(hi[2 * i + 1], z);
-                    lo[2 * i + 1] = fminf(lo[2 * i + 1], z);
+                    const uint32_t w = v[y][i];
+                    const s16x2 x = turned(__builtin_bit_cast(s16x2, w));
+                    hi[i] = __builtin_elementwise_max(hi[i], x);
+                    lo[i] = __builtin_elementwise_min(lo[i], x);
                 }
         }
     }
     for (int o = lanes; o < kWave; o <<= 1)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            hi[i] = fmaxf(hi[i], __shfl_xor(hi[i], o));
-            lo[i] = fminf(lo[i], __shfl_xor(lo[i], o));
+        for (int i = 0; i < 4; ++i) {
+            hi[i] = __builtin_elementwise_max(hi[i], shuffled(hi[i], o));
+            lo[i] = __builtin_elementwise_min(lo[i], shuffled(lo[i], o));
         }
-    float most = 0.0f;
+    // the largest absolute value: of two's complements, -x - 1 orders as a negative's
+    // magnitude does
+    s16x2 top = {0, 0};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) most = in ? fmaxf(most, fmaxf(hi[i], -lo[i])) : most;
-    for (int o = 1; o < lanes; o <<= 1) most = fmaxf(most, __shfl_xor(most, o));
-    // (the same in every lane group; a product and not a quotient, as stated in tl.h)
-    const bool bad = __any(special);
+    for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, __builtin_elementwise_max(hi[i], ~lo[i]));
+    int32_t bits = in ? max((int32_t)top[0], (int32_t)top[1]) : 0;
+    for (int o = 1; o < lanes; o <<= 1) bits = max(bits, __shfl_xor(bits, o));
+    const bool bad = bits >= (F16 ? 0x7c00 : 0x7f80);
+    const float most = to_float<F16>((uint16_t)bits);
+    // (a product and not a quotient, as stated in tl.h)
     const float scale = bad ? INFINITY : most * kInv127;
     // (a largest value so small that its 127th is 0 counts as 0)
     const bool none = bad || scale == 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        hi[i] = none ? 0.0f : fminf(fmaxf(ceilf(hi[i] / scale), -127.0f), 127.0f);
-        lo[i] = none ? 0.0f : fminf(fmaxf(floorf(lo[i] / scale), -127.0f), 127.0f);
-    }
     const int64_t at = (int64_t)page * c.n_kv_heads + kvh;
-    if (sub == 0 && in) {
-        int8_t* const to = P.bounds + at * 2 * c.head_dim + piece * 8;
-        *(uint2*)to = make_uint2(pack_bytes(lo, 0), pack_bytes(lo, 4));
-        *(uint2*)(to + c.head_dim) = make_uint2(pack_bytes(hi, 0), pack_bytes(hi, 4));
+    int8_t* const to = P.bounds + at * 2 * c.head_dim + piece * 8;
+    // the quotients by the lanes that have the same elements: a word each, or two
+    const int words = per >= 4 ? 1 : 2;
+    for (int k = 0; k < words; ++k) {
+        const int word = sub * words + k;
+        s16x2 h = hi[0], l = lo[0];
+#pragma unroll
+        for (int i = 1; i < 4; ++i) {
+            h = word == i ? hi[i] : h;
+            l = word == i ? lo[i] : l;
+        }
+        h = turned(h);
+        l = turned(l);
+        uint32_t low = 0, high = 0;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float x = to_float<F16>((uint16_t)h[e]), y = to_float<F16>((uint16_t)l[e]);
+            const float a = none ? 0.0f : fminf(fmaxf(ceilf(x / scale), -127.0f), 127.0f);
+            const float z = none ? 0.0f : fminf(fmaxf(floorf(y / scale), -127.0f), 127.0f);
+            high |= ((uint32_t)(int32_t)a & 0xffu) << (8 * e);
+            low |= ((uint32_t)(int32_t)z & 0xffu) << (8 * e);
+        }
+        if (in && word < 4) {
+            *(uint16_t*)(to + 2 * word) = (uint16_t)low;
+            *(uint16_t*)(to + c.head_dim + 2 * word) = (uint16_t)high;
+        }
     }
     if (lane_id() == 0) P.scale[(int64_t)page * P.scale_stride + kvh] = scale;
 }
