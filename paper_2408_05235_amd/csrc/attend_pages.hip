@@ -6,6 +6,12 @@
 // alike; it reads every page that one of them names once.  The products are
 // few_rows': a step is 32 tokens a wavefront, K Q^T and V^T P^T, and a lane keeps one
 // row.
+//
+// Single tokens are bound by reading: 64 of them, 64 pages of 16 tokens for each of 8
+// KV heads (268 MB), take 48 us, 5.6 TB/s, past the caches.  Through them it is 45 us call
+// after call, but 107 in place of 56 behind other work that left its writes there, as an
+// iteration's other layers do.  Chunks are bound by the vector
+// instructions around the products (half of the cycles) and the waits between them.
 #include <hip/hip_runtime.h>
 
 #include <float.h>
@@ -472,7 +478,9 @@ __global__ __launch_bounds__(kPagesThreads) void join_pages_kernel(AttendLaunch 
     join_row<F16, LANES, 1>(F, F.few, to, to, 1.0f);
 }
 
-// Workgroups of two tiles from which on they are taken.
+// Workgroups of two tiles from which on they are taken: 512 tokens of one sequence with 48
+// pages each take 61 us so and 79 with one, 4 times 64 with 128 pages 71 and 106; 32 tokens
+// take 22 with one tile and 26 with two.
 constexpr int64_t kTwoTiles = 256;
 
 int64_t out_slots(const AttendParams& p) { return p.c.n_tokens * p.n_heads; }
@@ -502,8 +510,11 @@ constexpr int kLeastTokens = kPagesWaves * kFewTile;
 int64_t wanted(const AttendPagesParams& q) {
     const RowTiles r = tiles_of(q);
     const int64_t blocks = workgroups(q, r), tokens = (int64_t)q.n_select * q.a.c.page_tokens;
-    // workgroups that the chip holds: three a CU, of two tiles two
-    const int64_t fill = r.tiles > 1 ? 512 : 768;
+    // workgroups that the chip holds: three a CU, of two tiles two.  Single tokens take
+    // one a CU, as fewer parts are joined (8 sequences of 128 pages 22 us, 26 with three;
+    // 32 of them 54 and 60), and tokens that share their lists more, as a workgroup's union is
+    // longer than a list (4 times 8 tokens of 128 pages 31 us, 41 with one).
+    const int64_t fill = r.tiles > 1 ? 512 : r.slots > 1 ? 768 : 256;
     if (tokens <= 2 * kLeastTokens || (3 * blocks >= 2 * fill && tokens <= 16 * kLeastTokens)) return 1;
     int64_t n = std::min((fill + blocks - 1) / std::max<int64_t>(blocks, 1), (tokens + kLeastTokens - 1) / kLeastTokens);
     while (n > 1 && 5 * n * n > 2 * tokens) --n;

@@ -17,7 +17,9 @@ namespace tl {
 namespace {
 
 constexpr double kUnit = 0x1p40;
-constexpr int kShortRow = 2048;         // rows that one list holds
+// Rows that one list of four wavefronts holds: 4096 rows of 2000 with top-p take 216 us so
+// and 324 as longer ones do, 64 of them, which do not fill the card, 26 and 22.
+constexpr int kShortRow = 2048;
 
 template <int DT>
 using elem = std::conditional_t<DT == TL_F32, float, uint16_t>;
@@ -54,7 +56,7 @@ __device__ __forceinline__ double exponent(float x, float m, double inverse) {
 // e = n ln 2 / 64 + r, |r| < 0.0055, and five terms of exp(r), off by less than 2^-47
 // of itself.  The sum with 2^52 rounds to a whole number, which the mantissa then is.
 // (Half the instructions of the library's exponential, which sampling without filters
-// is bound by: 256 rows of 128000 take 119 us with that.)
+// is bound by: 256 rows of 128000 take 82 us with that and 69 so.)
 struct Weights {
     const double* table;        // 2^(j / 64), in LDS
     double m, inverse;          // (of an infinite largest logit: 1e300 and 1)
@@ -209,6 +211,10 @@ struct Kept {
     }
 };
 
+// Bound by the weights' arithmetic in 64 bits and the round trips of few wavefronts
+// (two a SIMD).  256 rows of 128000 normal fp32 logits: the best token 26 us, without
+// filters 69, top-k of 50 51, top-p of 0.9 94 us; 131 MB read once take 18.
+//
 // One workgroup a row.  The row is read twice and once in part: for its largest
 // logit and the counts of its bins, which say where the thresholds of top-k and top-p
 // can lie; then for the sums of what is surely kept (and, for top-p alone, of all), while
