@@ -553,8 +553,9 @@ def tl_page_bounds(key_pages, bounds, scale, page_table, length, n_tokens, q_off
     stride = _summaries(bounds, scale, n_pages, heads, dim, device)
     if q_offset is not None:
         _need(q_offset, torch.int64, "q_offset", (page_table.shape[0] + 1,), device)
-    if n_tokens >> 31:
+    if n_tokens >> 31 or page_table.shape[1] >> 31:
         _int32(n_tokens, "n_tokens")
+        _int32(page_table.shape[1], "table_width")
     a = _lib.PageBoundsArgs(_BOUNDS_SIZE, 0, v, n_tokens, _p(q_offset), bounds.data_ptr(), scale.data_ptr(), stride,
                             None if granted is None else _granted(granted, page_table.shape[0], device))
     check(lib().tl_page_bounds(ctypes.byref(a), _stream_on(device)))
@@ -590,6 +591,9 @@ def tl_select_pages(query, bounds, scale, page_table, length, page_tokens, n_sel
     if page_table is None or page_table.dim() != 2:
         raise ValueError("page_table must be [n_seqs, table_width]")
     n_seqs, width = page_table.shape
+    if (heads | kv_heads | dim | width) >> 31:
+        for name, n in (("heads", heads), ("n_kv_heads", kv_heads), ("head_dim", dim), ("table_width", width)):
+            _int32(n, name)
     if page_table.get_device() != index or page_table.dtype != torch.int32 or not page_table.is_contiguous():
         _need(page_table, torch.int32, "page_table", None, index)
     if (length is None or length.get_device() != index or length.dtype != torch.int32 or not length.is_contiguous()
@@ -637,6 +641,9 @@ def tl_attend_pages(query, key_pages, value_pages, page_table, length, selected,
             or selected.shape[:2] != (T, key_pages.shape[1]) or not selected.is_contiguous()):
         _need(selected, torch.int32, "selected", None, index)
         raise ValueError(f"selected must be [{T}, {key_pages.shape[1]}, n_select], got {tuple(selected.shape)}")
+    if (heads | selected.shape[2] | page_table.shape[1]) >> 31:
+        for name, n in (("heads", heads), ("n_select", selected.shape[2]), ("table_width", page_table.shape[1])):
+            _int32(n, name)
     if q_offset is not None:
         _need(q_offset, torch.int64, "q_offset", (page_table.shape[0] + 1,), index)
     if out is None:
@@ -695,6 +702,8 @@ def tl_norm(x, weight, eps=1e-6, residual=None, group=None, out=None, sum_out=No
         raise ValueError(f"x must be bfloat16, float16 or float32, got {dtype}")
     xs = _rows2(x, "x")
     rows, cols = shape
+    if cols >> 31:
+        _int32(cols, "columns")
     if weight.get_device() != device or weight.dtype != dtype or weight.shape != (cols,) or not weight.is_contiguous():
         _need(weight, dtype, "weight", (cols,), device)
     number, kept, scale = _lib.NORM_SAME, dtype, None
@@ -738,6 +747,8 @@ def tl_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, w
         raise ValueError(f"logits must be bfloat16, float16 or float32, got {logits.dtype}")
     stride = _rows2(logits, "logits")
     rows, cols = logits.shape
+    if cols >> 31:
+        _int32(cols, "columns")
     row = (rows,)
     _need(u, torch.float32, "u", row, device)
     for name, t in (("temperature", temperature), ("top_p", top_p), ("min_p", min_p)):

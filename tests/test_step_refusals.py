@@ -253,3 +253,37 @@ def test_shapes_and_types(monkeypatch):
         for call, needle in bad:
             with pytest.raises(ValueError, match=needle):
                 call()
+
+
+def test_sizes_beyond_32_bits(monkeypatch):
+    """Sizes whose low 32 bits would pass are refused, not cut to them."""
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    monkeypatch.setattr(api, "_raw_device", lambda: 0)
+    monkeypatch.setattr(api, "_raw_stream", lambda d: 0)
+    reached = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: reached.append(name) or 0
+    monkeypatch.setattr(api, "lib", Library)
+    far = (1 << 32) + 64
+    with FakeTensorMode():
+        t = tensors("cuda:0")
+        z = lambda *s, dtype=torch.bfloat16: torch.empty(s, dtype=dtype, device="cuda:0")
+        ints = lambda *s: z(*s, dtype=torch.int32)
+        calls = [
+            lambda: api.tl_norm(z(1, far), z(far)), lambda: api.tl_norm(z(1, far), z(far), group=0),
+            lambda: api.tl_sample(z(1, far), z(1, dtype=torch.float32)),
+            lambda: api.tl_attend_pages(t["query"], t["key_pages"], t["value_pages"], t["page_table"], t["length"],
+                                        ints(3, t["key_pages"].shape[1], far)),
+            lambda: api.tl_select_pages(t["query"][:, :1].expand(3, far, 64), t["bounds"], t["scale"], t["page_table"],
+                                        t["length"], 16, 2),
+            lambda: api.tl_select_pages(t["query"], t["bounds"], t["scale"], ints(t["page_table"].shape[0], far),
+                                        t["length"], 16, 2),
+            lambda: api.tl_attend_pages(t["query"][:, :1].expand(3, far, 64), t["key_pages"], t["value_pages"],
+                                        t["page_table"], t["length"], ints(3, t["key_pages"].shape[1], 2)),
+        ]
+        for call in calls:
+            with pytest.raises(ValueError, match="32 bits"):
+                call()
+    assert not [n for n in reached if "workspace" not in n], reached
