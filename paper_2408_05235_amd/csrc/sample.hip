@@ -408,7 +408,8 @@ __global__ __launch_bounds__(WAVES * kWave) void sample_kernel(SampleParams P, i
                 listed = false;
             }
         } else {
-            limited = false;                        // (all with a weight)
+            limited = false;                        // (all with a weight: top-p counts the row's)
+            counts_all = by_p;
             if (by_p) {
                 const float reach = p * all_sum, error = 5.0f * 0.29f / kPerT * sqrtf(all_square) + 1e-4f * all_sum;
                 int32_t mine_low = kBins - 2, mine_high = kBins - 2;
@@ -594,10 +595,13 @@ __global__ __launch_bounds__(WAVES * kWave) void sample_kernel(SampleParams P, i
             const double need = ceil((double)p * (double)total);
             left = need < 1.0 ? 1 : min((uint64_t)need, total);
             if (fine) left = of_p;
-            if (!whole && (left <= all_above || left > all_above + inside)) {
-                // (the estimate was wrong)
-                whole = true;
-            } else if (!whole) {
+            if (!whole) {
+                if (left <= all_above || left > all_above + inside) {
+                    // (the estimate was wrong: again, with the whole row's sum)
+                    whole = true;
+                    --stage;
+                    continue;
+                }
                 left -= all_above;
             }
         }
