@@ -159,8 +159,13 @@ struct Chunks {
 constexpr int kBins = 4096, kAboveBins = 2304;
 constexpr float kPerT = 59.0f;
 struct Binning {
-    float scale, shift;         // finite, scale < 0
-    __device__ __forceinline__ float place(float x) const { return fmaf(x, scale, shift); }
+    // (halves: a difference of two logits can be beyond fp32)
+    float half_from, per_half, shift;       // finite, per_half > 0
+    // The difference first, which is exact near `from`: by x times the scale, bins of logits
+    // that are large for the temperature would be off by more than there are.
+    __device__ __forceinline__ float place(float x) const {
+        return fmaf(fmaf(x, -0.5f, half_from), per_half, shift);
+    }
     // (monotone: each operation is; NaN goes to the last one, as -inf does)
     __device__ __forceinline__ float clamped(float x) const {
         return fmaxf(fminf(place(x), (float)(kBins - 1)), 0.0f);
@@ -242,9 +247,9 @@ __global__ __launch_bounds__(WAVES * kWave) void sample_kernel(SampleParams P, i
     const bool binned = V > CAP && (by_k || by_p);
 
     // the largest logit, and its first place: its key above the place's complement;
-    // the counts of the bins (without bins all of it is one that is not counted)
+    // the counts of the bins (without them all finite logits go to the list)
     uint64_t top = 0;
-    Binning bin = {-1e-38f, (float)kAboveBins};      // (one bin, and the last one)
+    Binning bin = {0.0f, 2e-38f, (float)kAboveBins};     // (a few bins, and the last one)
     if (binned) {
         // bins begin a little above the largest of a few
         float m0 = -INFINITY;
@@ -256,7 +261,7 @@ __global__ __launch_bounds__(WAVES * kWave) void sample_kernel(SampleParams P, i
         __syncthreads();
         for (int w = 0; w < WAVES; ++w) m0 = fmaxf(m0, lds.wave_low[w]);
         const float per = fminf(fmaxf(kPerT / T, 1e-37f), 1e30f), from = fminf(fmaxf(m0, -3e38f), 3e38f);
-        bin = {-per, fminf(fmaxf(from * per, -3e38f), 3e38f) + (float)kAboveBins};
+        bin = {0.5f * from, 2.0f * per, (float)kAboveBins};
     }
     {
         float m1 = -INFINITY, m2 = -INFINITY;       // a lane's largest, and of the chunk
@@ -446,7 +451,7 @@ __global__ __launch_bounds__(WAVES * kWave) void sample_kernel(SampleParams P, i
     uint64_t of_p = 0;                              // what top-p has to reach, if known
     if (CAP > kShortRow && fine) {
         const float finer = (float)(kBins - 2) / (float)(high - low + 1);
-        bin = {bin.scale * finer, fmaf(bin.shift - (float)low, finer, 1.0f)};
+        bin = {bin.half_from, bin.per_half * finer, fmaf(bin.shift - (float)low, finer, 1.0f)};
         for (int e = tid; e < kBins; e += kThreads) lds.fine[e] = 0;
         __syncthreads();
         uint64_t over = 0, under = 0;
