@@ -78,12 +78,16 @@ struct Weights {
 };
 
 // How a row's elements are read: 16 bytes a lane, rows from any element on.
-typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t piece16;
-typedef __attribute__((ext_vector_type(4), aligned(4))) uint32_t piece32;
 template <int DT>
 struct Piece {
     static constexpr int kPer = DT == TL_F32 ? 4 : 8;
-    typedef std::conditional_t<DT == TL_F32, piece32, piece16> vec;
+    typedef __attribute__((ext_vector_type(4))) uint32_t vec;
+    // (a struct of its own: a template's argument loses what a typedef says of alignment)
+    struct __attribute__((packed, aligned(sizeof(elem<DT>)))) Memory {
+        vec v;
+    };
+    static_assert(alignof(Memory) == alignof(elem<DT>) && sizeof(Memory) == sizeof(vec));
+    __device__ static __forceinline__ vec load(const elem<DT>* p) { return ((const Memory*)p)->v; }
     __device__ static __forceinline__ void split(vec v, float (&x)[kPer]) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -113,14 +117,14 @@ struct Chunks {
         typename P::vec v[kBatch], next[kBatch];
         if (V >= kSize)
 #pragma unroll
-            for (int b = 0; b < kBatch; ++b) next[b] = *(const typename P::vec*)(x + i + b * kStep);
+            for (int b = 0; b < kBatch; ++b) next[b] = P::load(x + i + b * kStep);
         for (; V - chunk * kSize >= kSize; ++chunk, i += kSize) {
 #pragma unroll
             for (int b = 0; b < kBatch; ++b) v[b] = next[b];
             // (the next chunk is on its way under this one's work)
             if (V - chunk * kSize >= 2 * kSize)
 #pragma unroll
-                for (int b = 0; b < kBatch; ++b) next[b] = *(const typename P::vec*)(x + i + kSize + b * kStep);
+                for (int b = 0; b < kBatch; ++b) next[b] = P::load(x + i + kSize + b * kStep);
 #pragma unroll
             for (int b = 0; b < kBatch; ++b) {
                 float y[kPer];
@@ -146,7 +150,7 @@ struct Chunks {
     }
     __device__ static __forceinline__ void piece(const elem<DT>* x, int32_t i, int32_t end, float (&y)[kPer]) {
         if (end - i >= kPer) {
-            P::split(*(const typename P::vec*)(x + i), y);
+            P::split(P::load(x + i), y);
         } else {
 #pragma unroll
             for (int e = 0; e < kPer; ++e) y[e] = i + e < end ? raw<DT>(x[i + e]) : -INFINITY;
