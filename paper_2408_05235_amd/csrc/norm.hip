@@ -98,10 +98,12 @@ __device__ __forceinline__ void load_piece(const elem<DT>* p, int n, float (&x)[
 }
 
 // `past`: outputs that the caches would not hold until somebody reads them.
-template <class V>
-__device__ __forceinline__ void store(bool past, V v, V* to) {
-    if (past) __builtin_nontemporal_store(v, to);
-    else *to = v;
+// (ALIGN bytes: of a template's argument a typedef's alignment would be lost.)
+template <int ALIGN, class V>
+__device__ __forceinline__ void store(bool past, V v, void* to) {
+    typedef V there __attribute__((aligned(ALIGN)));
+    if (past) __builtin_nontemporal_store(v, (there*)to);
+    else *(there*)to = v;
 }
 
 template <int DT>
@@ -114,8 +116,8 @@ __device__ __forceinline__ void store_piece(elem<DT>* p, int n, const float (&x)
                 a[i] = __builtin_bit_cast(uint32_t, x[i]);
                 b[i] = __builtin_bit_cast(uint32_t, x[4 + i]);
             }
-            store(past, a, (piece32*)p);
-            store(past, b, (piece32*)(p + 4));
+            store<4>(past, a, p);
+            store<4>(past, b, p + 4);
         } else {
             piece16 a;
 #pragma unroll
@@ -124,7 +126,7 @@ __device__ __forceinline__ void store_piece(elem<DT>* p, int n, const float (&x)
                     a[i] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)x[2 * i], (_Float16)x[2 * i + 1]});
                 else a[i] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x[2 * i], (__bf16)x[2 * i + 1]});
             }
-            store(past, a, (piece16*)p);
+            store<2>(past, a, p);
         }
         return;
     }
@@ -150,7 +152,7 @@ __device__ __forceinline__ void store_e4m3(uint8_t* p, int n, const float (&y)[k
         q[i] = (uint32_t)w;
     }
     if (n == kPer) {
-        store(past, q, (piece8*)p);
+        store<1>(past, q, p);
         return;
     }
 #pragma unroll

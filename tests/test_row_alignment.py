@@ -1,4 +1,4 @@
-"""The sampling's kernels as the compiler makes them (CPU only): rows begin
+"""The norm's and the sampling's kernels as the compiler makes them (CPU only): rows begin
 at any element, so no access of several elements is taken for aligned to more than one of them."""
 import os
 import re
@@ -15,7 +15,7 @@ ACCESS = re.compile(r"\b(load|store) <(\d+) x (\w+)>.*ptr addrspace\(1\).*, alig
 
 
 @needs_hipcc
-@pytest.mark.parametrize("name", ["sample.hip"])
+@pytest.mark.parametrize("name", ["norm.hip", "sample.hip"])
 def test_accesses(tmp_path, name):
     flags = [f for f in build.HIPCC_FLAGS if f not in ("-shared", "-fPIC")]
     out = str(tmp_path / "out.ll")
