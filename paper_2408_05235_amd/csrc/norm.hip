@@ -135,13 +135,26 @@ __device__ __forceinline__ void store_piece(elem<DT>* p, int n, const float (&x)
         if (i < n) p[i] = round_to<DT>(x[i]);
 }
 
-// y times the scale's inverse, to e4m3: nearest even, NaN stays NaN.  (The
-// largest value of a scale is 448 times it up to a rounding, hence the clamp.)
-__device__ __forceinline__ void store_e4m3(uint8_t* p, int n, const float (&y)[kPer], float inverse, bool past) {
+// Division by a scale s: the product with 1 / s, corrected by what it leaves of y, which
+// is the quotient rounded once (P. Markstein, "Computation of elementary functions on the
+// IBM RISC System/6000 processor", 1990; 1 / s is rounded correctly).  By an infinite s
+// the product alone: 0, or NaN.
+struct Scale {
+    float value, inverse;
+    __device__ __forceinline__ explicit Scale(float s) : value(s == INFINITY ? 0.0f : s), inverse(1.0f / s) {}
+    __device__ __forceinline__ float quotient(float y) const {
+        const float q = y * inverse;
+        return fmaf(fmaf(-q, value, y), inverse, q);
+    }
+};
+
+// y / s to e4m3: nearest even, NaN stays NaN.  (The largest value of a scale is
+// 448 times it up to a rounding, hence the clamp.)
+__device__ __forceinline__ void store_e4m3(uint8_t* p, int n, const float (&y)[kPer], Scale s, bool past) {
     float z[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-        const float t = y[i] * inverse;
+        const float t = s.quotient(y[i]);
         z[i] = t != t ? t : fminf(fmaxf(t, -kMostE4m3), kMostE4m3);
     }
     piece8 q;
@@ -272,17 +285,18 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(Nor
         } else {
             const float s = scale_of(group_most(max_abs(h[c], 0), P.group / kPer));
             if (real && n > 0) {
-                store_e4m3((uint8_t*)P.out + row * W + col, n, h[c], 1.0f / s, P.past);
+                store_e4m3((uint8_t*)P.out + row * W + col, n, h[c], Scale(s), P.past);
                 if (col % P.group == 0) P.scale[row * ((W + P.group - 1) / P.group) + col / P.group] = s;
             }
         }
     }
     if constexpr (OUT == kRowScale) {
-        const float s = scale_of(reduce.most(most)), inverse = 1.0f / s;
+        const float s = scale_of(reduce.most(most));
+        const Scale by(s);
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * THREADS + t) * kPer, n = min(W - col, kPer);
-            if (real && n > 0) store_e4m3((uint8_t*)P.out + row * W + col, n, h[c], inverse, P.past);
+            if (real && n > 0) store_e4m3((uint8_t*)P.out + row * W + col, n, h[c], by, P.past);
         }
         if (real && t == 0) P.scale[row] = s;
     }
@@ -353,7 +367,7 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormParams P, int64_t f
         } else {
             if constexpr (OUT == kGroupScale) s = scale_of(group_most(max_abs(h, 0), P.group / kPer));
             if (n > 0) {
-                store_e4m3((uint8_t*)P.out + row * W + col, n, h, 1.0f / s, P.past);
+                store_e4m3((uint8_t*)P.out + row * W + col, n, h, Scale(s), P.past);
                 if constexpr (OUT == kGroupScale)
                     if (col % P.group == 0) P.scale[row * ((W + P.group - 1) / P.group) + col / P.group] = s;
             }
