@@ -224,6 +224,13 @@ __device__ __forceinline__ uint32_t group_most(uint32_t v, int lanes) {
 
 enum { kSame, kRowScale, kGroupScale };
 
+// What is behind a row's end has no say in a scale: where the root is infinite it would be
+// NaN (0 x inf).  (Without a branch around it: 16384 rows of 8192 take 155 us, 157 with one.)
+__device__ __forceinline__ void none_behind(float (&y)[kPer], int n) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) y[i] = i < n ? y[i] : 0.0f;
+}
+
 __device__ __forceinline__ float inverse_root(float squares, const NormParams& P) {
     return 1.0f / sqrtf(squares / (float)P.n_cols + P.eps);
 }
@@ -278,6 +285,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(Nor
         expand<DT>(w[c], y);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) h[c][i] = h[c][i] * f * y[i];
+        if constexpr (OUT != kSame) none_behind(h[c], n);
         if constexpr (OUT == kSame) {
             if (real && n > 0) store_piece<DT>((elem<DT>*)P.out + row * W + col, n, h[c], P.past);
         } else if constexpr (OUT == kRowScale) {
@@ -338,6 +346,7 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormParams P, int64_t f
         load_piece<DT>(weight + col, n, w);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) h[i] = h[i] * f * w[i];
+        if constexpr (OUT != kSame) none_behind(h, n);
     };
     float s = 0.0f;
     if constexpr (OUT == kRowScale) {
