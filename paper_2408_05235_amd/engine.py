@@ -69,6 +69,7 @@ class Engine:
             self.inputs = lambda n: self.embedding[torch.randint(vocabulary, (n,), generator=g, device=device)]
             self.numbers = lambda n: torch.rand(n, generator=g, device=device)
         if quantize:
+            self.one = torch.ones((), device=device)
             self.quantize = [self._eight_bits(w) for w in self.qkv + ([self.head] if vocabulary else [])]
         self.stopped = torch.zeros(len(self.tokens), dtype=torch.bool, device=device)
         self.iteration = 0
@@ -93,7 +94,11 @@ class Engine:
         total = x if residual is None else r[-1]
         if eight is None:
             return r[0] @ weight, total
-        return torch._scaled_mm(r[0], eight[0], scale_a=r[1][:, None], scale_b=eight[1], out_dtype=torch.bfloat16).to(x.dtype), total
+        if x.dtype == torch.bfloat16:
+            return torch._scaled_mm(r[0], eight[0], scale_a=r[1][:, None], scale_b=eight[1], out_dtype=x.dtype), total
+        # (the library scales rows in bf16 alone, three bits short of f16: here in fp32, rounded once)
+        y = torch._scaled_mm(r[0], eight[0], scale_a=self.one, scale_b=self.one, out_dtype=torch.float32)
+        return y.mul_(r[1][:, None]).mul_(eight[1]).to(x.dtype), total
 
     def _draw(self, x):
         """A token for each slot from its hidden state."""
