@@ -107,7 +107,8 @@ class Engine:
 
     def _attend(self, layer, query, q_offset):
         if self.select and q_offset is None:
-            pages = self.cache.select(layer, query, self.select, q_offset)
+            # (the last page always, and of two or more the first one)
+            pages = self.cache.select(layer, query, self.select, q_offset, first=min(1, self.select - 1))
             return self.cache.attend_pages(layer, query, pages, q_offset)
         return self.cache.attend(layer, query, q_offset, window=self.window, sinks=self.sinks, max_length=self.max_tokens)
 
