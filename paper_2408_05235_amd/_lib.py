@@ -23,6 +23,7 @@ BF16, F16, F32 = 1, 2, 3
 NORM_SAME = -1
 PAGES_OK, PAGES_NONE_FREE, PAGES_TABLE_FULL, PAGES_BAD = 0, 1, 2, 3
 MAX_HEAD_DIM = 256
+MAX_SELECTED, MAX_GROUP, MAX_COLUMNS = 4096, 128, 1 << 22
 MAX_HORIZON, MAX_BLOCK_TOKENS, MAX_FREQS, MAX_FEATURES, MAX_DEPTH = 8192, 65536, 4096, 4, 14
 
 EXPORTED = ("tl_abi_version", "tl_last_error", "tl_forest_create", "tl_forest_destroy",

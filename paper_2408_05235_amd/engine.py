@@ -32,7 +32,8 @@ class Engine:
     sinks as in tl_attend.
 
     ``norm``: a norm before each product, the residual's sum in the same call.
-    ``quantize``: the products behind a norm in e4m3, a scale a row (implies ``norm``).
+    ``quantize``: the products behind a norm in e4m3, a scale a row (implies ``norm``;
+    widths and the vocabulary are multiples of 16).
     ``select``: single tokens attend over so many pages, their choice by score (0: all).
     ``vocabulary``: inputs are the embeddings of tokens, drawn from the last hidden
     states' logits (0: random inputs); ``sampling`` holds tl_sample's settings, and
@@ -43,6 +44,18 @@ class Engine:
                  quantize=False, select=0, vocabulary=0):
         if select and (window or sinks):
             raise ValueError("select has no window")
+        if not 0 <= select <= _lib.MAX_SELECTED:
+            raise ValueError(f"select {select} outside [0, {_lib.MAX_SELECTED}]")
+        if select and n_heads > n_kv_heads * _lib.MAX_GROUP:
+            raise ValueError(f"select takes up to {_lib.MAX_GROUP} query heads per KV head, not {n_heads // n_kv_heads} query heads")
+        if not 0 <= vocabulary <= _lib.MAX_COLUMNS:
+            raise ValueError(f"vocabulary {vocabulary} outside [0, {_lib.MAX_COLUMNS}]")
+        # (what the library's product in 8 bits takes)
+        sizes = (("width", n_heads * head_dim), ("width of queries, keys and values", (n_heads + 2 * n_kv_heads) * head_dim),
+                 ("vocabulary", vocabulary))
+        for name, n in sizes if quantize else ():
+            if n % 16:
+                raise ValueError(f"quantize needs multiples of 16, not a {name} of {n}")
         self.tokens = np.asarray(prompt, np.int64) + np.asarray(generated, np.int64)
         self.remaining = np.asarray(remaining, np.int64)
         self.n_heads, self.n_kv_heads, self.head_dim = n_heads, n_kv_heads, head_dim
