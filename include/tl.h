@@ -735,7 +735,8 @@ tl_status tl_pages_copy(void* pages, int64_t n_pages, int64_t page_bytes, int64_
  * A row with a NaN or an infinity has NaN in its outputs (infinities 0 x inf; the
  * scales of what holds a NaN are NaN).
  * Rows may begin at any element.  out (group TL_NORM_SAME) and sum may be x or residual
- * themselves where those are contiguous; otherwise no output overlaps an input. */
+ * themselves where those are contiguous; otherwise no output overlaps an input, and none
+ * another output (which is refused). */
 typedef struct tl_norm_args {
     uint32_t struct_size;          /* sizeof(tl_norm_args) */
     int32_t dtype;                 /* TL_BF16, TL_F16 or TL_F32: of x, residual, weight, sum */

@@ -19,6 +19,16 @@ constexpr int64_t kMaxCount = 0x7fffffffll;
 bool known_type(int32_t dtype) { return dtype == TL_BF16 || dtype == TL_F16 || dtype == TL_F32; }
 bool aligned(const void* p, int32_t dtype) { return ((uintptr_t)p & (dtype == TL_F32 ? 3u : 1u)) == 0; }
 
+// A call's output: where it lies, and its bytes (0: there is none).
+struct Output {
+    const void* at;
+    uint64_t bytes;
+};
+bool overlap(const Output& a, const Output& b) {
+    const uintptr_t x = (uintptr_t)a.at, y = (uintptr_t)b.at;
+    return a.bytes && b.bytes && (x <= y ? y - x < a.bytes : x - y < b.bytes);
+}
+
 }  // namespace
 
 extern "C" {
@@ -48,6 +58,12 @@ tl_status tl_norm(const tl_norm_args* a, void* stream) {
         ((uintptr_t)a->scale & 3u) != 0)
         return fail(TL_EINVAL, "%s: pointers must be aligned to their elements", who);
     if (a->n_rows == 0) return ok();
+    const uint64_t rows = (uint64_t)a->n_rows, cols = (uint64_t)a->n_cols, size = a->dtype == TL_F32 ? 4 : 2;
+    const uint64_t scales = a->group < 0 ? 0 : a->group == 0 ? 1 : (cols + a->group - 1) / a->group;
+    const Output out{a->out, rows * cols * (a->group < 0 ? size : 1)}, scale{a->scale, rows * scales * sizeof(float)},
+        sum{a->sum, a->sum ? rows * cols * size : 0};
+    if (overlap(out, sum) || overlap(out, scale) || overlap(scale, sum))
+        return fail(TL_EINVAL, "%s: out, scale and sum must not overlap", who);
     tl::NormParams p{};
     p.n_rows = a->n_rows;
     p.n_cols = a->n_cols;
