@@ -20,7 +20,6 @@ struct NormParams {
     void* out;
     float* scale;
     void* sum;                      // nullable
-    bool past;                      // outputs past the caches
 };
 
 struct SampleParams {
