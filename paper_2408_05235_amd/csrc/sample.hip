@@ -220,13 +220,13 @@ struct Kept {
     }
 };
 
-// Bound by the weights' arithmetic in 64 bits and the round trips of few wavefronts
-// (two a SIMD).  256 rows of 128000 normal fp32 logits: the best token 26 us, without
-// filters 69, top-k of 50 51, top-p of 0.9 94 us; 131 MB read once take 18.
+// Bound by the round trips of few wavefronts (two a SIMD; with all filters they wait for 65%
+// of their cycles, and vector instructions, the weights' in 64 bits most of all, take 20%).  256 rows of 128000 normal fp32 logits: the best token 27 us, without
+// filters 70, top-k of 50 52, top-p of 0.9 95 us; 131 MB read once take 18.
 //
 // One workgroup a row.  The row is read twice and once in part: for its largest
 // logit and the counts of its bins, which say where the thresholds of top-k and top-p
-// can lie; then for the sums of what is surely kept (and, for top-p alone, of all), while
+// can lie; then for the sums of what is surely kept (and, for top-p of all that weighs, of all), while
 // the tokens of the bins between go to LDS, where the thresholds are found; and the
 // chunk that the number falls into.  Where those bins hold too many tokens the
 // thresholds are found by digits of the whole row's keys.
