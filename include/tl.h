@@ -727,7 +727,7 @@ tl_status tl_pages_copy(void* pages, int64_t n_pages, int64_t page_bytes, int64_
 
 /* With h = x (+ residual) per row of W columns, in fp32:
  *   sum = h, rounded to dtype
- *   y   = h / sqrt(mean h^2 + eps) x weight
+ *   y   = h x (1 / sqrt(mean h^2 + eps)) x weight
  * out is y rounded to dtype (group TL_NORM_SAME), or in 8 bits (e4m3: 4 exponent
  * bits, 3 of mantissa, no infinities), out = e4m3(y / s), nearest even:
  *   group 0   a scale a row,          s = max |y| / 448, at least 2^-100
